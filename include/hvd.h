@@ -339,6 +339,115 @@ hvd_status hvd_flow_trace(hvd_kv kv, uint64_t* dev_buf, int64_t n_words);
  * hvd_status. */
 int hvd_measure_mfma_peak(void* stream, double* tflops);
 
+/* ---------------------------------------------------------------------------
+ * Operators of an expert layer: the MLP block of a decoder layer whose rows
+ * each go through a few of many SwiGLU experts.  A verify step of such a
+ * target is hvd_route, hvd_experts_forward and hvd_block_norm in place of the
+ * dense MLP.
+ *
+ * Buffers are DEVICE memory of the current device, which is also the
+ * device of `stream`; matrices are row-major with unit column stride and a
+ * row stride given in elements.  Calls enqueue on `stream` (hipStream_t,
+ * NULL = default stream) and return without waiting; they allocate nothing
+ * and may be captured into a graph.  They hold no state between calls, so
+ * any number may run at once on buffers of their own.  rows = 0 does nothing.
+ * Bad arguments are HVD_ERR_ARG, and nothing is enqueued. */
+typedef enum { HVD_F16 = 0, HVD_BF16 = 1, HVD_F32 = 2 } hvd_dtype;
+typedef enum { HVD_SCORE_SOFTMAX = 0, HVD_SCORE_SIGMOID = 1 } hvd_score;
+
+/* Routing.  1 <= n_experts <= 512; 1 <= top_k <= min(16, n_experts);
+ * 1 <= n_groups <= 64 divides n_experts (groups are runs of experts, 1 = no
+ * grouping); 1 <= top_groups <= n_groups; top_k fits the top_groups groups. */
+typedef struct {
+  int32_t n_experts;
+  int32_t top_k;
+  int32_t score;       /* hvd_score */
+  int32_t n_groups;
+  int32_t top_groups;
+  int32_t renorm;      /* 1: the chosen scores are divided by their sum */
+  float scale;         /* factor of the weights */
+} hvd_route_config;
+
+/* Chooses top_k experts for each row of logits [rows][n_experts] (type
+ * logits_dtype).  s = softmax or sigmoid of the logits, c = s + bias (bias:
+ * nullable float [n_experts]).  A group counts the sum of its two best c; the
+ * top_groups best groups stay, and of their experts the top_k best c are
+ * chosen, best first, the lower index on ties.  ids [rows][top_k] receives
+ * them, weights [rows][top_k] their s (without the bias), over the sum of the
+ * chosen if renorm, times scale.  An expert whose logit is -inf or NaN is
+ * never chosen; places left over get id -1 and weight 0.  Scores are computed
+ * in 64 bits. */
+hvd_status hvd_route(const hvd_route_config* cfg, int32_t rows, const void* logits, int32_t logits_dtype,
+                     int64_t logits_stride, const float* bias, int32_t* ids, float* weights, void* stream);
+
+/* Experts of one layer: n_experts SwiGLU MLPs d_model -> ffn_dim -> d_model.
+ * 1 <= n_experts <= 512, d_model % 64 == 0, ffn_dim % 32 == 0; dtype HVD_F16
+ * or HVD_BF16. */
+typedef struct {
+  int32_t n_experts;
+  int32_t d_model;
+  int32_t ffn_dim;
+  int32_t dtype;
+} hvd_experts_config;
+typedef struct hvd_experts_s* hvd_experts;
+
+/* Device bytes of the packed weights (0 for an unsupported config). */
+size_t hvd_experts_bytes(const hvd_experts_config* cfg);
+
+/* Packs the weights: gate, up [n_experts][ffn_dim][d_model] and down
+ * [n_experts][d_model][ffn_dim], DEVICE, contiguous, 16-byte aligned, of the
+ * config's dtype.  The packing is enqueued on stream: the sources must stay
+ * as they are until it is done, and forward calls on other streams wait for
+ * it.  dev_buf (nullable, 16-byte aligned) must hold hvd_experts_bytes. */
+hvd_status hvd_experts_load(const hvd_experts_config* cfg, const void* gate, const void* up, const void* down,
+                            void* dev_buf, size_t dev_bytes, void* stream, hvd_experts* out);
+void hvd_experts_free(hvd_experts e);
+
+/* Workspace bytes of a forward call (0 for arguments it would refuse). */
+size_t hvd_experts_workspace(hvd_experts e, int32_t rows, int32_t top_k, int32_t x_dtype);
+
+/* out[t] = sum over j of weights[t][j] * down(silu(gate x[t]) * (up x[t])) of
+ * expert ids[t][j], for rows of x [rows][d_model]; 1 <= top_k <= 16, rows <=
+ * 262144.  x_dtype is the weights' type, or HVD_F32 with HVD_F16 weights: then
+ * activations run as fp16 hi + lo pairs (about 22 bits).  out [rows][d_model]
+ * has x's type.  ids outside [0, n_experts) (hvd_route's -1) add nothing,
+ * whatever their weight; a row without an expert is written 0; an id that
+ * comes twice counts twice.  The product silu * up is rounded to 16 bits (to
+ * the pair with HVD_F32); with HVD_F16 and HVD_F32 it and the activations must
+ * stay within fp16's range.  x, out and work are 16-byte aligned, their row
+ * strides multiples of 16 bytes; out may not overlap x.  work holds
+ * hvd_experts_workspace bytes and belongs to this call until it is done:
+ * calls that may overlap, and graphs that may run at once, need one each. */
+hvd_status hvd_experts_forward(hvd_experts e, int32_t rows, int32_t top_k, const void* x, int32_t x_dtype,
+                               int64_t x_stride, const int32_t* ids, const float* weights, void* out,
+                               int64_t out_stride, void* work, size_t work_bytes, void* stream);
+
+/* Norms before and after a block, with its gate and residual scale; for each
+ * row, with rms(v) = v / sqrt(mean(v^2) + eps):
+ *     v = rms(y) * post_gain,  x' = x + scale * gate * v,  h = rms(x') * gain.
+ * y NULL: x' = x.  post_gain NULL: v = y.  gate NULL: 1; its strides may be 0
+ * (one value for a row or a column).  x_out NULL: x' is not written; it has
+ * x's type and may be x itself.  h NULL (or gain NULL with h NULL): no h.
+ * gains are float [dim].  1 <= dim <= 16384, any alignment the types allow.
+ * Sums are 32-bit, and h is computed from x' before its rounding to x's type. */
+typedef struct {
+  const void* x;
+  int64_t x_stride;
+  const void* y;
+  int64_t y_stride;
+  const void* gate;
+  int64_t gate_row_stride, gate_col_stride;  /* column stride 0 or 1 */
+  const float* post_gain;
+  const float* gain;
+  void* x_out;
+  int64_t x_out_stride;
+  void* h;
+  int64_t h_stride;
+  int32_t x_dtype, y_dtype, gate_dtype, h_dtype;
+  float scale, eps;
+} hvd_block_norm_args;
+hvd_status hvd_block_norm(const hvd_block_norm_args* args, int32_t rows, int32_t dim, void* stream);
+
 /* Message of the last failing call on this thread ("" if none). */
 const char* hvd_last_error(void);
 

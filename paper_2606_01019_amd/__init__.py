@@ -14,3 +14,8 @@ from .hvd import (  # noqa: F401
     measure_mfma_peak,
     tensor_names,
 )
+from .operators import (  # noqa: F401
+    Experts,
+    block_norm,
+    route,
+)

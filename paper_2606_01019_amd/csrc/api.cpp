@@ -15,6 +15,7 @@
 
 #include "../../include/hvd.h"
 #include "attn_order.h"
+#include "error.h"
 #include "host_state.h"
 #include "kernels.h"
 
@@ -24,10 +25,18 @@ namespace {
 
 thread_local std::string g_err;
 
+}  // namespace
+
+namespace hvd {
+
 hvd_status set_err(hvd_status s, const std::string& m) {
   g_err = m;
   return s;
 }
+
+}  // namespace hvd
+
+namespace {
 
 #define HIP_TRY(expr)                                                                          \
   do {                                                                                         \

@@ -21,7 +21,8 @@ EXPORTS = ("hvd_model_bytes", "hvd_model_load", "hvd_model_free", "hvd_kv_bytes"
            "hvd_prefill", "hvd_verify", "hvd_verify_tree", "hvd_commit", "hvd_truncate", "hvd_seq_free", "hvd_seq_info",
            "hvd_kv_free_pages", "hvd_profile_enable", "hvd_profile_read", "hvd_kv_set_option", "hvd_last_error",
            "hvd_async_begin", "hvd_async_step", "hvd_async_end", "hvd_verify_noalloc", "hvd_flow_trace",
-           "hvd_measure_mfma_peak")
+           "hvd_measure_mfma_peak", "hvd_route", "hvd_experts_bytes", "hvd_experts_load", "hvd_experts_free",
+           "hvd_experts_workspace", "hvd_experts_forward", "hvd_block_norm")
 HVD_OPT_GRAPHS = 1
 HVD_OPT_MLP_SINGLE = 2
 HVD_OPT_LM_SINGLE = 3
@@ -81,7 +82,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     if not os.path.exists(path):
         raise RuntimeError(f"libhvd.so not built at {path}: run `python -m paper_2606_01019_amd.build`")
     L = ctypes.CDLL(path)
-    P, I32, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+    P, I32, SZ, I64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_int64
     PI32 = ctypes.POINTER(ctypes.c_int32)
     sig = {
         "hvd_model_bytes": (SZ, [ctypes.POINTER(Config)]),
@@ -109,6 +110,13 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "hvd_async_end": (I32, [P, PI32]),
         "hvd_flow_trace": (I32, [P, P, ctypes.c_int64]),
         "hvd_measure_mfma_peak": (I32, [P, ctypes.POINTER(ctypes.c_double)]),
+        "hvd_route": (I32, [P, I32, P, I32, I64, P, P, P, P]),
+        "hvd_experts_bytes": (SZ, [P]),
+        "hvd_experts_load": (I32, [P, P, P, P, P, SZ, P, ctypes.POINTER(P)]),
+        "hvd_experts_free": (None, [P]),
+        "hvd_experts_workspace": (SZ, [P, I32, I32, I32]),
+        "hvd_experts_forward": (I32, [P, I32, I32, P, I32, I64, P, P, P, I64, P, SZ, P]),
+        "hvd_block_norm": (I32, [P, I32, I32, P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
