@@ -381,7 +381,8 @@ hvd_status hvd_route(const hvd_route_config* cfg, int32_t rows, const void* logi
                      int64_t logits_stride, const float* bias, int32_t* ids, float* weights, void* stream);
 
 /* Experts of one layer: n_experts SwiGLU MLPs d_model -> ffn_dim -> d_model.
- * 1 <= n_experts <= 512, d_model % 64 == 0, ffn_dim % 32 == 0; dtype HVD_F16
+ * 1 <= n_experts <= 512, d_model % 64 == 0, ffn_dim % 32 == 0, both at most
+ * 131072; dtype HVD_F16
  * or HVD_BF16. */
 typedef struct {
   int32_t n_experts;

@@ -118,13 +118,16 @@ __global__ __launch_bounds__(256) void experts_sort(ExpertsArgs a) {
 
 // ---------------------------------------------------------------- row tiles
 
-// Row tile `tile` of BM rows over all experts' lists, found by every wave for
-// itself: lane l sums the tiles of 8 experts.
-struct RowTile {
-  int e, row0, rows;  // expert, first place, rows (0: no such tile)
+// The row tile and column block of a workgroup, found by every wave for itself
+// from the experts' slot counts: lane l sums the tiles of 8 experts.  Tiles are
+// numbered expert by expert, within one by column block, then row tile, and
+// each XCD takes a run of them: an expert's row tiles of one column block are
+// neighbours there and share its weights in that XCD's L2.
+struct Tile {
+  int e, row0, rows, cb;  // expert, first place, rows (0: no such tile), column block
 };
 template <int BM>
-__device__ __forceinline__ RowTile find_tile(const ExpertsArgs& a, int tile) {
+__device__ __forceinline__ Tile find_tile(const ExpertsArgs& a, int CB) {
   const int lane = threadIdx.x & 63;
   int nt[8], sum = 0;
 #pragma unroll
@@ -139,83 +142,561 @@ __device__ __forceinline__ RowTile find_tile(const ExpertsArgs& a, int tile) {
     const int v = __shfl_up(inc, o);
     if (lane >= o) inc += v;
   }
-  int before = inc - sum, e = -1, r = 0;
+  const int total = __builtin_amdgcn_readlane(inc, 63) * CB;
+  if ((int)blockIdx.x >= total) return {0, 0, 0, 0};
+  // XCD x (= id % 8 under the round-robin dispatch) takes the x-th run of positions
+  const int x = blockIdx.x & 7, q = total >> 3;
+  const int at = x * q + min(x, total & 7) + (blockIdx.x >> 3);
+  int before = (inc - sum) * CB, e = -1, r = 0, nte = 1;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    if (tile >= before && tile < before + nt[i]) {
+    if (at >= before && at < before + nt[i] * CB) {
       e = lane * 8 + i;
-      r = tile - before;
+      r = at - before;
+      nte = nt[i];
     }
-    before += nt[i];
+    before += nt[i] * CB;
   }
-  const uint64_t hit = __builtin_amdgcn_ballot_w64(e >= 0);
-  if (!hit) return {0, 0, 0};
-  const int src = __builtin_ctzll(hit);
+  const int src = __builtin_ctzll(__builtin_amdgcn_ballot_w64(e >= 0));
   e = __builtin_amdgcn_readlane(e, src);
   r = __builtin_amdgcn_readlane(r, src);
-  return {e, a.off[e] + r * BM, min(BM, a.cnt[e] - r * BM)};
+  nte = __builtin_amdgcn_readlane(nte, src);
+  const int cb = r / nte, tile = r - cb * nte;
+  return {e, a.off[e] + tile * BM, min(BM, a.cnt[e] - tile * BM), cb};
 }
 
-// ---------------------------------------------------------------- products
+// ---------------------------------------------------------------- products, many rows
 
-// 16 rows x 256 columns per workgroup, 64 columns per wave, operands straight
-// from global memory.  GU: rows of x gathered through perm, silu(gate) * up
-// out; else rows of that, the expert's output out.
-template <bool GU, bool BF, bool HL>
-__global__ __launch_bounds__(256) void experts_gemm(ExpertsArgs a) {
-  const RowTile rt = find_tile<16>(a, blockIdx.x);
-  if (rt.rows == 0) return;
-  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+// The grouped product on MFMA 32x32x16, the ring of gemm_tiled: a workgroup of
+// WY x WX waves owns BM = 32 WM WY places of one expert's list and BN = 32 WN WX
+// columns.  Every 32-wide K step's operands are copied straight into a ring of
+// LDS slots (global_load_lds), ST - 1 steps ahead of the MFMAs; the rows'
+// operand fragments are gathered there from wherever the rows are (each lane
+// copies 16 bytes of one row), so no gathered copy of x exists.  Places past
+// the list repeat its last one and are not stored; a tile belongs to one
+// expert.
+// GU: rows of x, silu(gate) * up out (OP: as a pair); else rows of that
+// product, the expert's output out.  AP: the row operand is a pair.
+template <int WY_, int WX_, int WM_, int WN_>
+struct TileShape {
+  static constexpr int WY = WY_, WX = WX_, WM = WM_, WN = WN_, NW = WY * WX;
+  static constexpr int BM = 32 * WM * WY, BN = 32 * WN * WX;
+};
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+template <bool BF>
+__device__ __forceinline__ f32x16 mfma32(const u32x4& a, const u32x4& b, f32x16 c) {
+  if constexpr (BF)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// Eight values as 16-bit elements, and what they leave over (the pair's lo part).
+template <bool BF>
+__device__ __forceinline__ void to16x8(const float (&v)[8], uint4& hi) {
+  uint32_t h[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = to16<BF>(v[2 * i]) | (uint32_t)to16<BF>(v[2 * i + 1]) << 16;
+  hi = uint4{h[0], h[1], h[2], h[3]};
+}
+template <bool BF>
+__device__ __forceinline__ float from16(uint16_t b) {
+  if constexpr (BF) return bf2f(b);
+  else return h2f(b);
+}
+template <bool BF>
+__device__ __forceinline__ void pair8(const float (&v)[8], uint4& hi, uint4& lo) {
+  to16x8<BF>(v, hi);
+  const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w};
+  float r[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r[2 * i] = v[2 * i] - from16<BF>((uint16_t)(h[i] & 0xFFFFu));
+    r[2 * i + 1] = v[2 * i + 1] - from16<BF>((uint16_t)(h[i] >> 16));
+  }
+  to16x8<BF>(r, lo);
+}
+
+constexpr int kRegionStride = 72;  // floats per row of a wave's epilogue region: rows 4 apart land 32 banks apart
+constexpr int kRegionBytes = 32 * kRegionStride * 4;
+
+template <class S, bool GU, bool BF, bool AP, bool OP>
+__global__ __launch_bounds__(64 * S::NW, 2) void experts_tiled(ExpertsArgs a, int CB) {
+  constexpr int NW = S::NW, WM = S::WM, WN = S::WN, BM = S::BM, BN = S::BN;
+  constexpr int AF = BM / 16, NA = AP ? 2 * AF : AF, WF = BN / 16, NF = NA + WF;
+  constexpr int LPT = NF / NW;
+  static_assert(NF % NW == 0, "fragments per step");
+  constexpr int BUDGET = NW == 8 ? 150 * 1024 : NW == 4 ? 76 * 1024 : 38 * 1024;
+  constexpr int ST0 = BUDGET / (NF * 1024);
+  constexpr int ST = ST0 < 3 ? 3 : (ST0 > 6 ? 6 : ST0);
+  __shared__ u32x4 sbuf[ST][NF][64];
+  static_assert(NW * kRegionBytes <= (int)sizeof(sbuf), "the epilogue's regions fit the ring");
+
+  const Tile tl = find_tile<BM>(a, CB);
+  if (tl.rows == 0) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wy = wave / S::WX, wx = wave % S::WX;
   const int D = a.w.D, F = a.w.F;
   const int K = GU ? D : F, N = GU ? 2 * F : D, KT = K / 32;
-  const int cb = blockIdx.y * 4 + wv;  // 64-column block
-  if (cb * 64 >= N) return;
-  const int p = rt.row0 + min(lane & 15, rt.rows - 1);
-  const uint16_t *ah, *al = nullptr;
-  if constexpr (GU) {
-    const int t = a.perm[p] / a.k;
-    if constexpr (HL) {
-      ah = a.xhi + (size_t)t * D;
-      al = a.xlo + (size_t)t * D;
-    } else {
-      ah = (const uint16_t*)a.x + t * a.x_stride;
-    }
-  } else {
-    ah = a.hhi + (size_t)p * F;
-    if constexpr (HL) al = a.hlo + (size_t)p * F;
-  }
-  const int kc = (lane >> 4) * 8;
-  const u32x4* w = (const u32x4*)(GU ? a.w.gu : a.w.dn) + ((size_t)rt.e * (N / 64) + cb) * KT * 256 + lane;
-  f32x4 acc[4];
+
+  const char* src[LPT];
+  uint32_t kstride[LPT];
 #pragma unroll
-  for (int s = 0; s < 4; ++s) acc[s] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int kt = 0; kt < KT; ++kt) {
-    const u32x4 h = *(const u32x4*)(ah + kt * 32 + kc);
-    u32x4 l = h;
-    if constexpr (HL) l = *(const u32x4*)(al + kt * 32 + kc);
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const u32x4 b = w[(size_t)kt * 256 + s * 64];
-      acc[s] = mfma16<BF>(h, b, acc[s]);
-      if constexpr (HL) acc[s] = mfma16<BF>(l, b, acc[s]);
-    }
-  }
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const int m = 4 * (lane >> 4) + r;
-    if (m >= rt.rows) continue;
-    const size_t row = rt.row0 + m;
-    if constexpr (GU) {
-#pragma unroll
-      for (int s = 0; s < 4; s += 2) {
-        const float v = silu(acc[s][r]) * acc[s + 1][r];
-        const size_t at = row * F + cb * 32 + s * 8 + (lane & 15);
-        if constexpr (HL) split_f16(v, a.hhi[at], a.hlo[at]);
-        else a.hhi[at] = to16<BF>(v);
+  for (int q = 0; q < LPT; ++q) {
+    const int f = q * NW + wave;
+    if (f < NA) {
+      const int p = tl.row0 + min(f % AF * 16 + (lane & 15), tl.rows - 1);
+      const uint16_t* row;
+      if constexpr (GU) {
+        const int t = a.perm[p] / a.k;
+        if constexpr (AP) row = (f < AF ? a.xhi : a.xlo) + (size_t)t * D;
+        else row = (const uint16_t*)a.x + t * a.x_stride;
+      } else {
+        row = (f < AF ? a.hhi : a.hlo) + (size_t)p * F;
       }
+      src[q] = (const char*)(row + (lane >> 4) * 8);
+      kstride[q] = 64;
     } else {
+      const int st = min(tl.cb * WF + (f - NA), N / 16 - 1);  // strips past the matrix: any valid one
+      src[q] = (const char*)((GU ? a.w.gu : a.w.dn) + (((size_t)tl.e * (N / 64) + (st >> 2)) * KT * 4 + (st & 3)) * 512 + lane * 8);
+      kstride[q] = 4096;
+    }
+  }
+  // Steps past the range re-copy the last one, so every iteration issues the
+  // same number of copies (constant vmcnt targets).
+  auto issue = [&](int slot, int kt) __attribute__((always_inline)) {
+    kt = min(kt, KT - 1);
 #pragma unroll
-      for (int s = 0; s < 4; ++s) a.y[row * D + cb * 64 + s * 16 + (lane & 15)] = acc[s][r];
+    for (int q = 0; q < LPT; ++q)
+      __builtin_amdgcn_global_load_lds((const void*)(src[q] + (size_t)kt * kstride[q]),
+                                       (lds_void*)&sbuf[slot][q * NW + wave][0], 16, 0, 0);
+  };
+
+  f32x16 acc[WM][WN];
+#pragma unroll
+  for (int i = 0; i < WM; ++i)
+#pragma unroll
+    for (int j = 0; j < WN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+  // 32 rows (columns) of one 16-wide K sub-step s: lane l takes row l%32, K 16s + 8(l/32)..+8
+  const int fl = (lane & 15) + 16 * (lane >> 5), fo = (lane >> 4) & 1;
+  struct Ops {
+    u32x4 ah[WM], al[AP ? WM : 1], bw[WN];
+  };
+  auto read_ops = [&](int buf, int s, Ops& o) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < WM; ++i) {
+      o.ah[i] = sbuf[buf][wy * 2 * WM + 2 * i + fo][fl + 32 * s];
+      if constexpr (AP) o.al[i] = sbuf[buf][AF + wy * 2 * WM + 2 * i + fo][fl + 32 * s];
+    }
+#pragma unroll
+    for (int j = 0; j < WN; ++j) o.bw[j] = sbuf[buf][NA + wx * 2 * WN + 2 * j + fo][fl + 32 * s];
+  };
+  auto mfma_ops = [&](const Ops& o, auto&& between) __attribute__((always_inline)) {
+    acc[0][0] = mfma32<BF>(o.ah[0], o.bw[0], acc[0][0]);
+    __builtin_amdgcn_sched_barrier(0);
+    between();
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < WM; ++i)
+#pragma unroll
+      for (int j = 0; j < WN; ++j) {
+        if (i != 0 || j != 0) acc[i][j] = mfma32<BF>(o.ah[i], o.bw[j], acc[i][j]);
+        if constexpr (AP) acc[i][j] = mfma32<BF>(o.al[i], o.bw[j], acc[i][j]);
+      }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // Step j lives in slot j % ST.  Iteration i multiplies the first half of step
+  // i while its second half is read; then it waits until step i+1 has landed,
+  // refills the slot of step i-1, and multiplies the second half while the
+  // first half of step i+1 is read.
+  {
+    Ops o0, o1;
+#pragma unroll
+    for (int st = 0; st < ST - 1; ++st) issue(st, st);
+    vm_wait<LPT * (ST - 2)>();
+    block_barrier();
+    read_ops(0, 0, o0);
+    int slot = 0;
+    for (int i = 0; i < KT; ++i) {
+      const int next = slot + 1 == ST ? 0 : slot + 1, prev = slot == 0 ? ST - 1 : slot - 1;
+      mfma_ops(o0, [&]() { read_ops(slot, 1, o1); });
+      vm_wait<LPT * (ST - 3)>();
+      block_barrier();
+      issue(prev, i + ST - 1);
+      mfma_ops(o1, [&]() { read_ops(next, 0, o0); });
+      slot = next;
+    }
+  }
+  vm_wait<0>();  // no copy may land after the ring is reused or released
+  __syncthreads();
+
+  // Blocks of 32 rows x 64 columns through the wave's LDS region, so that the
+  // stores are 16 bytes of one row per lane (MFMA 32x32: element r of lane l is
+  // row 8 (r/4) + 4 (l/32) + r%4, column l%32).
+  float* lds = (float*)&sbuf[0][0][0] + wave * (kRegionBytes / 4);
+#pragma unroll
+  for (int i = 0; i < WM; ++i) {
+#pragma unroll
+    for (int j = 0; j < WN; j += 2) {
+      const int col0 = tl.cb * BN + wx * 32 * WN + 32 * j, row0 = wy * 32 * WM + 32 * i;
+      if (col0 >= N || row0 >= tl.rows) continue;  // (wave-uniform)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float* p = lds + (8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * kRegionStride + (lane & 31);
+        p[0] = acc[i][j][r];
+        p[32] = acc[i][j + 1][r];
+      }
+      __builtin_amdgcn_wave_barrier();  // (one wave's LDS accesses execute in order)
+      auto oct = [&](int row, int c, float (&v)[8]) __attribute__((always_inline)) {
+        const float4 x = *(const float4*)(lds + row * kRegionStride + c), y = *(const float4*)(lds + row * kRegionStride + c + 4);
+        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+        v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+      };
+      if constexpr (GU) {
+        // a 32-column tile is one (gate strip, up strip) pair
+        const int o = lane & 3, c = 32 * (o >> 1) + 8 * (o & 1);
+#pragma unroll
+        for (int it = 0; it < 2; ++it) {
+          const int row = (lane >> 2) + 16 * it;
+          float g[8], u[8];
+          oct(row, c, g);
+          oct(row, c + 16, u);
+#pragma unroll
+          for (int n = 0; n < 8; ++n) g[n] = silu(g[n]) * u[n];
+          if (row0 + row < tl.rows) {
+            const size_t at = (size_t)(tl.row0 + row0 + row) * F + (col0 >> 1) + o * 8;
+            uint4 hi, lo;
+            if constexpr (OP) {
+              pair8<BF>(g, hi, lo);
+              *(uint4*)(a.hlo + at) = lo;
+            } else {
+              to16x8<BF>(g, hi);
+            }
+            *(uint4*)(a.hhi + at) = hi;
+          }
+        }
+      } else {
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+          const int row = (lane >> 3) + 8 * it;
+          if (row0 + row < tl.rows) {
+            const float* p = lds + row * kRegionStride + (lane & 7) * 8;
+            float* y = a.y + (size_t)(tl.row0 + row0 + row) * D + col0 + (lane & 7) * 8;
+            *(float4*)y = *(const float4*)p;
+            *(float4*)(y + 4) = *(const float4*)(p + 4);
+          }
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+}
+
+// ---------------------------------------------------------------- products, few rows
+
+// Up to 16 MT rows: every product streams the chosen experts' weights once,
+// straight into registers, and all rows ride along (the MFMA work of rows that
+// did not choose an expert is free while the launch waits for weights).  The
+// workgroups find the distinct experts of the call themselves, in ascending
+// order, so nothing runs before them: two launches in all.
+constexpr int kFewSlots = 256;   // slots (T * k) of the few-row form
+constexpr int kFewRows = 32;
+constexpr int kFewWaves = 8;
+
+// The distinct experts among n slots, ascending: dist[0..count).
+struct Distinct {
+  uint32_t bits[kMaxExperts / 32];
+  int count;
+  int16_t list[kFewSlots];
+};
+__device__ __forceinline__ void find_distinct(const ExpertsArgs& a, int n, Distinct& d) {
+  const int tid = threadIdx.x;
+  if (tid < kMaxExperts / 32) d.bits[tid] = 0u;
+  __syncthreads();
+  if (tid < n) {
+    const int e = a.ids[tid];
+    if ((unsigned)e < (unsigned)a.w.E) atomicOr(&d.bits[e >> 5], 1u << (e & 31));
+  }
+  __syncthreads();
+  // thread e (one per possible expert): its rank among the chosen
+  int below = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kMaxExperts / 32; ++w) {
+    const uint32_t b = d.bits[w];
+    below += w < (tid >> 5) ? __popc(b) : w == (tid >> 5) ? __popc(b & ((1u << (tid & 31)) - 1u)) : 0;
+    all += __popc(b);
+  }
+  if (d.bits[tid >> 5] >> (tid & 31) & 1u) d.list[below] = (int16_t)tid;
+  if (tid == 0) d.count = all;
+  __syncthreads();
+}
+
+// Gate/up: workgroup (column block, y) streams NS strips of the y-th distinct
+// expert; its 8 waves deal the K steps among themselves, so that the workgroup
+// reads one contiguous window, and sum in LDS.  h of expert y, row t goes to
+// row y * 16 MT + t, as a pair.
+// XF: x is 32-bit and becomes the fp16 pair here.
+template <int MT, int NS, bool BF, bool XF>
+__global__ __launch_bounds__(64 * kFewWaves, MT == 1 ? 4 : 2) void experts_gu_few(ExpertsArgs a) {
+  constexpr int U = MT == 1 ? (XF ? 3 : 4) : (XF ? 3 : 4);
+  constexpr int XQ = XF ? 2 : 1;  // 16-byte loads per lane and row tile
+  __shared__ Distinct ds;
+  __shared__ float red[kFewWaves][MT][NS][256];
+  const int n = a.T * a.k;
+  find_distinct(a, n, ds);
+  if ((int)blockIdx.y >= ds.count) return;
+  const int e = ds.list[blockIdx.y];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int D = a.w.D, F = a.w.F, KT = D / 32;
+  const int nsteps = wave < KT ? (KT - wave + kFewWaves - 1) / kFewWaves : 0;
+  const u32x4* wp[NS];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    const int st = blockIdx.x * NS + s;
+    wp[s] = (const u32x4*)a.w.gu + ((size_t)e * (2 * F / 64) + (st >> 2)) * KT * 256 + (st & 3) * 64 + lane;
+  }
+  const char* xp[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int t = min(m * 16 + (lane & 15), a.T - 1);
+    xp[m] = (const char*)a.x + (t * a.x_stride + (lane >> 4) * 8) * (XF ? 4 : 2);
+  }
+  f32x4 acc[MT][NS];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int s = 0; s < NS; ++s) acc[m][s] = f32x4{0.f, 0.f, 0.f, 0.f};
+  u32x4 qw[U][NS], qx[U][MT][XQ];
+  auto load = [&](int u, int j) __attribute__((always_inline)) {
+    const int kt = wave + j * kFewWaves;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) qw[u][s] = __builtin_nontemporal_load(wp[s] + (size_t)kt * 256);
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int q = 0; q < XQ; ++q) qx[u][m][q] = *(const u32x4*)(xp[m] + (size_t)kt * (XF ? 128 : 64) + q * 16);
+  };
+  auto consume = [&](int u) __attribute__((always_inline)) {
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      if constexpr (XF) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[i] = __uint_as_float(qx[u][m][0][i]);
+          v[4 + i] = __uint_as_float(qx[u][m][1][i]);
+        }
+        uint4 hi, lo;
+        pair8<false>(v, hi, lo);
+        const u32x4 h{hi.x, hi.y, hi.z, hi.w}, l{lo.x, lo.y, lo.z, lo.w};
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          acc[m][s] = mfma16<BF>(h, qw[u][s], acc[m][s]);
+          acc[m][s] = mfma16<BF>(l, qw[u][s], acc[m][s]);
+        }
+      } else {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) acc[m][s] = mfma16<BF>(qx[u][m][0], qw[u][s], acc[m][s]);
+      }
+    }
+  };
+  if (nsteps >= U) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) load(u, u);
+    int j = 0;
+    for (; j + 2 * U <= nsteps; j += U) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        consume(u);
+        load(u, j + u + U);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      consume(u);
+      if (j + u + U < nsteps) load(u, j + u + U);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (j + u + U < nsteps) consume(u);
+  } else {
+    for (int j = 0; j < nsteps; ++j) {
+      load(0, j);
+      consume(0);
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int s = 0; s < NS; ++s) *(f32x4*)&red[wave][m][s][lane * 4] = acc[m][s];
+  __syncthreads();
+  // element (row, col) of a 16 x 16 tile is at [16 (row/4) + col] * 4 + row%4
+  for (int i = threadIdx.x; i < MT * (NS / 2) * 256; i += 64 * kFewWaves) {
+    const int c = i & 15, row = i >> 4 & 15, sp = (i >> 8) % (NS / 2), m = (i >> 8) / (NS / 2);
+    const int at = ((row >> 2) * 16 + c) * 4 + (row & 3);
+    float g = 0.f, u = 0.f;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) {
+      g += red[w][m][2 * sp][at];
+      u += red[w][m][2 * sp + 1][at];
+    }
+    const int t = m * 16 + row;
+    if (t < a.T) {
+      const float v = silu(g) * u;
+      const uint16_t hi = to16<BF>(v);
+      const size_t o = ((size_t)blockIdx.y * (16 * MT) + t) * F + (blockIdx.x * (NS / 2) + sp) * 16 + c;
+      a.hhi[o] = hi;
+      a.hlo[o] = to16<BF>(v - from16<BF>(hi));
+    }
+  }
+}
+
+// Down: a workgroup owns NS strips of d_model and runs over all distinct
+// experts, the K steps of each dealt to its 8 waves; after an expert, each
+// row's products are weighted and added to its total (rows that did not choose
+// the expert add nothing, whatever is in them).  So the workgroups all stream
+// alike, however the rows chose, the sums over k need no further pass, and a
+// row's result does not depend on the other rows of the call.
+template <int MT, int NS, bool BF>
+__global__ __launch_bounds__(64 * kFewWaves, 2) void experts_down_few(ExpertsArgs a) {
+  constexpr int U = MT == 1 ? 8 : 4;
+  __shared__ Distinct ds;
+  __shared__ float wmap[kFewSlots][16 * MT];  // weight of (expert, row)
+  __shared__ uint32_t vmask[kFewSlots];       // rows that chose the expert
+  __shared__ float red[kFewWaves][MT][NS][256];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int T = a.T, k = a.k, D = a.w.D, F = a.w.F, KT = F / 32;
+  find_distinct(a, T * k, ds);
+  const int nd = ds.count;
+  for (int i = tid; i < nd; i += 64 * kFewWaves) vmask[i] = 0u;
+  for (int i = tid; i < nd * 16 * MT; i += 64 * kFewWaves) (&wmap[0][0])[i] = 0.f;
+  __syncthreads();
+  if (tid < T)  // one thread per row: an id that comes twice adds up, in order
+    for (int j = 0; j < k; ++j) {
+      const int e = a.ids[tid * k + j];
+      if ((unsigned)e >= (unsigned)a.w.E) continue;
+      int r = __popc(ds.bits[e >> 5] & ((1u << (e & 31)) - 1u));
+      for (int w = 0; w < (e >> 5); ++w) r += __popc(ds.bits[w]);
+      wmap[r][tid] += a.weights[tid * k + j];
+      atomicOr(&vmask[r], 1u << tid);
+    }
+  __syncthreads();
+
+  f32x4 tot[MT][NS], acc[MT][NS];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int s = 0; s < NS; ++s) tot[m][s] = acc[m][s] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int spw = wave < KT ? (KT - wave + kFewWaves - 1) / kFewWaves : 0;  // steps per expert
+  const int total = spw * nd;
+  if (total > 0) {
+    u32x4 qw[U][NS], qh[U][MT], ql[U][MT];
+    // the loader's place: expert ld, step li of it
+    int ld = 0, li = 0;
+    const u32x4* wp;
+    uint32_t hoff[MT];  // halves; rows that did not choose the expert read its first row that did
+    auto enter = [&]() __attribute__((always_inline)) {
+      const int e = __builtin_amdgcn_readfirstlane(ds.list[ld]);
+      const uint32_t vm = __builtin_amdgcn_readfirstlane(vmask[ld]);
+      wp = (const u32x4*)a.w.dn + (size_t)e * (D / 64) * KT * 256 + lane;
+      const int any = __builtin_ctz(vm);
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const int t = m * 16 + (lane & 15);
+        hoff[m] = (uint32_t)(ld * (16 * MT) + (vm >> t & 1u ? t : any)) * F + (lane >> 4) * 8;
+      }
+    };
+    enter();
+    auto load = [&](int u) __attribute__((always_inline)) {
+      const int kt = wave + li * kFewWaves;
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        const int st = blockIdx.x * NS + s;
+        qw[u][s] = __builtin_nontemporal_load(wp + ((size_t)(st >> 2) * KT + kt) * 256 + (st & 3) * 64);
+      }
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        qh[u][m] = *(const u32x4*)(a.hhi + hoff[m] + kt * 32);
+        ql[u][m] = *(const u32x4*)(a.hlo + hoff[m] + kt * 32);
+      }
+      if (++li == spw) {
+        li = 0;
+        if (ld + 1 < nd) ++ld;
+        enter();
+      }
+    };
+    int cd = 0, ci = 0;  // the consumer's place
+    auto consume = [&](int u) __attribute__((always_inline)) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          acc[m][s] = mfma16<BF>(qh[u][m], qw[u][s], acc[m][s]);
+          acc[m][s] = mfma16<BF>(ql[u][m], qw[u][s], acc[m][s]);
+        }
+      if (++ci == spw) {
+        const uint32_t vm = vmask[cd];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          const int r0 = m * 16 + 4 * (lane >> 4);
+          const f32x4 w = *(const f32x4*)&wmap[cd][r0];
+#pragma unroll
+          for (int s = 0; s < NS; ++s) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) tot[m][s][r] = vm >> (r0 + r) & 1u ? tot[m][s][r] + w[r] * acc[m][s][r] : tot[m][s][r];
+            acc[m][s] = f32x4{0.f, 0.f, 0.f, 0.f};
+          }
+        }
+        ci = 0;
+        ++cd;
+      }
+    };
+    if (total >= U) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) load(u);
+      int j = 0;
+      for (; j + 2 * U <= total; j += U) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          consume(u);
+          load(u);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        consume(u);
+        if (j + u + U < total) load(u);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (j + u + U < total) consume(u);
+    } else {
+      for (int j = 0; j < total; ++j) {
+        load(0);
+        consume(0);
+      }
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int s = 0; s < NS; ++s) *(f32x4*)&red[wave][m][s][lane * 4] = tot[m][s];
+  __syncthreads();
+  for (int i = tid; i < MT * NS * 256; i += 64 * kFewWaves) {
+    const int c = i & 15, row = i >> 4 & 15, s = (i >> 8) % NS, m = (i >> 8) / NS;
+    const int at = ((row >> 2) * 16 + c) * 4 + (row & 3);
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) v += red[w][m][s][at];
+    const int t = m * 16 + row;
+    if (t < T) {
+      const int64_t o = t * a.out_stride + (blockIdx.x * NS + s) * 16 + c;
+      if (a.x_type == ET_F32) ((float*)a.out)[o] = v;
+      else ((uint16_t*)a.out)[o] = to16<BF>(v);
     }
   }
 }
@@ -268,6 +749,15 @@ __global__ __launch_bounds__(256) void experts_combine(ExpertsArgs a) {
 
 // ---------------------------------------------------------------- the call
 
+// The form of a call, by its rows alone (the host does not see the choice).
+enum Form { FORM_FEW16, FORM_FEW32, FORM_T32, FORM_T64, FORM_T128, FORM_T256 };
+static Form form_of(const ExpertsArgs& a) {
+  const int n = a.T * a.k, per = n / a.w.E;  // rows per expert if spread evenly
+  if (a.T <= 16 && n <= kFewSlots) return FORM_FEW16;
+  if (a.T <= kFewRows && n <= kFewSlots) return FORM_FEW32;
+  return per < 24 ? FORM_T32 : per < 64 ? FORM_T64 : per < 192 ? FORM_T128 : FORM_T256;
+}
+
 size_t experts_carve(ExpertsArgs& a, void* base) {
   size_t off = 0;
   auto take = [&](size_t bytes) {
@@ -276,36 +766,62 @@ size_t experts_carve(ExpertsArgs& a, void* base) {
     return p;
   };
   const size_t n = (size_t)a.T * a.k, D = a.w.D, F = a.w.F;
+  const Form f = form_of(a);
+  if (f <= FORM_FEW32) {
+    const size_t rows = std::min(n, (size_t)a.w.E) * (f == FORM_FEW16 ? 16 : 32);
+    a.hhi = (uint16_t*)take(rows * F * 2);
+    a.hlo = (uint16_t*)take(rows * F * 2);
+    return off;
+  }
   const bool pair = a.x_type == ET_F32;
   a.perm = (int32_t*)take(n * 4);
   a.pos = (int32_t*)take(n * 4);
   a.cnt = (int32_t*)take((size_t)a.w.E * 4);
   a.off = (int32_t*)take((size_t)a.w.E * 4);
   a.hhi = (uint16_t*)take(n * F * 2);
-  a.hlo = pair ? (uint16_t*)take(n * F * 2) : nullptr;
+  a.hlo = pair || f <= FORM_T64 ? (uint16_t*)take(n * F * 2) : nullptr;
   a.xhi = pair ? (uint16_t*)take((size_t)a.T * D * 2) : nullptr;
   a.xlo = pair ? (uint16_t*)take((size_t)a.T * D * 2) : nullptr;
   a.y = (float*)take(n * D * 4);
   return off;
 }
 
-template <bool BF, bool HL>
-static void launch_products(const ExpertsArgs& a, hipStream_t s) {
-  const int n = a.T * a.k, tiles = n / 16 + std::min(n, a.w.E);  // at most: whole tiles, and a ragged one per expert
-  hvd_launch((experts_gemm<true, BF, HL>), dim3(tiles, (2 * a.w.F / 64 + 3) / 4), dim3(256), 0, s, a);
-  hvd_launch((experts_gemm<false, BF, HL>), dim3(tiles, (a.w.D / 64 + 3) / 4), dim3(256), 0, s, a);
+template <int MT, bool BF, bool XF>
+static void launch_few(const ExpertsArgs& a, hipStream_t s) {
+  const int n = std::min(a.T * a.k, a.w.E);
+  hvd_launch((experts_gu_few<MT, 4, BF, XF>), dim3(2 * a.w.F / 64, n), dim3(64 * kFewWaves), 0, s, a);
+  hvd_launch((experts_down_few<MT, 1, BF>), dim3(a.w.D / 16), dim3(64 * kFewWaves), 0, s, a);
+}
+
+// XP: x is a pair; HP: silu(gate) * up is.
+template <class S, bool BF, bool XP, bool HP>
+static void launch_shape(const ExpertsArgs& a, hipStream_t s) {
+  const int n = a.T * a.k, tiles = n / S::BM + std::min(n, a.w.E);  // at most: whole tiles, and a ragged one per expert
+  const int cg = (2 * a.w.F + S::BN - 1) / S::BN, cd = (a.w.D + S::BN - 1) / S::BN;
+  hvd_launch((experts_tiled<S, true, BF, XP, HP>), dim3(tiles * cg), dim3(64 * S::NW), 0, s, a, cg);
+  hvd_launch((experts_tiled<S, false, BF, HP, false>), dim3(tiles * cd), dim3(64 * S::NW), 0, s, a, cd);
+}
+template <bool BF, bool XP>
+static void launch_tiled(const ExpertsArgs& a, Form f, hipStream_t s) {
+  switch (f) {
+    case FORM_T32: return launch_shape<TileShape<1, 2, 1, 2>, BF, XP, true>(a, s);
+    case FORM_T64: return launch_shape<TileShape<2, 2, 1, 2>, BF, XP, true>(a, s);
+    case FORM_T128: return launch_shape<TileShape<2, 2, 2, 2>, BF, XP, XP>(a, s);
+    default: return launch_shape<TileShape<4, 2, 2, 4>, BF, XP, XP>(a, s);
+  }
 }
 
 hipError_t launch_experts(const ExpertsArgs& a, hipStream_t s) {
-  hvd_launch(experts_sort, dim3(a.w.E), dim3(256), 0, s, a);
-  if (a.x_type == ET_F32) {
-    hvd_launch(experts_split, dim3((a.T * (a.w.D / 8) + 255) / 256), dim3(256), 0, s, a);
-    launch_products<false, true>(a, s);
-  } else if (a.w.wtype == ET_BF16) {
-    launch_products<true, false>(a, s);
-  } else {
-    launch_products<false, false>(a, s);
+  const Form f = form_of(a);
+  const bool pair = a.x_type == ET_F32, bf = a.w.wtype == ET_BF16;
+  if (f <= FORM_FEW32) {
+    if (f == FORM_FEW16) pair ? launch_few<1, false, true>(a, s) : bf ? launch_few<1, true, false>(a, s) : launch_few<1, false, false>(a, s);
+    else pair ? launch_few<2, false, true>(a, s) : bf ? launch_few<2, true, false>(a, s) : launch_few<2, false, false>(a, s);
+    return hipGetLastError();
   }
+  hvd_launch(experts_sort, dim3(a.w.E), dim3(256), 0, s, a);
+  if (pair) hvd_launch(experts_split, dim3((a.T * (a.w.D / 8) + 255) / 256), dim3(256), 0, s, a);
+  pair ? launch_tiled<false, true>(a, f, s) : bf ? launch_tiled<true, false>(a, f, s) : launch_tiled<false, false>(a, f, s);
   hvd_launch(experts_combine, dim3(a.T, (a.w.D / 4 + 255) / 256), dim3(256), 0, s, a);
   return hipGetLastError();
 }

@@ -2,6 +2,7 @@
 // route.hip, experts.hip and block_norm.hip.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <new>
 #include <string>
@@ -53,8 +54,8 @@ RouteArgs route_args(const hvd_route_config& c, int rows, const void* logits, in
 hvd_status check_experts_config(const hvd_experts_config* c) {
   if (!c) return set_err(HVD_ERR_ARG, "null config");
   if (c->n_experts < 1 || c->n_experts > kMaxExperts) return set_err(HVD_ERR_ARG, "n_experts must be in [1, 512]");
-  if (c->d_model < 64 || c->d_model % 64 || c->d_model > (1 << 20)) return set_err(HVD_ERR_ARG, "d_model must be a positive multiple of 64");
-  if (c->ffn_dim < 32 || c->ffn_dim % 32 || c->ffn_dim > (1 << 20)) return set_err(HVD_ERR_ARG, "ffn_dim must be a positive multiple of 32");
+  if (c->d_model < 64 || c->d_model % 64 || c->d_model > (1 << 17)) return set_err(HVD_ERR_ARG, "d_model must be a positive multiple of 64, at most 131072");
+  if (c->ffn_dim < 32 || c->ffn_dim % 32 || c->ffn_dim > (1 << 17)) return set_err(HVD_ERR_ARG, "ffn_dim must be a positive multiple of 32, at most 131072");
   if (c->dtype != HVD_F16 && c->dtype != HVD_BF16) return set_err(HVD_ERR_ARG, "experts' dtype must be HVD_F16 or HVD_BF16");
   return HVD_OK;
 }
@@ -138,7 +139,7 @@ extern "C" size_t hvd_experts_workspace(hvd_experts e, int32_t rows, int32_t top
   a.T = rows;
   a.k = top_k;
   a.x_type = x_dtype;
-  return experts_carve(a, nullptr);
+  return std::max<size_t>(experts_carve(a, nullptr), 256);  // (0 is a refusal)
 }
 
 extern "C" hvd_status hvd_experts_forward(hvd_experts e, int32_t rows, int32_t top_k, const void* x, int32_t x_dtype,
