@@ -38,13 +38,24 @@ def _refuse(msg):
     raise HvdError(HVD_ERR_ARG, msg)
 
 
-_codes = {}
+# The calls below are a few microseconds of host time each, of which a decode
+# step makes dozens: torch is looked up once, configs are built once, and the
+# current device and raw stream are asked for without making objects.
+torch = None
+_codes, _configs = {}, {}
+
+
+def _library():
+    global torch
+    lib = load_library()
+    if torch is None:
+        import torch as t
+        _codes.update({t.float16: 0, t.bfloat16: 1, t.float32: 2})
+        torch = t
+    return lib
 
 
 def _dtype(t, what):
-    if not _codes:
-        import torch
-        _codes.update({torch.float16: 0, torch.bfloat16: 1, torch.float32: 2})
     c = _codes.get(t)
     if c is None:
         _refuse(f"{what} must be float16, bfloat16 or float32, not {t}")
@@ -55,46 +66,37 @@ def _matrix(t, what, device=None, rows=None, cols=None):
     """Checks a [rows, cols] tensor with unit column stride; returns its row stride."""
     if t.dim() != 2 or not t.is_cuda or (device is not None and t.device != device):
         _refuse(f"{what} must be a matrix on the GPU, on one device with the other arguments")
-    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+    n, m = t.shape
+    if (rows is not None and n != rows) or (cols is not None and m != cols):
         _refuse(f"{what} has shape {tuple(t.shape)}, not ({rows}, {cols})")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    rs, cs = t.stride()
+    if cs != 1 and m > 1:
         _refuse(f"{what} must have unit column stride")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return rs if n > 1 else m
 
 
 def _vector(t, what, n, device):
-    import torch
     if t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != n or t.device != device or not t.is_contiguous():
         _refuse(f"{what} must be a contiguous float32 vector of {n} on the arguments' device")
     return t.data_ptr()
 
 
 def _exact(t, what, shape, dtype, device):
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
         _refuse(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on the arguments' device")
     return t.data_ptr()
 
 
-class _On:
-    """Makes a device current for a call where it is not already."""
-
-    def __init__(self, device):
-        import torch
-        self.cuda = torch.cuda
-        self.index = device.index
-        self.prev = None
-
-    def __enter__(self):
-        now = self.cuda.current_device()
-        if self.index is not None and now != self.index:
-            self.prev = now
-            self.cuda.set_device(self.index)
-        return self.cuda.current_stream()
-
-    def __exit__(self, *exc):
-        if self.prev is not None:
-            self.cuda.set_device(self.prev)
-        return False
+def _call(device, fn, *args):
+    """fn(*args, stream) on the device's current stream, with the device current."""
+    now = torch._C._cuda_getDevice()
+    if now == device.index:
+        st = fn(*args, torch._C._cuda_getCurrentRawStream(now))
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    if st:
+        _check(st)
 
 
 def route(logits, top_k, *, score="softmax", bias=None, n_groups=1, top_groups=1, renorm=True, scale=1.0):
@@ -102,23 +104,26 @@ def route(logits, top_k, *, score="softmax", bias=None, n_groups=1, top_groups=1
 
     Returns (ids int32 [rows, top_k], weights float32 [rows, top_k]): best
     first, id -1 and weight 0 where no unmasked expert is left."""
-    import torch
-    lib = load_library()
+    lib = _library()
     stride = _matrix(logits, "logits")
     code = _dtype(logits.dtype, "logits")
     rows, E = logits.shape
-    if score not in _SCORES:
-        _refuse(f"score must be one of {sorted(_SCORES)}")
+    dev = logits.device
+    key = (E, top_k, score, n_groups, top_groups, renorm, scale)
+    cfg = _configs.get(key)
+    if cfg is None:
+        if score not in _SCORES:
+            _refuse(f"score must be one of {sorted(_SCORES)}")
+        if len(_configs) >= 256:
+            _configs.clear()
+        # (an address that stays: the library reads the config during the call only)
+        cfg = _configs[key] = ctypes.pointer(RouteConfig(E, top_k, _SCORES[score], n_groups, top_groups, bool(renorm), scale))
     if not 1 <= top_k <= 16:
         _refuse("top_k must be in [1, 16]")
-    dev = logits.device
     bp = _vector(bias, "bias", E, dev) if bias is not None else None
-    cfg = RouteConfig(E, top_k, _SCORES[score], n_groups, top_groups, 1 if renorm else 0, scale)
-    with _On(dev) as s:
-        ids = torch.empty((rows, top_k), dtype=torch.int32, device=dev)
-        w = torch.empty((rows, top_k), dtype=torch.float32, device=dev)
-        _check(lib.hvd_route(ctypes.byref(cfg), rows, logits.data_ptr(), code, stride, bp, ids.data_ptr(), w.data_ptr(),
-                             s.cuda_stream))
+    ids = torch.empty((rows, top_k), dtype=torch.int32, device=dev)
+    w = torch.empty((rows, top_k), dtype=torch.float32, device=dev)
+    _call(dev, lib.hvd_route, cfg, rows, logits.data_ptr(), code, stride, bp, ids.data_ptr(), w.data_ptr())
     return ids, w
 
 
@@ -128,9 +133,8 @@ class Experts:
     or bfloat16, packed once."""
 
     def __init__(self, gate, up, down):
-        import torch
-        self.lib = load_library()
         self.handle = None
+        self.lib = _library()
         if gate.dim() != 3 or not gate.is_cuda:
             _refuse("gate must be [n_experts, ffn_dim, d_model] on the GPU")
         E, F, D = gate.shape
@@ -143,50 +147,56 @@ class Experts:
         if n == 0:
             raise HvdError(HVD_ERR_ARG, self.lib.hvd_last_error().decode())
         h = ctypes.c_void_p()
-        with _On(self.device) as s:
-            self.buf = torch.empty(n, dtype=torch.uint8, device=self.device)
-            _check(self.lib.hvd_experts_load(ctypes.byref(cfg), gate.data_ptr(), up.data_ptr(), down.data_ptr(),
-                                             self.buf.data_ptr(), n, s.cuda_stream, ctypes.byref(h)))
-            s.synchronize()  # packed: later calls may run on any stream
-            self.stream = s
+        self.buf = torch.empty(n, dtype=torch.uint8, device=self.device)
+        load = lambda stream: self.lib.hvd_experts_load(ctypes.byref(cfg), gate.data_ptr(), up.data_ptr(), down.data_ptr(),
+                                                        self.buf.data_ptr(), n, stream, ctypes.byref(h))
+        _call(self.device, load)
         self.handle = h
+        self.home = torch.cuda.current_stream(self.device)
+        self.home.synchronize()  # packed: later calls may run on any stream
+        self.sizes = {}
 
     def forward(self, x, ids, weights, out=None):
         """out[t] = sum_j weights[t, j] * expert ids[t, j] of x[t]; x
         [rows, d_model] of the weights' dtype, or float32 with float16
         weights; ids int32, weights float32 [rows, top_k].  An id outside
         [0, n_experts) adds nothing."""
-        import torch
         if self.handle is None:
             _refuse("the experts are closed")
         code = _dtype(x.dtype, "x")
-        dev = self.device
-        xs = _matrix(x, "x", dev, None, self.d_model)
-        T = x.shape[0]
+        dev, D = self.device, self.d_model
+        xs = _matrix(x, "x", dev, None, D)
         if ids.dim() != 2:
             _refuse("ids must be [rows, top_k]")
-        k = ids.shape[1]
-        ip = _exact(ids, "ids", (T, k), torch.int32, dev)
-        wp = _exact(weights, "weights", (T, k), torch.float32, dev)
-        es = x.element_size()
-        with _On(dev) as s:
-            if x.data_ptr() % 16 or xs * es % 16:
-                x = x.contiguous() if x.data_ptr() % 16 == 0 else x.clone(memory_format=torch.contiguous_format)
-                xs = self.d_model
-            dst = out
-            if out is None:
-                dst = torch.empty((T, self.d_model), dtype=x.dtype, device=dev)
-            os_ = _matrix(dst, "out", dev, T, self.d_model)
-            if dst.dtype != x.dtype:
-                _refuse("out must have x's dtype")
+        shape = ids.shape
+        T, k = shape
+        if T != x.shape[0]:
+            _refuse("ids must have x's rows")
+        ip = _exact(ids, "ids", shape, torch.int32, dev)
+        wp = _exact(weights, "weights", shape, torch.float32, dev)
+        n = self.sizes.get((T, k, code))
+        if n is None:
             n = self.lib.hvd_experts_workspace(self.handle, T, k, code)
             if n == 0:
                 raise HvdError(HVD_ERR_ARG, self.lib.hvd_last_error().decode())
-            if s != self.stream and not torch.cuda.is_current_stream_capturing():
-                self.buf.record_stream(s)  # close() may give the weights back while this call runs
-            work = torch.empty(n, dtype=torch.uint8, device=dev)
-            _check(self.lib.hvd_experts_forward(self.handle, T, k, x.data_ptr(), code, xs, ip, wp, dst.data_ptr(), os_,
-                                                work.data_ptr(), n, s.cuda_stream))
+            if len(self.sizes) >= 4096:
+                self.sizes.clear()
+            self.sizes[(T, k, code)] = n
+        xp = x.data_ptr()
+        if xp % 16 or xs * x.element_size() % 16:
+            x = x.clone(memory_format=torch.contiguous_format)
+            xp, xs = x.data_ptr(), D
+        if out is None:
+            dst, ds = torch.empty((T, D), dtype=x.dtype, device=dev), D
+        else:
+            dst, ds = out, _matrix(out, "out", dev, T, D)
+            if out.dtype != x.dtype:
+                _refuse("out must have x's dtype")
+        work = torch.empty(n, dtype=torch.uint8, device=dev)
+        _call(dev, self.lib.hvd_experts_forward, self.handle, T, k, xp, code, xs, ip, wp, dst.data_ptr(), ds,
+              work.data_ptr(), n)
+        if torch._C._cuda_getCurrentRawStream(dev.index) != self.home.cuda_stream and not torch.cuda.is_current_stream_capturing():
+            self.buf.record_stream(torch.cuda.current_stream(dev))  # close() may give the weights back while this call runs
         return dst
 
     __call__ = forward
@@ -211,17 +221,24 @@ def block_norm(x, y=None, *, gain=None, post_gain=None, gate=None, scale=1.0, ep
 
     Returns (x', h).  Without a y, x' is x itself; without a gain, h is None.
     ``x_out`` (which may be x) receives x'; ``h_dtype`` defaults to x's."""
-    import torch
-    lib = load_library()
-    rows, dim = x.shape if x.dim() == 2 else _refuse("x must be a matrix")
+    lib = _library()
+    xs, xc = _matrix(x, "x"), _dtype(x.dtype, "x")
+    rows, dim = x.shape
     dev = x.device
-    a = BlockNormArgs()
-    a.x, a.x_stride, a.x_dtype = x.data_ptr(), _matrix(x, "x"), _dtype(x.dtype, "x")
-    a.scale, a.eps = scale, eps
+    yp, ys, yc, gp, gr, gs, gc = None, 0, 0, None, 0, 0, 0
     if y is not None:
-        a.y, a.y_stride, a.y_dtype = y.data_ptr(), _matrix(y, "y", dev, rows, dim), _dtype(y.dtype, "y")
+        yp, ys, yc = y.data_ptr(), _matrix(y, "y", dev, rows, dim), _dtype(y.dtype, "y")
+        if x_out is None:
+            x_out, os_ = torch.empty((rows, dim), dtype=x.dtype, device=dev), dim
+        else:
+            os_ = _matrix(x_out, "x_out", dev, rows, dim)
+            if x_out.dtype != x.dtype:
+                _refuse("x_out must have x's dtype")
+        op = x_out.data_ptr()
     elif gate is not None or post_gain is not None or x_out is not None:
         _refuse("gate, post_gain and x_out belong to a y")
+    else:
+        op, os_ = None, 0
     if gate is not None:
         if gate.device != dev:
             _refuse("gate must be on the arguments' device")
@@ -229,23 +246,18 @@ def block_norm(x, y=None, *, gain=None, post_gain=None, gate=None, scale=1.0, ep
             g = gate.expand(rows, dim)
         except RuntimeError:
             _refuse(f"gate of shape {tuple(gate.shape)} does not broadcast to ({rows}, {dim})")
-        if dim > 1 and g.stride(1) not in (0, 1):
+        gr, gs = g.stride()
+        if dim == 1:
+            gs = 0
+        elif gs not in (0, 1):
             _refuse("gate must have unit column stride")
-        a.gate, a.gate_dtype = g.data_ptr(), _dtype(gate.dtype, "gate")
-        a.gate_row_stride, a.gate_col_stride = g.stride(0), g.stride(1) if dim > 1 else 0
-    if post_gain is not None:
-        a.post_gain = _vector(post_gain, "post_gain", dim, dev)
-    h = None
-    with _On(dev) as s:
-        if y is not None:
-            if x_out is None:
-                x_out = torch.empty((rows, dim), dtype=x.dtype, device=dev)
-            elif x_out.dtype != x.dtype:
-                _refuse("x_out must have x's dtype")
-            a.x_out, a.x_out_stride = x_out.data_ptr(), _matrix(x_out, "x_out", dev, rows, dim)
-        if gain is not None:
-            a.gain = _vector(gain, "gain", dim, dev)
-            h = torch.empty((rows, dim), dtype=h_dtype or x.dtype, device=dev)
-            a.h, a.h_stride, a.h_dtype = h.data_ptr(), dim, _dtype(h.dtype, "h")
-        _check(lib.hvd_block_norm(ctypes.byref(a), rows, dim, s.cuda_stream))
+        gp, gc = g.data_ptr(), _dtype(gate.dtype, "gate")
+    h, hp, gainp, hc = None, None, None, 0
+    if gain is not None:
+        gainp = _vector(gain, "gain", dim, dev)
+        h = torch.empty((rows, dim), dtype=h_dtype or x.dtype, device=dev)
+        hp, hc = h.data_ptr(), _dtype(h.dtype, "h")
+    a = BlockNormArgs(x.data_ptr(), xs, yp, ys, gp, gr, gs, _vector(post_gain, "post_gain", dim, dev) if post_gain is not None else None,
+                      gainp, op, os_, hp, dim, xc, yc, gc, hc, scale, eps)
+    _call(dev, lib.hvd_block_norm, ctypes.byref(a), rows, dim)
     return (x if y is None else x_out), h
