@@ -17,6 +17,8 @@
 #include "kernels.h"
 #include "moe.h"
 
+#include <type_traits>
+
 namespace hvd {
 
 // ---------------------------------------------------------------- weights
@@ -79,17 +81,27 @@ __device__ __forceinline__ float silu(float v) { return v / (1.f + __expf(-v)); 
 // experts places its list, so no workgroup waits for another.  Each thread
 // takes a contiguous run of slots, and a prefix sum over the threads keeps the
 // list ascending.
+typedef int32_t i32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));  // (ids may lie at any 4-byte aligned address)
 __global__ __launch_bounds__(256) void experts_sort(ExpertsArgs a) {
   __shared__ int s_lt[4], s_eq[4];
   const int e = blockIdx.x, n = a.T * a.k, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-  const int run = (n + 255) / 256, i0 = min(n, tid * run), i1 = min(n, i0 + run);
+  const int run = ((n + 255) / 256 + 3) & ~3, i0 = min(n, tid * run), i1 = min(n, i0 + run);
   int lt = 0, eq = 0;
-  for (int i = i0; i < i1; ++i) {
-    const int id = a.ids[i];
+  auto scan = [&](auto&& f) __attribute__((always_inline)) {  // f(slot, id) over the run, four ids a load
+    int i = i0;
+#pragma unroll 4
+    for (; i + 4 <= i1; i += 4) {
+      const i32x4_a4 v = *(const i32x4_a4*)(a.ids + i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f(i + j, v[j]);
+    }
+    for (; i < i1; ++i) f(i, a.ids[i]);
+  };
+  scan([&](int i, int id) {
     lt += id >= 0 && id < e;
     eq += id == e;
     if (e == 0 && (unsigned)id >= (unsigned)a.w.E) a.pos[i] = -1;
-  }
+  });
   int inc = eq;  // inclusive prefix within the wave
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -104,12 +116,14 @@ __global__ __launch_bounds__(256) void experts_sort(ExpertsArgs a) {
   const int base = s_lt[0] + s_lt[1] + s_lt[2] + s_lt[3];
   int p = base + inc - eq;
   for (int w = 0; w < wv; ++w) p += s_eq[w];
-  for (int i = i0; i < i1; ++i)
-    if (a.ids[i] == e) {
-      a.perm[p] = i;
-      a.pos[i] = p;
-      ++p;
-    }
+  if (eq)
+    scan([&](int i, int id) {
+      if (id == e) {
+        a.perm[p] = i;
+        a.pos[i] = p;
+        ++p;
+      }
+    });
   if (tid == 0) {
     a.off[e] = base;
     a.cnt[e] = s_eq[0] + s_eq[1] + s_eq[2] + s_eq[3];
@@ -227,7 +241,7 @@ __global__ __launch_bounds__(64 * S::NW, 2) void experts_tiled(ExpertsArgs a, in
   constexpr int AF = BM / 16, NA = AP ? 2 * AF : AF, WF = BN / 16, NF = NA + WF;
   constexpr int LPT = NF / NW;
   static_assert(NF % NW == 0, "fragments per step");
-  constexpr int BUDGET = NW == 8 ? 150 * 1024 : NW == 4 ? 76 * 1024 : 38 * 1024;
+  constexpr int BUDGET = NW == 8 ? 150 * 1024 : 76 * 1024;  // one or two workgroups per CU
   constexpr int ST0 = BUDGET / (NF * 1024);
   constexpr int ST = ST0 < 3 ? 3 : (ST0 > 6 ? 6 : ST0);
   __shared__ u32x4 sbuf[ST][NF][64];
@@ -283,40 +297,43 @@ __global__ __launch_bounds__(64 * S::NW, 2) void experts_tiled(ExpertsArgs a, in
 
   // 32 rows (columns) of one 16-wide K sub-step s: lane l takes row l%32, K 16s + 8(l/32)..+8
   const int fl = (lane & 15) + 16 * (lane >> 5), fo = (lane >> 4) & 1;
-  struct Ops {
-    u32x4 ah[WM], al[AP ? WM : 1], bw[WN];
-  };
-  auto read_ops = [&](int buf, int s, Ops& o) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < WM; ++i) {
-      o.ah[i] = sbuf[buf][wy * 2 * WM + 2 * i + fo][fl + 32 * s];
-      if constexpr (AP) o.al[i] = sbuf[buf][AF + wy * 2 * WM + 2 * i + fo][fl + 32 * s];
-    }
-#pragma unroll
-    for (int j = 0; j < WN; ++j) o.bw[j] = sbuf[buf][NA + wx * 2 * WN + 2 * j + fo][fl + 32 * s];
-  };
-  auto mfma_ops = [&](const Ops& o, auto&& between) __attribute__((always_inline)) {
-    acc[0][0] = mfma32<BF>(o.ah[0], o.bw[0], acc[0][0]);
-    __builtin_amdgcn_sched_barrier(0);
-    between();
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int i = 0; i < WM; ++i)
-#pragma unroll
-      for (int j = 0; j < WN; ++j) {
-        if (i != 0 || j != 0) acc[i][j] = mfma32<BF>(o.ah[i], o.bw[j], acc[i][j]);
-        if constexpr (AP) acc[i][j] = mfma32<BF>(o.al[i], o.bw[j], acc[i][j]);
-      }
-    __builtin_amdgcn_sched_barrier(0);
-  };
   // Step j lives in slot j % ST.  Iteration i multiplies the first half of step
   // i while its second half is read; then it waits until step i+1 has landed,
   // refills the slot of step i-1, and multiplies the second half while the
-  // first half of step i+1 is read.
-  {
-    Ops o0, o1;
+  // first half of step i+1 is read.  L of the wave's WM row blocks hold rows of
+  // the list: the others are neither read nor multiplied (a wave without any
+  // only copies).
+  auto k_loop = [&](auto live) __attribute__((always_inline)) {
+    constexpr int L = decltype(live)::value;
+    struct Ops {
+      u32x4 ah[L ? L : 1], al[AP && L ? L : 1], bw[WN];
+    };
+    auto read_ops = [&](int buf, int s, Ops& o) __attribute__((always_inline)) {
+      if constexpr (L > 0) {
 #pragma unroll
-    for (int st = 0; st < ST - 1; ++st) issue(st, st);
+        for (int i = 0; i < L; ++i) {
+          o.ah[i] = sbuf[buf][wy * 2 * WM + 2 * i + fo][fl + 32 * s];
+          if constexpr (AP) o.al[i] = sbuf[buf][AF + wy * 2 * WM + 2 * i + fo][fl + 32 * s];
+        }
+#pragma unroll
+        for (int j = 0; j < WN; ++j) o.bw[j] = sbuf[buf][NA + wx * 2 * WN + 2 * j + fo][fl + 32 * s];
+      }
+    };
+    auto mfma_ops = [&](const Ops& o, auto&& between) __attribute__((always_inline)) {
+      if constexpr (L > 0) acc[0][0] = mfma32<BF>(o.ah[0], o.bw[0], acc[0][0]);
+      __builtin_amdgcn_sched_barrier(0);
+      between();
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+#pragma unroll
+        for (int j = 0; j < WN; ++j) {
+          if (i != 0 || j != 0) acc[i][j] = mfma32<BF>(o.ah[i], o.bw[j], acc[i][j]);
+          if constexpr (AP) acc[i][j] = mfma32<BF>(o.al[i], o.bw[j], acc[i][j]);
+        }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    Ops o0, o1;
     vm_wait<LPT * (ST - 2)>();
     block_barrier();
     read_ops(0, 0, o0);
@@ -330,7 +347,13 @@ __global__ __launch_bounds__(64 * S::NW, 2) void experts_tiled(ExpertsArgs a, in
       mfma_ops(o1, [&]() { read_ops(next, 0, o0); });
       slot = next;
     }
-  }
+  };
+#pragma unroll
+  for (int st = 0; st < ST - 1; ++st) issue(st, st);
+  const int live = (tl.rows - wy * 32 * WM + 31) / 32;  // row blocks of this wave that hold rows
+  if (live >= WM) k_loop(std::integral_constant<int, WM>{});
+  else if (WM > 1 && live == 1) k_loop(std::integral_constant<int, 1>{});
+  else k_loop(std::integral_constant<int, 0>{});
   vm_wait<0>();  // no copy may land after the ring is reused or released
   __syncthreads();
 
@@ -407,20 +430,20 @@ constexpr int kFewSlots = 256;   // slots (T * k) of the few-row form
 constexpr int kFewRows = 32;
 constexpr int kFewWaves = 8;
 
-// The distinct experts among n slots, ascending: dist[0..count).
+// The distinct experts among n slots, ascending.
 struct Distinct {
   uint32_t bits[kMaxExperts / 32];
   int count;
   int16_t list[kFewSlots];
 };
-__device__ __forceinline__ void find_distinct(const ExpertsArgs& a, int n, Distinct& d) {
+// This thread's slot's expert (-1: none); the list is ready after a barrier.
+__device__ __forceinline__ int find_distinct(const ExpertsArgs& a, int n, Distinct& d) {
   const int tid = threadIdx.x;
+  int mine = tid < n ? a.ids[tid] : -1;
+  if ((unsigned)mine >= (unsigned)a.w.E) mine = -1;
   if (tid < kMaxExperts / 32) d.bits[tid] = 0u;
   __syncthreads();
-  if (tid < n) {
-    const int e = a.ids[tid];
-    if ((unsigned)e < (unsigned)a.w.E) atomicOr(&d.bits[e >> 5], 1u << (e & 31));
-  }
+  if (mine >= 0) atomicOr(&d.bits[mine >> 5], 1u << (mine & 31));
   __syncthreads();
   // thread e (one per possible expert): its rank among the chosen
   int below = 0, all = 0;
@@ -432,7 +455,7 @@ __device__ __forceinline__ void find_distinct(const ExpertsArgs& a, int n, Disti
   }
   if (d.bits[tid >> 5] >> (tid & 31) & 1u) d.list[below] = (int16_t)tid;
   if (tid == 0) d.count = all;
-  __syncthreads();
+  return mine;
 }
 
 // Gate/up: workgroup (column block, y) streams NS strips of the y-th distinct
@@ -448,6 +471,7 @@ __global__ __launch_bounds__(64 * kFewWaves, MT == 1 ? 4 : 2) void experts_gu_fe
   __shared__ float red[kFewWaves][MT][NS][256];
   const int n = a.T * a.k;
   find_distinct(a, n, ds);
+  __syncthreads();
   if ((int)blockIdx.y >= ds.count) return;
   const int e = ds.list[blockIdx.y];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -567,24 +591,40 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void experts_down_few(ExpertsArg
   __shared__ Distinct ds;
   __shared__ float wmap[kFewSlots][16 * MT];  // weight of (expert, row)
   __shared__ uint32_t vmask[kFewSlots];       // rows that chose the expert
+  __shared__ int16_t s_rank[kFewSlots];       // place of each slot's expert among the distinct ones
+  __shared__ float s_w[kFewSlots];
   __shared__ float red[kFewWaves][MT][NS][256];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int T = a.T, k = a.k, D = a.w.D, F = a.w.F, KT = F / 32;
-  find_distinct(a, T * k, ds);
-  const int nd = ds.count;
-  for (int i = tid; i < nd; i += 64 * kFewWaves) vmask[i] = 0u;
-  for (int i = tid; i < nd * 16 * MT; i += 64 * kFewWaves) (&wmap[0][0])[i] = 0.f;
-  __syncthreads();
-  if (tid < T)  // one thread per row: an id that comes twice adds up, in order
-    for (int j = 0; j < k; ++j) {
-      const int e = a.ids[tid * k + j];
-      if ((unsigned)e >= (unsigned)a.w.E) continue;
-      int r = __popc(ds.bits[e >> 5] & ((1u << (e & 31)) - 1u));
-      for (int w = 0; w < (e >> 5); ++w) r += __popc(ds.bits[w]);
-      wmap[r][tid] += a.weights[tid * k + j];
-      atomicOr(&vmask[r], 1u << tid);
+  // each slot's weight comes in with its id; one thread per row then adds a
+  // row's up, in order, while the first weights are on their way
+  const float my_w = tid < T * k ? a.weights[tid] : 0.f;
+  if (tid < kFewSlots) {
+    vmask[tid] = 0u;
+#pragma unroll
+    for (int r = 0; r < 16 * MT; r += 4) *(float4*)&wmap[tid][r] = float4{0.f, 0.f, 0.f, 0.f};
+  }
+  const int mine = find_distinct(a, T * k, ds);
+  if (tid < T * k) {
+    int r = -1;
+    if (mine >= 0) {
+      r = __popc(ds.bits[mine >> 5] & ((1u << (mine & 31)) - 1u));
+      for (int w = 0; w < (mine >> 5); ++w) r += __popc(ds.bits[w]);
+      atomicOr(&vmask[r], 1u << (tid / k));
     }
+    s_rank[tid] = (int16_t)r;
+    s_w[tid] = my_w;
+  }
   __syncthreads();
+  const int nd = ds.count;
+  auto weigh = [&]() __attribute__((always_inline)) {
+    if (tid < T)
+      for (int j = 0; j < k; ++j) {
+        const int r = s_rank[tid * k + j];
+        if (r >= 0) wmap[r][tid] += s_w[tid * k + j];
+      }
+    __syncthreads();
+  };
 
   f32x4 tot[MT][NS], acc[MT][NS];
 #pragma unroll
@@ -658,6 +698,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void experts_down_few(ExpertsArg
     if (total >= U) {
 #pragma unroll
       for (int u = 0; u < U; ++u) load(u);
+      weigh();
       int j = 0;
       for (; j + 2 * U <= total; j += U) {
 #pragma unroll
@@ -675,11 +716,14 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void experts_down_few(ExpertsArg
       for (int u = 0; u < U; ++u)
         if (j + u + U < total) consume(u);
     } else {
+      weigh();
       for (int j = 0; j < total; ++j) {
         load(0);
         consume(0);
       }
     }
+  } else {
+    weigh();  // (every wave takes part in its barrier)
   }
 #pragma unroll
   for (int m = 0; m < MT; ++m)
@@ -749,13 +793,32 @@ __global__ __launch_bounds__(256) void experts_combine(ExpertsArgs a) {
 
 // ---------------------------------------------------------------- the call
 
-// The form of a call, by its rows alone (the host does not see the choice).
-enum Form { FORM_FEW16, FORM_FEW32, FORM_T32, FORM_T64, FORM_T128, FORM_T256 };
+// The form of a call, from its sizes alone (the host does not see the choice).
+// Measured with 64 experts of 4096 x 1024, top 8, unless said otherwise (us a
+// call, bf16; few-row form / 64-row tiles / 128-row tiles / 256-row tiles):
+//   16 rows 196 / 222 / 230 / -, 40 rows - / 248 / 259 / 266, 200 rows - / 394 / 314 / 315,
+//   848 rows - / 561 / 440 / 467; 2000 rows, 8 experts, top 2: - / 271 / 224 / 207.
+// * The few-row form up to 16 rows.  Up to 32 rows it multiplies two row tiles
+//   for every expert, which pays where the tiles of few experts would leave CUs
+//   without weights to stream: 32 rows, 8 experts, top 2: 46 / 128 / 72; 32 rows
+//   of 64 experts: 281 / 245 / 255.
+// * 64-row tiles (4 waves, several workgroups per CU) while an expert has few
+//   rows, if there are enough of them; 128-row tiles (8 waves) otherwise: 32 rows
+//   of 16 experts of 1024 x 512: - / 36 / 26.
+// * 256-row tiles where most tiles fill: each weight is copied half as often.
+// With few rows per expert the products wait for weights, and silu(gate) * up
+// goes through the down product as a pair at no cost (40 rows: 259 -> 261); with
+// many it is one 16-bit value (848 rows: 480 -> 440).
+enum Form { FORM_FEW16, FORM_FEW32, FORM_T64_PAIR, FORM_T128_PAIR, FORM_T128, FORM_T256 };
+constexpr int kPairRows = 16;   // rows per expert below which the product stays a pair
+constexpr int kWideRows = 384;  // rows per expert from which 256-row tiles pay
 static Form form_of(const ExpertsArgs& a) {
   const int n = a.T * a.k, per = n / a.w.E;  // rows per expert if spread evenly
+  const bool fills = (int64_t)std::min(n, a.w.E) * a.w.F >= 128 * 256;  // a 256-column tile (gate and up) per CU
   if (a.T <= 16 && n <= kFewSlots) return FORM_FEW16;
-  if (a.T <= kFewRows && n <= kFewSlots) return FORM_FEW32;
-  return per < 24 ? FORM_T32 : per < 64 ? FORM_T64 : per < 192 ? FORM_T128 : FORM_T256;
+  if (a.T <= kFewRows && n <= kFewSlots && !fills) return FORM_FEW32;
+  if (per < kPairRows) return fills ? FORM_T64_PAIR : FORM_T128_PAIR;
+  return per < kWideRows ? FORM_T128 : FORM_T256;
 }
 
 size_t experts_carve(ExpertsArgs& a, void* base) {
@@ -779,7 +842,7 @@ size_t experts_carve(ExpertsArgs& a, void* base) {
   a.cnt = (int32_t*)take((size_t)a.w.E * 4);
   a.off = (int32_t*)take((size_t)a.w.E * 4);
   a.hhi = (uint16_t*)take(n * F * 2);
-  a.hlo = pair || f <= FORM_T64 ? (uint16_t*)take(n * F * 2) : nullptr;
+  a.hlo = pair || f <= FORM_T128_PAIR ? (uint16_t*)take(n * F * 2) : nullptr;
   a.xhi = pair ? (uint16_t*)take((size_t)a.T * D * 2) : nullptr;
   a.xlo = pair ? (uint16_t*)take((size_t)a.T * D * 2) : nullptr;
   a.y = (float*)take(n * D * 4);
@@ -803,11 +866,14 @@ static void launch_shape(const ExpertsArgs& a, hipStream_t s) {
 }
 template <bool BF, bool XP>
 static void launch_tiled(const ExpertsArgs& a, Form f, hipStream_t s) {
+  using T64 = TileShape<1, 4, 2, 2>;   // 64 x 256
+  using T128 = TileShape<2, 4, 2, 2>;  // 128 x 256
+  using T256 = TileShape<4, 2, 2, 4>;  // 256 x 256
   switch (f) {
-    case FORM_T32: return launch_shape<TileShape<1, 2, 1, 2>, BF, XP, true>(a, s);
-    case FORM_T64: return launch_shape<TileShape<2, 2, 1, 2>, BF, XP, true>(a, s);
-    case FORM_T128: return launch_shape<TileShape<2, 2, 2, 2>, BF, XP, XP>(a, s);
-    default: return launch_shape<TileShape<4, 2, 2, 4>, BF, XP, XP>(a, s);
+    case FORM_T64_PAIR: return launch_shape<T64, BF, XP, true>(a, s);
+    case FORM_T128_PAIR: return launch_shape<T128, BF, XP, true>(a, s);
+    case FORM_T128: return launch_shape<T128, BF, XP, XP>(a, s);
+    default: return launch_shape<T256, BF, XP, XP>(a, s);
   }
 }
 
