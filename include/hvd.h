@@ -253,7 +253,8 @@ int32_t hvd_kv_free_pages(hvd_kv kv);
  * attention, 6 = attention combine, 7 = everything else, 8 = the one-launch
  * verify step (HVD_OPT_FLOW: the whole forward, its bytes the step's weights
  * and K/V), 9 = the attention + O launch (HVD_OPT_ATTN_O: its bytes the K/V
- * and the O weights).  hvd_profile_read returns the
+ * and the O weights), 10 = the experts of a layer (its bytes the weights of as
+ * many experts as its rows can choose).  hvd_profile_read returns the
  * summed event time (ms), launch count and algorithmic bytes since the last
  * enable.  The events add a little time to every bracketed launch. */
 hvd_status hvd_profile_enable(hvd_kv kv, int32_t enable);
@@ -341,9 +342,9 @@ int hvd_measure_mfma_peak(void* stream, double* tflops);
 
 /* ---------------------------------------------------------------------------
  * Operators of an expert layer: the MLP block of a decoder layer whose rows
- * each go through a few of many SwiGLU experts.  A verify step of such a
- * target is hvd_route, hvd_experts_forward and hvd_block_norm in place of the
- * dense MLP.
+ * each go through a few of many SwiGLU experts.  The steps of a model loaded
+ * with hvd_model_load_moe run hvd_route, hvd_experts_forward and
+ * hvd_block_norm in place of the dense MLP.
  *
  * Buffers are DEVICE memory of the current device, which is also the
  * device of `stream`; matrices are row-major with unit column stride and a
@@ -448,6 +449,35 @@ typedef struct {
   float scale, eps;
 } hvd_block_norm_args;
 hvd_status hvd_block_norm(const hvd_block_norm_args* args, int32_t rows, int32_t dim, void* stream);
+
+/* Decoders with expert layers.  Layers first_layer .. n_layers - 1 have
+ * route.n_experts SwiGLU experts of ffn_dim (% 32 == 0) each in place of the
+ * dense MLP: with h the normalised MLP input,
+ *     X += out_scale * N(sum over the chosen experts of w_e * expert_e(h)),
+ * the choice by hvd_route on the logits router h, N the RMSNorm with a gain of
+ * its own if post_norm, else nothing.  Router and experts run on h's fp16
+ * hi + lo pair (about 22 bits) whatever the HVD_OPT_*_SINGLE options say. */
+typedef struct {
+  int32_t first_layer;   /* in [0, n_layers) */
+  int32_t ffn_dim;
+  hvd_route_config route;
+  float out_scale;
+  int32_t post_norm;
+} hvd_moe_config;
+
+/* hvd_model_bytes, hvd_kv_bytes and hvd_model_load for a decoder with expert
+ * layers (moe NULL: the same as those).  The tensors of a layer with experts,
+ * bf16 like the others, take the place of its nine:
+ *   attn_norm [D], wq, wk, wv, wo, mlp_norm [D] as before, router [E, D],
+ *   router_bias [E] (the bias of hvd_route; may be NULL), gate [E, F, D],
+ *   up [E, F, D], down [E, D, F], post_norm [D] (NULL without post_norm);
+ * count = 3 + 9 * first_layer + 12 * (n_layers - first_layer).  Handles from
+ * here work with every call of this header; HVD_OPT_FLOW has no effect on
+ * them. */
+size_t hvd_model_bytes_moe(const hvd_config* cfg, const hvd_moe_config* moe);
+size_t hvd_kv_bytes_moe(const hvd_config* cfg, const hvd_moe_config* moe, int32_t max_seqs, int32_t n_pages);
+hvd_status hvd_model_load_moe(const hvd_config* cfg, const hvd_moe_config* moe, const uint16_t* const* tensors,
+                              void* dev_buf, size_t dev_bytes, void* stream, hvd_model* out);
 
 /* Message of the last failing call on this thread ("" if none). */
 const char* hvd_last_error(void);

@@ -24,6 +24,7 @@ textbook softmax attention, Hkv = Hq, a library cross-check against
 cycles-per-1K identity printed in the paper's App. C and Table 4.
 """
 
+from .experts import OracleExpertsModel  # noqa: F401
 from .model import (  # noqa: F401
     OracleModel,
     SeqState,

@@ -55,6 +55,12 @@ class OracleModel:
         """h @ W^T for the [out, in] weight ``name`` (a plain matrix product)."""
         return h @ self.w(name).T
 
+    def mlp(self, h: np.ndarray, layer: int) -> np.ndarray:
+        """The SwiGLU MLP of a layer on its normalised input."""
+        p = f"layers.{layer}."
+        a = silu(self.linear(h, p + "wg")) * self.linear(h, p + "wu")
+        return self.linear(a, p + "wd")
+
 
 # ------------------------------------------------------------------ layers
 
@@ -133,8 +139,7 @@ def forward(model: OracleModel, K_cache, V_cache, tokens, positions, want_logits
         o = attend(q, Kc, Vc, positions).reshape(n, c.q_dim)
         x = x + model.linear(o, p + "wo")
         h2 = rms_norm(x, model.w(p + "mlp_norm"), c.rms_eps)
-        a = silu(model.linear(h2, p + "wg")) * model.linear(h2, p + "wu")
-        x = x + model.linear(a, p + "wd")
+        x = x + model.mlp(h2, l)
         new_k.append(k)
         new_v.append(v)
     logits = None
@@ -347,8 +352,7 @@ def forward_tree(model: OracleModel, K_cache, V_cache, tokens, positions, row_al
         o = attend_masked(q, Kc, Vc, allowed).reshape(n, c.q_dim)
         x = x + model.linear(o, p + "wo")
         h2 = rms_norm(x, model.w(p + "mlp_norm"), c.rms_eps)
-        a = silu(model.linear(h2, p + "wg")) * model.linear(h2, p + "wu")
-        x = x + model.linear(a, p + "wd")
+        x = x + model.mlp(h2, l)
         new_k.append(k)
         new_v.append(v)
     logits = model.linear(rms_norm(x, model.w("final_norm"), c.rms_eps), "lm_head")

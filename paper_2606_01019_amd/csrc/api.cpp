@@ -18,6 +18,7 @@
 #include "error.h"
 #include "host_state.h"
 #include "kernels.h"
+#include "moe.h"
 
 using namespace hvd;
 
@@ -73,7 +74,7 @@ constexpr int kPartSlots = 4096;   // attention partial slots (multi-chunk items
 constexpr size_t kMaxGraphs = 64;  // cached step graphs per KV handle
 // profiling families: GEMM by role, attention, combine, everything else
 enum { PF_QKV = 0, PF_O = 1, PF_GATEUP = 2, PF_DOWN = 3, PF_LM = 4, PF_ATTN = 5, PF_COMBINE = 6, PF_OTHER = 7,
-       PF_FLOW = 8, PF_ATTN_O = 9, kProfFamilies = 10 };
+       PF_FLOW = 8, PF_ATTN_O = 9, PF_EXPERTS = 10, kProfFamilies = 11 };
 
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
@@ -104,9 +105,27 @@ hvd_status check_config(const hvd_config* c) {
   return HVD_OK;
 }
 
+// Checks a decoder with expert layers (moe null: a dense one).
+hvd_status check_moe(const hvd_config* c, const hvd_moe_config* moe) {
+  if (hvd_status st = check_config(c); st != HVD_OK) return st;
+  if (!moe) return HVD_OK;
+  if (moe->first_layer < 0 || moe->first_layer >= c->n_layers) return set_err(HVD_ERR_ARG, "first_layer must be in [0, n_layers)");
+  if (moe->ffn_dim < 32 || moe->ffn_dim % 32 || moe->ffn_dim > (1 << 17) || c->d_model > (1 << 17))
+    return set_err(HVD_ERR_ARG, "the experts' ffn_dim must be a positive multiple of 32, it and d_model at most 131072");
+  if (c->d_model > kMaxNormDim) return set_err(HVD_ERR_ARG, "d_model of a decoder with experts must be at most 16384");
+  if (!std::isfinite(moe->out_scale)) return set_err(HVD_ERR_ARG, "out_scale must be finite");
+  return check_route_config(&moe->route);
+}
+// Router rows: padded with zeros to whole column tiles of the GEMMs.
+int router_rows(const hvd_moe_config& m) { return (m.route.n_experts + 127) / 128 * 128; }
+
+// gu and down are a dense layer's, router to post an expert layer's
 struct LayerW {
-  uint16_t *qkv, *o, *gu, *down;
+  uint16_t *qkv, *o, *gu = nullptr, *down = nullptr;
   float *g_attn, *g_mlp;
+  uint16_t* router = nullptr;
+  float *router_bias = nullptr, *g_post = nullptr;  // null: none
+  ExpertsW experts{};
 };
 
 }  // namespace
@@ -122,6 +141,9 @@ struct hvd_model_s {
   uint16_t* lm = nullptr;
   float2* rope = nullptr;
   hipStream_t stream = nullptr;
+  bool has_moe = false;
+  hvd_moe_config moe{};
+  bool experts_in(int layer) const { return has_moe && layer >= moe.first_layer; }
 };
 
 namespace {
@@ -134,11 +156,21 @@ size_t carve_model(hvd_model_s* m, void* base) {
                kd = (size_t)c.n_kv_heads * c.head_dim;
   m->embed = cv.take<uint16_t>(V * D);
   m->layers.resize(c.n_layers);
-  for (auto& L : m->layers) {
+  for (int l = 0; l < c.n_layers; ++l) {
+    LayerW& L = m->layers[l];
     L.qkv = cv.take<uint16_t>((qd + 2 * kd) * D);
     L.o = cv.take<uint16_t>(D * qd);
-    L.gu = cv.take<uint16_t>(2 * F * D);
-    L.down = cv.take<uint16_t>(D * F);
+    if (!m->experts_in(l)) {
+      L.gu = cv.take<uint16_t>(2 * F * D);
+      L.down = cv.take<uint16_t>(D * F);
+    } else {
+      const size_t E = m->moe.route.n_experts, Fe = m->moe.ffn_dim;
+      L.router = cv.take<uint16_t>((size_t)router_rows(m->moe) * D);
+      L.router_bias = cv.take<float>(E);
+      L.g_post = cv.take<float>(D);
+      uint16_t* gu = cv.take<uint16_t>(E * 2 * Fe * D);
+      L.experts = ExpertsW{gu, cv.take<uint16_t>(E * D * Fe), (int)E, (int)D, (int)Fe, ET_F16};
+    }
     L.g_attn = cv.take<float>(D);
     L.g_mlp = cv.take<float>(D);
   }
@@ -150,12 +182,15 @@ size_t carve_model(hvd_model_s* m, void* base) {
 
 }  // namespace
 
-extern "C" size_t hvd_model_bytes(const hvd_config* cfg) {
-  if (check_config(cfg) != HVD_OK) return 0;
+extern "C" size_t hvd_model_bytes_moe(const hvd_config* cfg, const hvd_moe_config* moe) {
+  if (check_moe(cfg, moe) != HVD_OK) return 0;
   hvd_model_s tmp;
   tmp.cfg = *cfg;
+  tmp.has_moe = moe != nullptr;
+  if (moe) tmp.moe = *moe;
   return carve_model(&tmp, nullptr);
 }
+extern "C" size_t hvd_model_bytes(const hvd_config* cfg) { return hvd_model_bytes_moe(cfg, nullptr); }
 
 namespace {
 
@@ -180,6 +215,7 @@ hvd_status pack_group(const std::vector<std::pair<const uint16_t*, size_t>>& par
                       int K, uint16_t* staging, int32_t* dmap, uint16_t* dst, hipStream_t s) {
   size_t off = 0;
   for (auto& p : parts) {
+    if (p.second == 0) continue;
     HIP_TRY(hipMemcpyAsync(staging + off, p.first, p.second * sizeof(uint16_t), hipMemcpyHostToDevice, s));
     off += p.second;
   }
@@ -191,16 +227,50 @@ hvd_status pack_group(const std::vector<std::pair<const uint16_t*, size_t>>& par
 
 }  // namespace
 
+namespace {
+
+// Experts go through the staging buffer as many at a time as fit it; src
+// [E][rows][cols] on the host, up null for the down projection.
+hvd_status pack_expert_tensors(const uint16_t* gate, const uint16_t* up, size_t E, size_t rows, size_t cols,
+                               uint16_t* staging, size_t stage_elems, uint16_t* dst, hipStream_t s) {
+  const size_t one = rows * cols, parts = up ? 2 : 1, per = std::max<size_t>(1, stage_elems / (parts * one));
+  for (size_t e = 0; e < E; e += per) {
+    const size_t n = std::min(per, E - e);
+    HIP_TRY(hipMemcpyAsync(staging, gate + e * one, n * one * 2, hipMemcpyHostToDevice, s));
+    if (up) HIP_TRY(hipMemcpyAsync(staging + n * one, up + e * one, n * one * 2, hipMemcpyHostToDevice, s));
+    HIP_TRY(launch_pack_experts(staging, up ? staging + n * one : nullptr, dst + e * parts * one, (int)n, (int)rows,
+                                (int)cols, true, s));
+    HIP_TRY(hipStreamSynchronize(s));
+  }
+  return HVD_OK;
+}
+
+}  // namespace
+
 extern "C" hvd_status hvd_model_load(const hvd_config* cfg, const uint16_t* const* t, void* dev_buf, size_t dev_bytes,
                                      void* stream, hvd_model* out) {
-  if (hvd_status st = check_config(cfg); st != HVD_OK) return st;
+  return hvd_model_load_moe(cfg, nullptr, t, dev_buf, dev_bytes, stream, out);
+}
+
+extern "C" hvd_status hvd_model_load_moe(const hvd_config* cfg, const hvd_moe_config* moe, const uint16_t* const* t,
+                                         void* dev_buf, size_t dev_bytes, void* stream, hvd_model* out) {
+  if (hvd_status st = check_moe(cfg, moe); st != HVD_OK) return st;
   if (!t || !out) return set_err(HVD_ERR_ARG, "null tensors or out");
   const hvd_config& c = *cfg;
-  const int n_t = 3 + 9 * c.n_layers;
-  for (int i = 0; i < n_t; ++i)
+  const int n_dense = moe ? moe->first_layer : c.n_layers;
+  auto layer_at = [&](int l) { return 1 + 9 * std::min(l, n_dense) + 12 * std::max(0, l - n_dense); };
+  const int n_t = layer_at(c.n_layers) + 2;
+  for (int i = 0; i < n_t; ++i) {
+    const int in_layer = i - layer_at(n_dense);  // among the expert layers' tensors
+    if (moe && in_layer >= 0 && i < n_t - 2 &&
+        (in_layer % 12 == 7 || (in_layer % 12 == 11 && !moe->post_norm)))
+      continue;  // router_bias and, without a post norm, post_norm may be null
     if (!t[i]) return set_err(HVD_ERR_ARG, "null tensor pointer");
+  }
   auto* m = new hvd_model_s();
   m->cfg = c;
+  m->has_moe = moe != nullptr;
+  if (moe) m->moe = *moe;
   m->stream = (hipStream_t)stream;
   const size_t need = carve_model(m, nullptr);
   if (dev_buf) {
@@ -224,6 +294,16 @@ extern "C" hvd_status hvd_model_load(const hvd_config* cfg, const uint16_t* cons
                kd = (size_t)c.n_kv_heads * dh;
   size_t stage_elems = std::max({(qd + 2 * kd) * D, 2 * F * D, D * F, V * D, D * qd});
   size_t map_elems = std::max({qd + 2 * kd, 2 * F, V, D});
+  std::vector<uint16_t> router_pad;  // the router's zero rows
+  std::vector<int32_t> map_R;
+  if (moe) {
+    const size_t R = router_rows(*moe);
+    stage_elems = std::max({stage_elems, 2 * (size_t)moe->ffn_dim * D, R * D});
+    map_elems = std::max(map_elems, R);
+    router_pad.assign((R - moe->route.n_experts) * D, 0);
+    map_R.resize(R);
+    for (size_t i = 0; i < R; ++i) map_R[i] = (int32_t)i;
+  }
   uint16_t* staging = nullptr;
   int32_t* dmap = nullptr;
   hvd_status st = HVD_OK;
@@ -273,17 +353,28 @@ extern "C" hvd_status hvd_model_load(const hvd_config* cfg, const uint16_t* cons
   if (hipMemcpyAsync(m->embed, t[0], V * D * 2, hipMemcpyHostToDevice, s) != hipSuccess)
     return fail(set_err(HVD_ERR_DEVICE, "embedding upload failed"));
   for (int l = 0; l < c.n_layers && st == HVD_OK; ++l) {
-    const uint16_t* const* lt = t + 1 + 9 * l;
+    const uint16_t* const* lt = t + layer_at(l);
     LayerW& L = m->layers[l];
     if ((st = upload_gain(lt[0], L.g_attn, (int)D, s)) != HVD_OK) break;
     if ((st = pack_group({{lt[1], qd * D}, {lt[2], kd * D}, {lt[3], kd * D}}, qkv_map, (int)D, staging, dmap, L.qkv, s)) != HVD_OK) break;
     if ((st = pack_group({{lt[4], D * qd}}, map_D, (int)qd, staging, dmap, L.o, s)) != HVD_OK) break;
     if ((st = upload_gain(lt[5], L.g_mlp, (int)D, s)) != HVD_OK) break;
+    if (m->experts_in(l)) {
+      const size_t E = moe->route.n_experts, Fe = moe->ffn_dim;
+      if ((st = pack_group({{lt[6], E * D}, {router_pad.data(), router_pad.size()}}, map_R, (int)D, staging, dmap, L.router, s)) != HVD_OK) break;
+      if (!lt[7]) L.router_bias = nullptr;
+      else if ((st = upload_gain(lt[7], L.router_bias, (int)E, s)) != HVD_OK) break;
+      if ((st = pack_expert_tensors(lt[8], lt[9], E, Fe, D, staging, stage_elems, (uint16_t*)L.experts.gu, s)) != HVD_OK) break;
+      if ((st = pack_expert_tensors(lt[10], nullptr, E, D, Fe, staging, stage_elems, (uint16_t*)L.experts.dn, s)) != HVD_OK) break;
+      if (!moe->post_norm) L.g_post = nullptr;
+      else if ((st = upload_gain(lt[11], L.g_post, (int)D, s)) != HVD_OK) break;
+      continue;
+    }
     if ((st = pack_group({{lt[6], F * D}, {lt[7], F * D}}, gu_map, (int)D, staging, dmap, L.gu, s)) != HVD_OK) break;
     if ((st = pack_group({{lt[8], D * F}}, map_D, (int)F, staging, dmap, L.down, s)) != HVD_OK) break;
   }
-  if (st == HVD_OK) st = upload_gain(t[1 + 9 * c.n_layers], m->g_final, (int)D, s);
-  if (st == HVD_OK) st = pack_group({{t[2 + 9 * c.n_layers], V * D}}, map_V, (int)D, staging, dmap, m->lm, s);
+  if (st == HVD_OK) st = upload_gain(t[n_t - 2], m->g_final, (int)D, s);
+  if (st == HVD_OK) st = pack_group({{t[n_t - 1], V * D}}, map_V, (int)D, staging, dmap, m->lm, s);
   if (st != HVD_OK) return fail(st);
 
   // rotary table: angle = pos * theta^(-2j/dh) in double, stored as fp32 (cos, sin)
@@ -412,6 +503,15 @@ struct hvd_kv_s {
   uint32_t* flow_cnt = nullptr;         // [kFlowCounterWords]: err word, then the step's counters
   void* static_base = nullptr;    // this device's static scratch (hipGetSymbolAddress at kv_alloc)
   size_t static_bytes = 0;
+  // expert layers: one layer's router logits, choice, MLP input and output, and the experts' workspace
+  float* moe_logits = nullptr;
+  float* moe_val = nullptr;    // (the router GEMM's argmax partials, unused)
+  int32_t* moe_idx = nullptr;
+  int32_t* moe_ids = nullptr;
+  float* moe_w = nullptr;
+  float* moe_h = nullptr;
+  float* moe_y = nullptr;
+  char* moe_work = nullptr;
   // profiling
   bool prof = false;
   std::vector<ProfRec> prof_pending;
@@ -438,7 +538,23 @@ size_t meta_capacity_ints(const hvd_config& c, int max_rows, int max_seqs, int p
          item_ints * (4 * units + 4 * kPartSlots + kAttnClasses * (64 + 16)) + 3 * (size_t)max_seqs * pt_stride + 64;
 }
 
-size_t carve_kv(hvd_kv_s* k, const hvd_config& c, int max_seqs, int n_pages, void* base) {
+// Workspace of the experts for any forward of at most `rows` rows: the few-row
+// forms have sizes of their own, above them it grows with the rows.
+size_t experts_bytes_for(int d_model, const hvd_moe_config& m, int rows) {
+  ExpertsArgs a{};
+  a.w = ExpertsW{nullptr, nullptr, m.route.n_experts, d_model, m.ffn_dim, ET_F16};
+  a.x_type = ET_F32;
+  a.T = rows;
+  a.k = m.route.top_k;
+  return experts_carve(a, nullptr);
+}
+size_t experts_work_bytes(const hvd_config& c, const hvd_moe_config& m, int rows) {
+  size_t most = 0;
+  for (int T = 1; T <= std::min(rows, kFewRows); ++T) most = std::max(most, experts_bytes_for(c.d_model, m, T));
+  return std::max(most, experts_bytes_for(c.d_model, m, rows));
+}
+
+size_t carve_kv(hvd_kv_s* k, const hvd_config& c, const hvd_moe_config* moe, int max_seqs, int n_pages, void* base) {
   Carver cv(base);
   const size_t D = c.d_model, F = c.ffn_dim, qd = (size_t)c.n_q_heads * c.head_dim;
   k->page_stride = (size_t)2 * c.n_kv_heads * kPage * c.head_dim;
@@ -505,6 +621,17 @@ size_t carve_kv(hvd_kv_s* k, const hvd_config& c, int max_seqs, int n_pages, voi
       f.ss_in = l ? k->flow_host[l - 1].ss_out : k->ss;
     }
   }
+  if (moe) {
+    const size_t R = router_rows(*moe), K = moe->route.top_k;
+    k->moe_logits = cv.take<float>(Mp * R);
+    k->moe_val = cv.take<float>(Mp * (R / 16));
+    k->moe_idx = cv.take<int32_t>(Mp * (R / 16));
+    k->moe_ids = cv.take<int32_t>(Mp * K);
+    k->moe_w = cv.take<float>(Mp * K);
+    k->moe_h = cv.take<float>(Mp * D);
+    k->moe_y = cv.take<float>(Mp * D);
+    k->moe_work = cv.take<char>(experts_work_bytes(c, *moe, k->max_rows));
+  }
   k->sx.gemm_part = k->gemm_part;
   k->sx.gemm_part_bytes = kGemmPartBytes;
   k->sx.gemm_cnt = k->gemm_cnt;
@@ -523,10 +650,13 @@ size_t carve_kv(hvd_kv_s* k, const hvd_config& c, int max_seqs, int n_pages, voi
 
 }  // namespace
 
-extern "C" size_t hvd_kv_bytes(const hvd_config* cfg, int32_t max_seqs, int32_t n_pages) {
-  if (check_config(cfg) != HVD_OK || max_seqs < 1 || n_pages < 1) return 0;
+extern "C" size_t hvd_kv_bytes_moe(const hvd_config* cfg, const hvd_moe_config* moe, int32_t max_seqs, int32_t n_pages) {
+  if (check_moe(cfg, moe) != HVD_OK || max_seqs < 1 || n_pages < 1) return 0;
   hvd_kv_s tmp;
-  return carve_kv(&tmp, *cfg, max_seqs, n_pages, nullptr);
+  return carve_kv(&tmp, *cfg, moe, max_seqs, n_pages, nullptr);
+}
+extern "C" size_t hvd_kv_bytes(const hvd_config* cfg, int32_t max_seqs, int32_t n_pages) {
+  return hvd_kv_bytes_moe(cfg, nullptr, max_seqs, n_pages);
 }
 
 extern "C" hvd_status hvd_kv_alloc(hvd_model m, int32_t max_seqs, int32_t n_pages, void* dev_buf, size_t dev_bytes,
@@ -543,7 +673,8 @@ extern "C" hvd_status hvd_kv_alloc(hvd_model m, int32_t max_seqs, int32_t n_page
   // 32B shape: whole-row error 2.7-2.9e-2 with gate/up single, 2.4e-2 with
   // the pair, against a 2.83e-2 bar)
   k->mlp_single_gu = c.n_layers <= kMlpSingleMaxLayers;
-  const size_t need = carve_kv(k, c, max_seqs, n_pages, nullptr);
+  const hvd_moe_config* moe = m->has_moe ? &m->moe : nullptr;
+  const size_t need = carve_kv(k, c, moe, max_seqs, n_pages, nullptr);
   if (dev_buf) {
     if (dev_bytes < need) {
       delete k;
@@ -557,7 +688,7 @@ extern "C" hvd_status hvd_kv_alloc(hvd_model m, int32_t max_seqs, int32_t n_page
     }
     k->owned = true;
   }
-  carve_kv(k, c, max_seqs, n_pages, k->base);
+  carve_kv(k, c, moe, max_seqs, n_pages, k->base);
   if (hipHostMalloc((void**)&k->meta_host, k->meta_ints * 4, hipHostMallocDefault) != hipSuccess ||
       hipHostMalloc((void**)&k->out_host, ((2 + kMaxTreeNodes) * (size_t)max_seqs + 1) * 4, hipHostMallocDefault) !=
           hipSuccess) {
@@ -891,7 +1022,7 @@ hvd_status forward(hvd_kv_s* k, const std::vector<SeqMeta>& seqs, std::vector<Ro
   // One-launch step (flow.hip): verify batches of at most two row tiles,
   // head dim 128, every sequence's query rows per kv head in one 128-row
   // attention item; chain drafts only, outside a device-resident loop.
-  bool flow = k->use_flow && lm_head && !tree && !acap && MT * 16 <= kFlowRows && dh == 128;
+  bool flow = k->use_flow && lm_head && !tree && !acap && MT * 16 <= kFlowRows && dh == 128 && !m->has_moe;
   for (int b = 0; b < B && flow; ++b) flow = (seqs[b].k + 1) * G <= kAttnRows;
   // Attention + merge + O GEMM as one launch (attn_o.hip): up to two row
   // tiles, head dim 128, an O GEMM of K = 4096 with at most one strip per CU;
@@ -1336,7 +1467,7 @@ hvd_status forward(hvd_kv_s* k, const std::vector<SeqMeta>& seqs, std::vector<Ro
       // many rows: MFMA-tiled kernel, weights read once per XCD
       const bool mlp = epi == EPI_SILU || family == PF_DOWN;
       const bool single = lm_head && ((mlp && (epi == EPI_SILU ? k->mlp_single_gu : k->mlp_single_down)) ||
-                                      (epi == EPI_LM && k->lm_single));
+                                      (family == PF_LM && k->lm_single));
       const int* force = k->tiled_force[family <= PF_LM ? family : 0];
       const bool forced = family <= PF_LM && force[0] && N % kTileBN[force[0] - 1] == 0;
       const TiledPlan plan = forced ? tiled_plan_forced(force[0] - 1, std::max(1, std::min(force[1], a.KT / 32)), MT, N,
@@ -1355,7 +1486,7 @@ hvd_status forward(hvd_kv_s* k, const std::vector<SeqMeta>& seqs, std::vector<Ro
     // k = 8 (gate/up 38.3 -> 36.0 us, down 23.9 -> 22.9 us per layer)
     const bool single = lm_head &&
                         ((epi == EPI_SILU && k->mlp_single_gu) || (family == PF_DOWN && k->mlp_single_down) ||
-                         (k->lm_single && epi == EPI_LM));
+                         (k->lm_single && family == PF_LM));
     if (mid_takes(MT, N, K)) {
       const MidPlan plan = mid_plan(MT, a.NT, a.KT, k->gemm_min_blocks, k->ns8_mt3, sx.gemm_part_bytes, k->gemm_force[family]);
       if (epi == EPI_LM) {
@@ -1378,6 +1509,76 @@ hvd_status forward(hvd_kv_s* k, const std::vector<SeqMeta>& seqs, std::vector<Ro
     }
     ProfScope ps(k, family, (double)N * K * 2.0);
     HIP_TRY(launch_gemm(epi, a, ns, splits, mblocks_g, mt_block_g, !single, s));
+    return HVD_OK;
+  };
+  // The MLP block of a layer with experts: router logits from the same operand
+  // as the dense GEMMs, the choice, the experts on the 32-bit normalised rows,
+  // and their output onto the residual stream with the next GEMM's operand.
+  auto moe_layer = [&](const LayerW& L, const float* gain_next) -> hvd_status {
+    const hvd_moe_config& mc = m->moe;
+    const int R = router_rows(mc);
+    {
+      GemmArgs a{};
+      a.W = (const uint4*)L.router;
+      a.Ahi = (const uint4*)k->Nhi;
+      a.Alo = (const uint4*)k->Nlo;
+      a.ss = k->ss;
+      a.ss_n = D / 16;
+      a.inv_dim = 1.f / D;
+      a.eps = c.rms_eps;
+      a.logits = k->moe_logits;
+      a.vocab = R;
+      a.part_val = k->moe_val;
+      a.part_idx = k->moe_idx;
+      if (hvd_status st = gemm(EPI_LM, a, R, D, PF_OTHER); st != HVD_OK) return st;
+    }
+    BlockNormArgs n{};
+    n.rows = M;
+    n.D = D;
+    n.eps = c.rms_eps;
+    n.x = k->X;
+    n.x_stride = D;
+    n.x_type = ET_F32;
+    {
+      BlockNormArgs pre = n;
+      pre.gain = L.g_mlp;
+      pre.h = k->moe_h;
+      pre.h_stride = D;
+      pre.h_type = ET_F32;
+      ProfScope ps(k, PF_OTHER, 0.0);
+      HIP_TRY(launch_route(route_args(mc.route, M, k->moe_logits, ET_F32, R, L.router_bias, k->moe_ids, k->moe_w), s));
+      HIP_TRY(launch_block_norm(pre, s));
+    }
+    {
+      ExpertsArgs a{};
+      a.w = L.experts;
+      a.x = k->moe_h;
+      a.x_stride = D;
+      a.x_type = ET_F32;
+      a.T = M;
+      a.k = mc.route.top_k;
+      a.ids = k->moe_ids;
+      a.weights = k->moe_w;
+      a.out = k->moe_y;
+      a.out_stride = D;
+      experts_carve(a, k->moe_work);
+      ProfScope ps(k, PF_EXPERTS, (double)std::min(M * a.k, a.w.E) * 3 * D * mc.ffn_dim * 2);
+      HIP_TRY(launch_experts(a, s));
+    }
+    n.y = k->moe_y;
+    n.y_stride = D;
+    n.y_type = ET_F32;
+    n.post_gain = L.g_post;
+    n.scale = mc.out_scale;
+    n.gain = gain_next;
+    n.x_out = k->X;
+    n.x_out_stride = D;
+    n.Nhi = k->Nhi;
+    n.Nlo = k->Nlo;
+    n.ss_out = k->ss;
+    n.MTtot = MT;
+    ProfScope ps(k, PF_OTHER, 0.0);
+    HIP_TRY(launch_block_norm(n, s));
     return HVD_OK;
   };
   double kv_bytes_cl[kAttnClasses] = {};  // KV bytes each attention launch reads
@@ -1537,6 +1738,11 @@ hvd_status forward(hvd_kv_s* k, const std::vector<SeqMeta>& seqs, std::vector<Ro
         if (hvd_status st = gemm(EPI_RESID, a, D, qd, PF_O); st != HVD_OK) return st;
       }
     }
+    const float* gain_next = (l + 1 < c.n_layers) ? m->layers[l + 1].g_attn : m->g_final;
+    if (m->experts_in(l)) {
+      if (hvd_status st = moe_layer(L, gain_next); st != HVD_OK) return st;
+      continue;
+    }
     {
       GemmArgs a{};
       a.W = (const uint4*)L.gu;
@@ -1557,7 +1763,7 @@ hvd_status forward(hvd_kv_s* k, const std::vector<SeqMeta>& seqs, std::vector<Ro
       a.Alo = (const uint4*)k->Alo;
       a.X = k->X;
       a.D = D;
-      a.gain_next = (l + 1 < c.n_layers) ? m->layers[l + 1].g_attn : m->g_final;
+      a.gain_next = gain_next;
       a.Nhi = k->Nhi;
       a.Nlo = k->Nlo;
       a.ss_out = k->ss;

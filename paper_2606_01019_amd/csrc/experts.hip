@@ -427,7 +427,6 @@ __global__ __launch_bounds__(64 * S::NW, 2) void experts_tiled(ExpertsArgs a, in
 // workgroups find the distinct experts of the call themselves, in ascending
 // order, so nothing runs before them: two launches in all.
 constexpr int kFewSlots = 256;   // slots (T * k) of the few-row form
-constexpr int kFewRows = 32;
 constexpr int kFewWaves = 8;
 
 // The distinct experts among n slots, ascending.

@@ -8,6 +8,8 @@
 
 #include <algorithm>
 
+#include "../../include/hvd.h"
+
 namespace hvd {
 
 // Element types of the operators' buffers (HVD_F16, HVD_BF16, HVD_F32).
@@ -18,6 +20,7 @@ constexpr int kMaxExperts = 512;
 constexpr int kMaxTopK = 16;
 constexpr int kMaxGroups = 64;
 constexpr int kMaxNormDim = 16384;
+constexpr int kFewRows = 32;               // most rows of the experts' few-row form
 constexpr int kMaxExpertRows = 1 << 18;  // rows of one call of the experts
 
 struct RouteArgs {
@@ -32,6 +35,10 @@ struct RouteArgs {
   float* weights;     // [rows][k]
 };
 hipError_t launch_route(const RouteArgs& a, hipStream_t s);
+// Checks of hvd_route's config, and its arguments as the launcher takes them (operators.cpp).
+hvd_status check_route_config(const hvd_route_config* c);
+RouteArgs route_args(const hvd_route_config& c, int rows, const void* logits, int dtype, int64_t stride,
+                     const float* bias, int32_t* ids, float* weights);
 
 // v = y (normalised, times post_gain, where post_gain is given) times gate;
 // x_out = x + scale * v; h = x_out normalised, times gain.

@@ -13,23 +13,7 @@
 
 using namespace hvd;
 
-struct hvd_experts_s {
-  hvd_experts_config cfg;
-  ExpertsW w;
-  void* base = nullptr;
-  bool owned = false;
-};
-
-namespace {
-
-bool float_type(int t) { return t == HVD_F16 || t == HVD_BF16 || t == HVD_F32; }
-
-bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
-
-hvd_status launched(hipError_t e, const char* what) {
-  if (e == hipSuccess) return HVD_OK;
-  return set_err(HVD_ERR_DEVICE, std::string(what) + ": " + hipGetErrorString(e));
-}
+namespace hvd {
 
 hvd_status check_route_config(const hvd_route_config* c) {
   if (!c) return set_err(HVD_ERR_ARG, "null config");
@@ -49,6 +33,26 @@ RouteArgs route_args(const hvd_route_config& c, int rows, const void* logits, in
                      const float* bias, int32_t* ids, float* weights) {
   return RouteArgs{logits, stride, dtype, rows, c.n_experts, c.top_k, c.score == HVD_SCORE_SIGMOID, c.n_groups,
                    c.top_groups, c.renorm != 0, c.scale, bias, ids, weights};
+}
+
+}  // namespace hvd
+
+struct hvd_experts_s {
+  hvd_experts_config cfg;
+  ExpertsW w;
+  void* base = nullptr;
+  bool owned = false;
+};
+
+namespace {
+
+bool float_type(int t) { return t == HVD_F16 || t == HVD_BF16 || t == HVD_F32; }
+
+bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
+hvd_status launched(hipError_t e, const char* what) {
+  if (e == hipSuccess) return HVD_OK;
+  return set_err(HVD_ERR_DEVICE, std::string(what) + ": " + hipGetErrorString(e));
 }
 
 hvd_status check_experts_config(const hvd_experts_config* c) {

@@ -22,7 +22,8 @@ EXPORTS = ("hvd_model_bytes", "hvd_model_load", "hvd_model_free", "hvd_kv_bytes"
            "hvd_kv_free_pages", "hvd_profile_enable", "hvd_profile_read", "hvd_kv_set_option", "hvd_last_error",
            "hvd_async_begin", "hvd_async_step", "hvd_async_end", "hvd_verify_noalloc", "hvd_flow_trace",
            "hvd_measure_mfma_peak", "hvd_route", "hvd_experts_bytes", "hvd_experts_load", "hvd_experts_free",
-           "hvd_experts_workspace", "hvd_experts_forward", "hvd_block_norm")
+           "hvd_experts_workspace", "hvd_experts_forward", "hvd_block_norm", "hvd_model_bytes_moe",
+           "hvd_kv_bytes_moe", "hvd_model_load_moe")
 HVD_OPT_GRAPHS = 1
 HVD_OPT_MLP_SINGLE = 2
 HVD_OPT_LM_SINGLE = 3
@@ -44,9 +45,17 @@ MAX_TREE_NODES = 63  # nodes per token tree (hvd_verify_tree)
 LAYER_TENSORS = ("attn_norm", "wq", "wk", "wv", "wo", "mlp_norm", "wg", "wu", "wd")
 
 
-def tensor_names(n_layers: int):
-    """Canonical order of the tensors hvd_model_load takes (include/hvd.h)."""
-    return (["embed"] + [f"layers.{l}.{n}" for l in range(n_layers) for n in LAYER_TENSORS]
+MOE_LAYER_TENSORS = LAYER_TENSORS[:6] + ("router", "router_bias", "experts_gate", "experts_up", "experts_down",
+                                         "post_norm")
+OPTIONAL_TENSORS = ("router_bias", "post_norm")
+
+
+def tensor_names(n_layers: int, first_moe_layer: int = None):
+    """Canonical order of the tensors hvd_model_load takes (include/hvd.h);
+    layers from first_moe_layer on are expert layers (hvd_model_load_moe)."""
+    moe = n_layers if first_moe_layer is None else first_moe_layer
+    return (["embed"] + [f"layers.{l}.{n}" for l in range(n_layers)
+                         for n in (LAYER_TENSORS if l < moe else MOE_LAYER_TENSORS)]
             + ["final_norm", "lm_head"])
 
 
@@ -66,6 +75,26 @@ class Config(ctypes.Structure):
     def from_model_config(cls, c):
         return cls(c.n_layers, c.d_model, c.n_q_heads, c.n_kv_heads, c.head_dim, c.ffn_dim, c.vocab,
                    c.max_draft, c.page_size, c.max_pos, c.rope_theta, c.rms_eps)
+
+
+class RouteConfig(ctypes.Structure):
+    _fields_ = [("n_experts", ctypes.c_int32), ("top_k", ctypes.c_int32), ("score", ctypes.c_int32),
+                ("n_groups", ctypes.c_int32), ("top_groups", ctypes.c_int32), ("renorm", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+class MoeConfig(ctypes.Structure):
+    _fields_ = [("first_layer", ctypes.c_int32), ("ffn_dim", ctypes.c_int32), ("route", RouteConfig),
+                ("out_scale", ctypes.c_float), ("post_norm", ctypes.c_int32)]
+
+    @classmethod
+    def from_moe_config(cls, m):
+        return cls(m.first_layer, m.ffn_dim,
+                   RouteConfig(m.n_experts, m.top_k, SCORES[m.score], m.n_groups, m.top_groups, int(m.renorm), m.scale),
+                   m.out_scale, int(m.post_norm))
 
 
 _lib = None
@@ -117,6 +146,9 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "hvd_experts_workspace": (SZ, [P, I32, I32, I32]),
         "hvd_experts_forward": (I32, [P, I32, I32, P, I32, I64, P, P, P, I64, P, SZ, P]),
         "hvd_block_norm": (I32, [P, I32, I32, P]),
+        "hvd_model_bytes_moe": (SZ, [P, P]),
+        "hvd_kv_bytes_moe": (SZ, [P, P, I32, I32]),
+        "hvd_model_load_moe": (I32, [P, P, P, P, SZ, P, ctypes.POINTER(P)]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -156,26 +188,31 @@ def _stream(stream):
 
 class Model:
     """Target model on the GPU.  ``tensors`` maps canonical names (see
-    workloads.weights) to uint16 bf16 arrays, or is a list in canonical order."""
+    workloads.weights) to uint16 bf16 arrays, or is a list in canonical order.
+    ``moe`` (fields of workloads.configs.MoeConfig): a decoder whose layers
+    from moe.first_layer on have experts; their router_bias, and post_norm
+    without moe.post_norm, may be absent (None in a list)."""
 
-    def __init__(self, cfg, tensors, names=None, stream=None):
+    def __init__(self, cfg, tensors, names=None, stream=None, moe=None):
         import torch
         self.lib = load_library()
         self.cfg = cfg
         self.ccfg = Config.from_model_config(cfg)
+        self.moe = moe
+        self.cmoe = ctypes.pointer(MoeConfig.from_moe_config(moe)) if moe is not None else None
         if isinstance(tensors, dict):
-            arrs = [np.ascontiguousarray(tensors[n], dtype=np.uint16) for n in tensor_names(cfg.n_layers)]
-        else:
-            arrs = [np.ascontiguousarray(t, dtype=np.uint16) for t in tensors]
-        ptrs = (ctypes.c_void_p * len(arrs))(*[a.ctypes.data for a in arrs])
-        nbytes = self.lib.hvd_model_bytes(ctypes.byref(self.ccfg))
+            want = tensor_names(cfg.n_layers, moe.first_layer if moe is not None else None)
+            tensors = [tensors.get(n) if n.rsplit(".", 1)[-1] in OPTIONAL_TENSORS else tensors[n] for n in want]
+        arrs = [np.ascontiguousarray(t, dtype=np.uint16) if t is not None else None for t in tensors]
+        ptrs = (ctypes.c_void_p * len(arrs))(*[a.ctypes.data if a is not None else None for a in arrs])
+        nbytes = self.lib.hvd_model_bytes_moe(ctypes.byref(self.ccfg), self.cmoe)
         if nbytes == 0:
             raise HvdError(HVD_ERR_ARG, "unsupported config")
         self.buf = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
         self.stream = stream
         h = ctypes.c_void_p()
-        _check(self.lib.hvd_model_load(ctypes.byref(self.ccfg), ptrs, ctypes.c_void_p(self.buf.data_ptr()),
-                                       nbytes, _stream(stream), ctypes.byref(h)))
+        _check(self.lib.hvd_model_load_moe(ctypes.byref(self.ccfg), self.cmoe, ptrs, ctypes.c_void_p(self.buf.data_ptr()),
+                                           nbytes, _stream(stream), ctypes.byref(h)))
         self.handle = h
 
     def close(self):
@@ -200,7 +237,7 @@ class KVCache:
         import torch
         self.lib = model.lib
         self.model = model
-        nbytes = self.lib.hvd_kv_bytes(ctypes.byref(model.ccfg), max_seqs, n_pages)
+        nbytes = self.lib.hvd_kv_bytes_moe(ctypes.byref(model.ccfg), model.cmoe, max_seqs, n_pages)
         if nbytes == 0:
             raise HvdError(HVD_ERR_ARG, "bad max_seqs / n_pages")
         self.buf = torch.empty(nbytes, dtype=torch.uint8, device="cuda")

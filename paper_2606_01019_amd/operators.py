@@ -8,15 +8,7 @@ tensors' device and returns without waiting; results are new tensors unless
 
 import ctypes
 
-from .hvd import HVD_ERR_ARG, HvdError, _check, load_library
-
-_SCORES = {"softmax": 0, "sigmoid": 1}
-
-
-class RouteConfig(ctypes.Structure):
-    _fields_ = [("n_experts", ctypes.c_int32), ("top_k", ctypes.c_int32), ("score", ctypes.c_int32),
-                ("n_groups", ctypes.c_int32), ("top_groups", ctypes.c_int32), ("renorm", ctypes.c_int32),
-                ("scale", ctypes.c_float)]
+from .hvd import HVD_ERR_ARG, SCORES, HvdError, RouteConfig, _check, load_library
 
 
 class ExpertsConfig(ctypes.Structure):
@@ -112,12 +104,12 @@ def route(logits, top_k, *, score="softmax", bias=None, n_groups=1, top_groups=1
     key = (E, top_k, score, n_groups, top_groups, renorm, scale)
     cfg = _configs.get(key)
     if cfg is None:
-        if score not in _SCORES:
-            _refuse(f"score must be one of {sorted(_SCORES)}")
+        if score not in SCORES:
+            _refuse(f"score must be one of {sorted(SCORES)}")
         if len(_configs) >= 256:
             _configs.clear()
         # (an address that stays: the library reads the config during the call only)
-        cfg = _configs[key] = ctypes.pointer(RouteConfig(E, top_k, _SCORES[score], n_groups, top_groups, bool(renorm), scale))
+        cfg = _configs[key] = ctypes.pointer(RouteConfig(E, top_k, SCORES[score], n_groups, top_groups, bool(renorm), scale))
     if not 1 <= top_k <= 16:
         _refuse("top_k must be in [1, 16]")
     bp = _vector(bias, "bias", E, dev) if bias is not None else None

@@ -45,6 +45,24 @@ class ModelConfig:
         return d * self.q_dim + 2 * d * self.kv_dim + self.q_dim * d + 3 * d * self.ffn_dim
 
 
+@dataclass(frozen=True)
+class MoeConfig:
+    """The expert layers of a decoder: layers first_layer.. have n_experts
+    SwiGLU experts of ffn_dim each in place of the dense MLP, of which a row's
+    router chooses top_k."""
+    n_experts: int
+    top_k: int
+    ffn_dim: int
+    first_layer: int = 0
+    score: str = "softmax"      # or "sigmoid"
+    n_groups: int = 1
+    top_groups: int = 1
+    renorm: bool = True
+    scale: float = 1.0          # factor of the routing weights
+    out_scale: float = 1.0      # factor of the experts' output on the residual stream
+    post_norm: bool = False     # RMSNorm of the experts' output, with a gain of its own
+
+
 # 2 layers, d_model 256, 4/4 heads of 64, SwiGLU 1024, vocab 4096, theta 1e4.
 TINY = ModelConfig("tiny", 2, 256, 4, 4, 64, 1024, 4096, 1.0e4, max_pos=4096)
 
