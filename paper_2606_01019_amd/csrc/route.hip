@@ -25,6 +25,38 @@ namespace hvd {
 
 constexpr int kRouteRows = 4;  // rows (waves) per workgroup
 
+// Exchanges within a wave in the vector ALU (data-parallel permutes): an LDS
+// shuffle costs a round trip per step, and a row is k wave-wide maxima.
+template <int CTRL>
+__device__ __forceinline__ double dpp_d(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (uint32_t)u, CTRL, 0xf, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (uint32_t)(u >> 32), CTRL, 0xf, 0xf, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// Every lane gets f over all 64 lanes' values: neighbours, pairs of two (quad
+// permutes), of four and eight (mirrors), then across the four rows of 16.
+template <class F>
+__device__ __forceinline__ double wave_all_d(double v, F f) {
+  v = f(v, dpp_d<0xB1>(v));
+  v = f(v, dpp_d<0x4E>(v));
+  v = f(v, dpp_d<0x141>(v));
+  v = f(v, dpp_d<0x140>(v));
+  uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const auto l16 = __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false);
+  const auto h16 = __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+  v = f(__builtin_bit_cast(double, (uint64_t)h16[0] << 32 | l16[0]), __builtin_bit_cast(double, (uint64_t)h16[1] << 32 | l16[1]));
+  u = __builtin_bit_cast(uint64_t, v);
+  const auto l32 = __builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false);
+  const auto h32 = __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+  return f(__builtin_bit_cast(double, (uint64_t)h32[0] << 32 | l32[0]), __builtin_bit_cast(double, (uint64_t)h32[1] << 32 | l32[1]));
+}
+__device__ __forceinline__ double wave_max_d(double v) {
+  return wave_all_d(v, [](double a, double b) { return a > b ? a : b; });
+}
+__device__ __forceinline__ double wave_sum_d(double v) {
+  return wave_all_d(v, [](double a, double b) { return a + b; });
+}
 __device__ __forceinline__ double shfl_xor_d(double v, int o) {
   const uint64_t u = __builtin_bit_cast(uint64_t, v);
   const uint32_t lo = __shfl_xor((uint32_t)u, o), hi = __shfl_xor((uint32_t)(u >> 32), o);
@@ -59,8 +91,7 @@ __global__ __launch_bounds__(64 * kRouteRows) void route_rows(RouteArgs a) {
     l[i] = v;
     m = fmaxf(m, v);
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  m = (float)wave_max_d((double)m);  // (exact both ways)
   double s[P], c[P];
   if (a.sigmoid) {
 #pragma unroll
@@ -72,8 +103,7 @@ __global__ __launch_bounds__(64 * kRouteRows) void route_rows(RouteArgs a) {
       s[i] = l[i] > -INFINITY ? exp((double)l[i] - (double)m) : 0.0;
       sum += s[i];
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sum += shfl_xor_d(sum, o);
+    sum = wave_sum_d(sum);
 #pragma unroll
     for (int i = 0; i < P; ++i) s[i] = s[i] / sum;
   }
@@ -123,41 +153,31 @@ __global__ __launch_bounds__(64 * kRouteRows) void route_rows(RouteArgs a) {
     }
   }
 
-  // k rounds: the best of each lane, then of the wave
+  // k rounds: the wave's best value, then the lowest expert that has it
   int my_id = -1;
   double my_s = 0.0, total = 0.0;
   for (int r = 0; r < a.k; ++r) {
-    double best = kNone, bs = 0.0;
-    int be = 0x7fffffff;
+    double best = c[0];
 #pragma unroll
-    for (int i = 0; i < P; ++i)
-      if (c[i] > best) {  // experts ascend: ties keep the lower one
-        best = c[i];
-        bs = s[i];
-        be = i * 64 + lane;
-      }
-    double wb = best;
-    int we = be;
+    for (int i = 1; i < P; ++i) best = c[i] > best ? c[i] : best;
+    best = wave_max_d(best);
+    if (!(best > kNone)) break;  // no expert is left
+    bool found = false;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const double ob = shfl_xor_d(wb, o);
-      const int oe = __shfl_xor(we, o);
-      if (ob > wb || (ob == wb && oe < we)) {
-        wb = ob;
-        we = oe;
+    for (int i = 0; i < P; ++i) {
+      const uint64_t has = __builtin_amdgcn_ballot_w64(c[i] == best);
+      if (!found && has) {  // (wave-uniform)
+        found = true;
+        const int src = __builtin_ctzll(has);
+        const double ws = read_lane_d(s[i], src);
+        total += ws;
+        if (lane == r) {
+          my_id = i * 64 + src;
+          my_s = ws;
+        }
+        if (lane == src) c[i] = kNone;
       }
     }
-    we = __builtin_amdgcn_readfirstlane(we);
-    if (we == 0x7fffffff) break;  // no expert is left
-    const double ws = read_lane_d(bs, we & 63);
-    total += ws;
-    if (lane == r) {
-      my_id = we;
-      my_s = ws;
-    }
-#pragma unroll
-    for (int i = 0; i < P; ++i)
-      if (i * 64 + lane == we) c[i] = kNone;
   }
   if (lane < a.k) {
     if (a.renorm) my_s = total > 0.0 ? my_s / total : 0.0;
