@@ -124,6 +124,7 @@ __global__ __launch_bounds__(256) void experts_sort(ExpertsArgs a) {
         ++p;
       }
     });
+  if (e == 0) a.arrived[tid] = 0u;  // (before the products that count on it)
   if (tid == 0) {
     a.off[e] = base;
     a.cnt[e] = s_eq[0] + s_eq[1] + s_eq[2] + s_eq[3];
@@ -137,11 +138,18 @@ __global__ __launch_bounds__(256) void experts_sort(ExpertsArgs a) {
 // numbered expert by expert, within one by column block, then row tile, and
 // each XCD takes a run of them: an expert's row tiles of one column block are
 // neighbours there and share its weights in that XCD's L2.
+//
+// SPLIT (one workgroup per CU): the tiles past the last whole round of CUs
+// would leave most of them idle for as long as a tile takes; their K range is
+// dealt to as many workgroups as fit one round, kMaxSplits at most.
+constexpr int kTileCUs = 256, kMaxSplits = 4;
 struct Tile {
   int e, row0, rows, cb;  // expert, first place, rows (0: no such tile), column block
+  int kb, ke;             // K steps (kb even)
+  int left, split, splits;  // tile shared by several workgroups: its number, this part, the parts
 };
-template <int BM>
-__device__ __forceinline__ Tile find_tile(const ExpertsArgs& a, int CB) {
+template <int BM, bool SPLIT>
+__device__ __forceinline__ Tile find_tile(const ExpertsArgs& a, int CB, int KT) {
   const int lane = threadIdx.x & 63;
   int nt[8], sum = 0;
 #pragma unroll
@@ -157,10 +165,26 @@ __device__ __forceinline__ Tile find_tile(const ExpertsArgs& a, int CB) {
     if (lane >= o) inc += v;
   }
   const int total = __builtin_amdgcn_readlane(inc, 63) * CB;
-  if ((int)blockIdx.x >= total) return {0, 0, 0, 0};
-  // XCD x (= id % 8 under the round-robin dispatch) takes the x-th run of positions
-  const int x = blockIdx.x & 7, q = total >> 3;
-  const int at = x * q + min(x, total & 7) + (blockIdx.x >> 3);
+  const int id = blockIdx.x;
+  Tile t{0, 0, 0, 0, 0, KT, -1, 0, 1};
+  const int rest = SPLIT ? total % kTileCUs : 0, whole = total - rest;
+  const int splits = rest ? min(min(kTileCUs / rest, kMaxSplits), max(1, KT / 16)) : 1;
+  const int run = splits > 1 ? whole : total;  // tiles in one piece
+  int at;
+  if (id < run) {
+    // XCD x (= id % 8 under the round-robin dispatch) takes the x-th run of positions
+    const int x = id & 7, q = run >> 3;
+    at = x * q + min(x, run & 7) + (id >> 3);
+  } else {
+    const int u = id - run;
+    if (u >= (total - run) * splits) return t;
+    t.left = __builtin_amdgcn_readfirstlane(u / splits);
+    t.split = u - t.left * splits;
+    t.splits = splits;
+    t.kb = __builtin_amdgcn_readfirstlane(t.split * KT / splits) & ~1;
+    t.ke = t.split + 1 == splits ? KT : __builtin_amdgcn_readfirstlane((t.split + 1) * KT / splits) & ~1;
+    at = run + t.left;
+  }
   int before = (inc - sum) * CB, e = -1, r = 0, nte = 1;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -176,26 +200,41 @@ __device__ __forceinline__ Tile find_tile(const ExpertsArgs& a, int CB) {
   r = __builtin_amdgcn_readlane(r, src);
   nte = __builtin_amdgcn_readlane(nte, src);
   const int cb = r / nte, tile = r - cb * nte;
-  return {e, a.off[e] + tile * BM, min(BM, a.cnt[e] - tile * BM), cb};
+  t.e = e;
+  t.row0 = a.off[e] + tile * BM;
+  t.rows = min(BM, a.cnt[e] - tile * BM);
+  t.cb = cb;
+  return t;
 }
 
 // ---------------------------------------------------------------- products, many rows
 
-// The grouped product on MFMA 32x32x16, the ring of gemm_tiled: a workgroup of
-// WY x WX waves owns BM = 32 WM WY places of one expert's list and BN = 32 WN WX
-// columns.  Every 32-wide K step's operands are copied straight into a ring of
-// LDS slots (global_load_lds), ST - 1 steps ahead of the MFMAs; the rows'
-// operand fragments are gathered there from wherever the rows are (each lane
-// copies 16 bytes of one row), so no gathered copy of x exists.  Places past
-// the list repeat its last one and are not stored; a tile belongs to one
-// expert.
+// The grouped product on MFMA 32x32x16: a workgroup of WY x WX waves owns
+// BM = 32 WM WY places of one expert's list and BN = 32 WN WX columns.  The
+// operands are copied straight into rings of LDS slots (global_load_lds) well
+// ahead of the MFMAs: weights, 1 KB fragments of 16 columns, in 32-wide K steps;
+// rows in slabs of 64, every second step.  The rows are gathered there from
+// wherever they are, so no gathered copy of x exists; a copy instruction takes
+// 8 rows of 128 bytes, whole cache lines (16 rows of 64 bytes come from L2 at 37
+// bytes per ns and CU, lines at 126), and the 16-byte pieces of a line are
+// permuted by the row's low bits so that reading 32 rows of one piece spreads
+// over the LDS banks.  Weights fresh from memory come at 28 bytes per ns and CU,
+// the whole chip's 7.3 TB/s: what bounds these products until an expert has
+// hundreds of rows.
+// Places past the list repeat its last one and are not stored; a tile belongs
+// to one expert.
 // GU: rows of x, silu(gate) * up out (OP: as a pair); else rows of that
 // product, the expert's output out.  AP: the row operand is a pair.
 template <int WY_, int WX_, int WM_, int WN_>
 struct TileShape {
   static constexpr int WY = WY_, WX = WX_, WM = WM_, WN = WN_, NW = WY * WX;
   static constexpr int BM = 32 * WM * WY, BN = 32 * WN * WX;
+  static constexpr int LDS = NW == 8 ? 160 * 1024 : 80 * 1024;  // one or two workgroups per CU
+  static constexpr bool SPLIT = NW == 8;                          // tiles past the last whole round are shared
 };
+
+using T64 = TileShape<1, 4, 2, 2>;   // 64 x 256, 4 waves: two workgroups per CU
+using T128 = TileShape<2, 4, 2, 2>;  // 128 x 256, 8 waves: one workgroup per CU
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 template <bool BF>
@@ -232,60 +271,76 @@ __device__ __forceinline__ void pair8(const float (&v)[8], uint4& hi, uint4& lo)
   to16x8<BF>(r, lo);
 }
 
+// f(constant of value i), i clamped to [0, N)
+template <int N, class F>
+__device__ __forceinline__ void with_constant(int i, F&& f) {
+  if constexpr (N == 1) {
+    f(std::integral_constant<int, 0>{});
+  } else {
+    if (i >= N - 1) f(std::integral_constant<int, N - 1>{});
+    else with_constant<N - 1>(i, f);
+  }
+}
+
 constexpr int kRegionStride = 72;  // floats per row of a wave's epilogue region: rows 4 apart land 32 banks apart
 constexpr int kRegionBytes = 32 * kRegionStride * 4;
+
+// Copies that may still be in flight when iteration i waits (before its own):
+// every iteration t copies a K step of weights (SW - 1 steps ahead, cw copies),
+// an even one a slab before it (PA slabs ahead, ca copies).  The wait covers
+// the weights of step i + 1 and, where i is odd, the slab of step i + 1.
+constexpr int in_flight(bool odd, int SW, int PA, int cw, int ca) {
+  auto issued = [&](int t) { return cw + ((odd ? t + 1 : t) % 2 == 0 ? ca : 0); };  // at iteration i + t
+  int w = 0;
+  for (int t = 3 - SW; t <= -1; ++t) w += issued(t);
+  if (!odd) return w;
+  int a = cw;  // the weights of the slab's own iteration follow it
+  for (int t = 2 - 2 * PA; t <= -1; ++t) a += issued(t);
+  return a < w ? a : w;
+}
 
 template <class S, bool GU, bool BF, bool AP, bool OP>
 __global__ __launch_bounds__(64 * S::NW, 2) void experts_tiled(ExpertsArgs a, int CB) {
   constexpr int NW = S::NW, WM = S::WM, WN = S::WN, BM = S::BM, BN = S::BN;
-  constexpr int AF = BM / 16, NA = AP ? 2 * AF : AF, WF = BN / 16, NF = NA + WF;
-  constexpr int LPT = NF / NW;
-  static_assert(NF % NW == 0, "fragments per step");
-  constexpr int BUDGET = NW == 8 ? 150 * 1024 : 76 * 1024;  // one or two workgroups per CU
-  constexpr int ST0 = BUDGET / (NF * 1024);
-  constexpr int ST = ST0 < 3 ? 3 : (ST0 > 6 ? 6 : ST0);
-  __shared__ u32x4 sbuf[ST][NF][64];
-  static_assert(NW * kRegionBytes <= (int)sizeof(sbuf), "the epilogue's regions fit the ring");
+  constexpr int NP = AP ? 2 : 1;                           // parts of the row operand
+  constexpr int WF = BN / 16, WPW = WF / NW;               // weight fragments of a step; per wave
+  constexpr int RPW = BM / 8 / NW;                         // row copies (8 rows) per wave, part and slab
+  constexpr int SLAB = NP * BM * 128, STEP = WF * 1024;    // bytes
+  constexpr int PA = 3 * SLAB + 4 * STEP <= S::LDS ? 2 : 1, SA = PA + 1;  // slabs ahead; slots
+  constexpr int SW0 = (S::LDS - SA * SLAB) / STEP, SW = SW0 > 6 ? 6 : SW0;
+  static_assert(WF % NW == 0 && BM % (8 * NW) == 0 && SW >= 3, "every wave copies alike");
+  __shared__ u32x4 sbuf[(SA * SLAB + SW * STEP) / 16];
+  static_assert(NW * kRegionBytes + 16 <= (int)sizeof(sbuf), "the epilogue's regions and a word fit the rings");
+  u32x4* const sw = sbuf + SA * SLAB / 16;
 
-  const Tile tl = find_tile<BM>(a, CB);
+  constexpr bool SPLIT = GU && S::SPLIT;  // (the down product's K range is too short)
+  const int D = a.w.D, F = a.w.F;
+  const int K = GU ? D : F, N = GU ? 2 * F : D, KT = K / 32;
+  const Tile tl = find_tile<BM, SPLIT>(a, CB, KT);
   if (tl.rows == 0) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wy = wave / S::WX, wx = wave % S::WX;
-  const int D = a.w.D, F = a.w.F;
-  const int K = GU ? D : F, N = GU ? 2 * F : D, KT = K / 32;
 
-  const char* src[LPT];
-  uint32_t kstride[LPT];
+  const char *asrc[NP][RPW], *wsrc[WPW];
 #pragma unroll
-  for (int q = 0; q < LPT; ++q) {
-    const int f = q * NW + wave;
-    if (f < NA) {
-      const int p = tl.row0 + min(f % AF * 16 + (lane & 15), tl.rows - 1);
+  for (int q = 0; q < RPW; ++q) {
+    const int p = tl.row0 + min((q * NW + wave) * 8 + (lane >> 3), tl.rows - 1);
+    const int piece = ((lane & 7) ^ (lane >> 3)) * 8;
+    const int t = GU ? a.perm[p] / a.k : 0;
+#pragma unroll
+    for (int n = 0; n < NP; ++n) {
       const uint16_t* row;
-      if constexpr (GU) {
-        const int t = a.perm[p] / a.k;
-        if constexpr (AP) row = (f < AF ? a.xhi : a.xlo) + (size_t)t * D;
-        else row = (const uint16_t*)a.x + t * a.x_stride;
-      } else {
-        row = (f < AF ? a.hhi : a.hlo) + (size_t)p * F;
-      }
-      src[q] = (const char*)(row + (lane >> 4) * 8);
-      kstride[q] = 64;
-    } else {
-      const int st = min(tl.cb * WF + (f - NA), N / 16 - 1);  // strips past the matrix: any valid one
-      src[q] = (const char*)((GU ? a.w.gu : a.w.dn) + (((size_t)tl.e * (N / 64) + (st >> 2)) * KT * 4 + (st & 3)) * 512 + lane * 8);
-      kstride[q] = 4096;
+      if constexpr (GU && AP) row = (n ? a.xlo : a.xhi) + (size_t)t * D;
+      else if constexpr (GU) row = (const uint16_t*)a.x + t * a.x_stride;
+      else row = (n ? a.hlo : a.hhi) + (size_t)p * F;
+      asrc[n][q] = (const char*)(row + piece);
     }
   }
-  // Steps past the range re-copy the last one, so every iteration issues the
-  // same number of copies (constant vmcnt targets).
-  auto issue = [&](int slot, int kt) __attribute__((always_inline)) {
-    kt = min(kt, KT - 1);
 #pragma unroll
-    for (int q = 0; q < LPT; ++q)
-      __builtin_amdgcn_global_load_lds((const void*)(src[q] + (size_t)kt * kstride[q]),
-                                       (lds_void*)&sbuf[slot][q * NW + wave][0], 16, 0, 0);
-  };
+  for (int q = 0; q < WPW; ++q) {
+    const int st = min(tl.cb * WF + q * NW + wave, N / 16 - 1);  // strips past the matrix: any valid one
+    wsrc[q] = (const char*)((GU ? a.w.gu : a.w.dn) + (((size_t)tl.e * (N / 64) + (st >> 2)) * KT * 4 + (st & 3)) * 512 + lane * 8);
+  }
 
   f32x16 acc[WM][WN];
 #pragma unroll
@@ -295,28 +350,51 @@ __global__ __launch_bounds__(64 * S::NW, 2) void experts_tiled(ExpertsArgs a, in
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-  // 32 rows (columns) of one 16-wide K sub-step s: lane l takes row l%32, K 16s + 8(l/32)..+8
+  // 32 columns of one 16-wide K sub-step s: lane l takes column l%32, K 16s + 8(l/32)..+8
   const int fl = (lane & 15) + 16 * (lane >> 5), fo = (lane >> 4) & 1;
-  // Step j lives in slot j % ST.  Iteration i multiplies the first half of step
-  // i while its second half is read; then it waits until step i+1 has landed,
-  // refills the slot of step i-1, and multiplies the second half while the
-  // first half of step i+1 is read.  L of the wave's WM row blocks hold rows of
-  // the list: the others are neither read nor multiplied (a wave without any
-  // only copies).
-  auto k_loop = [&](auto live) __attribute__((always_inline)) {
-    constexpr int L = decltype(live)::value;
+  const int live = (tl.rows - wy * 32 * WM + 31) / 32;  // row blocks of this wave that hold rows
+  // Iteration i multiplies the first half of step i while its second half is
+  // read; then it waits until step i+1 has landed, refills the slots of step
+  // i-1 (and slab i/2-1), and multiplies the second half while the first half of
+  // step i+1 is read.  L of the wave's WM row blocks hold rows of the list: the
+  // others are neither read nor multiplied (a wave without any only copies).
+  // Likewise the wave makes G of its RPW row copies.
+  auto k_loop = [&](auto blocks, auto copies) __attribute__((always_inline)) {
+    constexpr int L = decltype(blocks)::value, G = decltype(copies)::value, CA = NP * G;
+    const int m0 = tl.kb / 2, m1 = (tl.ke - 1) / 2;
+    // (steps and slabs past the range re-copy the last one: the counts stay constant)
+    auto issue_w = [&](int slot, int kt) __attribute__((always_inline)) {
+      kt = min(kt, tl.ke - 1);
+#pragma unroll
+      for (int q = 0; q < WPW; ++q)
+        __builtin_amdgcn_global_load_lds((const void*)(wsrc[q] + (size_t)kt * 4096),
+                                         (lds_void*)(sw + (slot * WF + q * NW + wave) * 64), 16, 0, 0);
+    };
+    auto issue_a = [&](int slot, int m) __attribute__((always_inline)) {
+      m = min(m, m1);
+#pragma unroll
+      for (int n = 0; n < NP; ++n)
+#pragma unroll
+        for (int q = 0; q < G; ++q)
+          __builtin_amdgcn_global_load_lds((const void*)(asrc[n][q] + (size_t)m * 128),
+                                           (lds_void*)(sbuf + (slot * SLAB + n * BM * 128 + (q * NW + wave) * 1024) / 16), 16, 0, 0);
+    };
     struct Ops {
       u32x4 ah[L ? L : 1], al[AP && L ? L : 1], bw[WN];
     };
-    auto read_ops = [&](int buf, int s, Ops& o) __attribute__((always_inline)) {
+    // sub-step s (0..3) of slab slot as_, of which weight slot ws holds s % 2
+    auto read_ops = [&](int as_, int ws, int s, Ops& o) __attribute__((always_inline)) {
       if constexpr (L > 0) {
+        const int piece = (s * 2 + (lane >> 5)) ^ (lane & 7);
+        const u32x4* ap = sbuf + as_ * (SLAB / 16) + (wy * WM * 32 + (lane & 31)) * 8 + piece;
 #pragma unroll
         for (int i = 0; i < L; ++i) {
-          o.ah[i] = sbuf[buf][wy * 2 * WM + 2 * i + fo][fl + 32 * s];
-          if constexpr (AP) o.al[i] = sbuf[buf][AF + wy * 2 * WM + 2 * i + fo][fl + 32 * s];
+          o.ah[i] = ap[i * 256];
+          if constexpr (AP) o.al[i] = ap[BM * 8 + i * 256];
         }
+        const u32x4* wp = sw + (ws * WF + wx * 2 * WN + fo) * 64 + fl + 32 * (s & 1);
 #pragma unroll
-        for (int j = 0; j < WN; ++j) o.bw[j] = sbuf[buf][NA + wx * 2 * WN + 2 * j + fo][fl + 32 * s];
+        for (int j = 0; j < WN; ++j) o.bw[j] = wp[j * 128];
       }
     };
     auto mfma_ops = [&](const Ops& o, auto&& between) __attribute__((always_inline)) {
@@ -334,33 +412,98 @@ __global__ __launch_bounds__(64 * S::NW, 2) void experts_tiled(ExpertsArgs a, in
       __builtin_amdgcn_sched_barrier(0);
     };
     Ops o0, o1;
-    vm_wait<LPT * (ST - 2)>();
-    block_barrier();
-    read_ops(0, 0, o0);
-    int slot = 0;
-    for (int i = 0; i < KT; ++i) {
-      const int next = slot + 1 == ST ? 0 : slot + 1, prev = slot == 0 ? ST - 1 : slot - 1;
-      mfma_ops(o0, [&]() { read_ops(slot, 1, o1); });
-      vm_wait<LPT * (ST - 3)>();
-      block_barrier();
-      issue(prev, i + ST - 1);
-      mfma_ops(o1, [&]() { read_ops(next, 0, o0); });
-      slot = next;
-    }
-  };
+    // what iterations before the first would have copied, in their order
+    constexpr int T0 = 2 * PA > SW - 1 ? 2 * PA : SW - 1;
 #pragma unroll
-  for (int st = 0; st < ST - 1; ++st) issue(st, st);
-  const int live = (tl.rows - wy * 32 * WM + 31) / 32;  // row blocks of this wave that hold rows
-  if (live >= WM) k_loop(std::integral_constant<int, WM>{});
-  else if (WM > 1 && live == 1) k_loop(std::integral_constant<int, 1>{});
-  else k_loop(std::integral_constant<int, 0>{});
+    for (int t = -T0; t < 0; ++t) {
+      if (t % 2 == 0 && t / 2 + PA >= 0) issue_a(t / 2 + PA, m0 + t / 2 + PA);
+      if (t + SW - 1 >= 0) issue_w(t + SW - 1, tl.kb + t + SW - 1);
+    }
+    vm_wait<in_flight(true, SW, PA, WPW, CA)>();
+    block_barrier();
+    read_ops(0, 0, 0, o0);
+    int ws = 0, as_ = 0;  // slots of step i and of its slab
+    auto iteration = [&](auto parity, int i) __attribute__((always_inline)) {
+      constexpr int ODD = decltype(parity)::value;
+      const int wn = ws + 1 == SW ? 0 : ws + 1, wprev = ws == 0 ? SW - 1 : ws - 1;
+      const int an = ODD ? (as_ + 1 == SA ? 0 : as_ + 1) : as_, aprev = as_ == 0 ? SA - 1 : as_ - 1;
+      mfma_ops(o0, [&]() { read_ops(as_, ws, 2 * ODD + 1, o1); });
+      vm_wait<in_flight(ODD, SW, PA, WPW, CA)>();
+      block_barrier();
+      if constexpr (!ODD) issue_a(aprev, i / 2 + PA);
+      issue_w(wprev, i + SW - 1);
+      mfma_ops(o1, [&]() { read_ops(an, wn, ODD ? 0 : 2, o0); });
+      ws = wn;
+      as_ = an;
+    };
+    int i = tl.kb;  // (even)
+    for (; i + 2 <= tl.ke; i += 2) {
+      iteration(std::integral_constant<int, 0>{}, i);
+      iteration(std::integral_constant<int, 1>{}, i + 1);
+    }
+    if (i < tl.ke) iteration(std::integral_constant<int, 0>{}, i);
+  };
+  auto with_blocks = [&](auto copies) __attribute__((always_inline)) {
+    with_constant<WM + 1>(live, [&](auto blocks) __attribute__((always_inline)) { k_loop(blocks, copies); });
+  };
+  if (RPW > 1 && tl.rows <= BM / 2) with_blocks(std::integral_constant<int, RPW / 2>{});
+  else with_blocks(std::integral_constant<int, RPW>{});
   vm_wait<0>();  // no copy may land after the ring is reused or released
   __syncthreads();
+
+  if constexpr (SPLIT) {
+    if (tl.splits > 1) {
+      // A shared tile: each part goes out in lane-native order with device-scope
+      // stores and is counted; the last to arrive sums the parts in K order
+      // (the same order whoever is last) and goes on as if it had them all.
+      constexpr int WAVE_BYTES = WM * WN * 64 * 64;  // 16 floats per lane and 32 x 32 block
+      const uint32_t mine = ((uint32_t)(tl.left * tl.splits) * NW + wave) * WAVE_BYTES + lane * 16;
+#pragma unroll
+      for (int i = 0; i < WM; ++i)
+        if (i < live)
+#pragma unroll
+          for (int j = 0; j < WN; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+              st_f4_dev(a.part, mine + (uint32_t)tl.split * NW * WAVE_BYTES + ((i * WN + j) * 4 + g) * 1024,
+                        float4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]});
+      vm_wait<0>();  // this wave's stores are done
+      // (in the ring: a second LDS variable makes the compiler wait for every
+      // copy in flight before each LDS read of the K loop)
+      int& last_part = *(int*)&sbuf[sizeof(sbuf) / 16 - 1];
+      __syncthreads();
+      if (threadIdx.x == 0) last_part = atomicAdd(a.arrived + tl.left, 1u) == (uint32_t)tl.splits - 1u;
+      __syncthreads();
+      if (!last_part) return;  // (the epilogue's regions lie below it)
+#pragma unroll
+      for (int i = 0; i < WM; ++i)
+        if (i < live)
+#pragma unroll
+          for (int j = 0; j < WN; ++j) {
+            float4 v[kMaxSplits][4];  // all parts of the block on their way at once
+#pragma unroll
+            for (int q = 0; q < kMaxSplits; ++q)
+#pragma unroll
+              for (int g = 0; g < 4; ++g)
+                v[q][g] = ld_f4_dev(a.part, mine + (uint32_t)(q < tl.splits ? q : 0) * NW * WAVE_BYTES + ((i * WN + j) * 4 + g) * 1024);
+#pragma unroll
+            for (int q = 0; q < kMaxSplits; ++q)
+              if (q < tl.splits) {
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                  const float o[4] = {v[q][g].x, v[q][g].y, v[q][g].z, v[q][g].w};
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) acc[i][j][4 * g + e] = q ? acc[i][j][4 * g + e] + o[e] : o[e];
+                }
+              }
+          }
+    }
+  }
 
   // Blocks of 32 rows x 64 columns through the wave's LDS region, so that the
   // stores are 16 bytes of one row per lane (MFMA 32x32: element r of lane l is
   // row 8 (r/4) + 4 (l/32) + r%4, column l%32).
-  float* lds = (float*)&sbuf[0][0][0] + wave * (kRegionBytes / 4);
+  float* lds = (float*)sbuf + wave * (kRegionBytes / 4);
 #pragma unroll
   for (int i = 0; i < WM; ++i) {
 #pragma unroll
@@ -794,30 +937,29 @@ __global__ __launch_bounds__(256) void experts_combine(ExpertsArgs a) {
 
 // The form of a call, from its sizes alone (the host does not see the choice).
 // Measured with 64 experts of 4096 x 1024, top 8, unless said otherwise (us a
-// call, bf16; few-row form / 64-row tiles / 128-row tiles / 256-row tiles):
-//   16 rows 196 / 222 / 230 / -, 40 rows - / 248 / 259 / 266, 200 rows - / 394 / 314 / 315,
-//   848 rows - / 561 / 440 / 467; 2000 rows, 8 experts, top 2: - / 271 / 224 / 207.
-// * The few-row form up to 16 rows.  Up to 32 rows it multiplies two row tiles
-//   for every expert, which pays where the tiles of few experts would leave CUs
-//   without weights to stream: 32 rows, 8 experts, top 2: 46 / 128 / 72; 32 rows
-//   of 64 experts: 281 / 245 / 255.
-// * 64-row tiles (4 waves, several workgroups per CU) while an expert has few
-//   rows, if there are enough of them; 128-row tiles (8 waves) otherwise: 32 rows
-//   of 16 experts of 1024 x 512: - / 36 / 26.
-// * 256-row tiles where most tiles fill: each weight is copied half as often.
+// call, bf16; few-row form / tiles):
+//   16 rows 196 / 230; 32 rows 281 / 255; 32 rows of 8 experts, top 2: 46 / 72.
+// * The few-row form up to 16 rows, and up to 32, where it multiplies two row
+//   tiles for every expert, if the tiles of few experts would leave CUs without
+//   weights to stream.
+// * Tiles of 64 rows and 4 waves, two workgroups per CU, while an expert has few
+//   rows and there are enough tiles: 33 rows of 128 experts of 5120 x 704, top 4:
+//   255 against 269 with 128 rows (40 rows 257 / 259; 32 rows of 16 experts of 1024 x
+//   512, top 2, where they are too few: 36 / 26).
+// * Tiles of 128 rows above: 848 rows 410 against 492 with 64 rows (and 411 with 256;
+//   2048 rows 683, 863, 660; 2000 rows of 8 experts, top 2: 188, 233, 203).
 // With few rows per expert the products wait for weights, and silu(gate) * up
-// goes through the down product as a pair at no cost (40 rows: 259 -> 261); with
-// many it is one 16-bit value (848 rows: 480 -> 440).
-enum Form { FORM_FEW16, FORM_FEW32, FORM_T64_PAIR, FORM_T128_PAIR, FORM_T128, FORM_T256 };
-constexpr int kPairRows = 16;   // rows per expert below which the product stays a pair
-constexpr int kWideRows = 384;  // rows per expert from which 256-row tiles pay
+// goes through the down product as a pair at little cost (40 rows: 259 -> 261);
+// with many it is one 16-bit value (848 rows: 480 -> 440).
+enum Form { FORM_FEW16, FORM_FEW32, FORM_T64_PAIR, FORM_T128_PAIR, FORM_T128 };
+constexpr int kPairRows = 16;  // rows per expert below which the product stays a pair
 static Form form_of(const ExpertsArgs& a) {
-  const int n = a.T * a.k, per = n / a.w.E;  // rows per expert if spread evenly
-  const bool fills = (int64_t)std::min(n, a.w.E) * a.w.F >= 128 * 256;  // a 256-column tile (gate and up) per CU
+  const int n = a.T * a.k;
+  const bool fills = (int64_t)std::min(n, a.w.E) * a.w.F >= 128 * kTileCUs;  // a 256-column tile (gate and up) per CU
   if (a.T <= 16 && n <= kFewSlots) return FORM_FEW16;
   if (a.T <= kFewRows && n <= kFewSlots && !fills) return FORM_FEW32;
-  if (per < kPairRows) return fills ? FORM_T64_PAIR : FORM_T128_PAIR;
-  return per < kWideRows ? FORM_T128 : FORM_T256;
+  if (n / a.w.E >= kPairRows) return FORM_T128;
+  return fills ? FORM_T64_PAIR : FORM_T128_PAIR;
 }
 
 size_t experts_carve(ExpertsArgs& a, void* base) {
@@ -840,11 +982,14 @@ size_t experts_carve(ExpertsArgs& a, void* base) {
   a.pos = (int32_t*)take(n * 4);
   a.cnt = (int32_t*)take((size_t)a.w.E * 4);
   a.off = (int32_t*)take((size_t)a.w.E * 4);
-  a.hhi = (uint16_t*)take(n * F * 2);
-  a.hlo = pair || f <= FORM_T128_PAIR ? (uint16_t*)take(n * F * 2) : nullptr;
+  // (64 bytes more: the last slab of an odd number of K steps is copied whole)
+  a.hhi = (uint16_t*)take(n * F * 2 + 64);
+  a.hlo = pair || f <= FORM_T128_PAIR ? (uint16_t*)take(n * F * 2 + 64) : nullptr;
   a.xhi = pair ? (uint16_t*)take((size_t)a.T * D * 2) : nullptr;
   a.xlo = pair ? (uint16_t*)take((size_t)a.T * D * 2) : nullptr;
   a.y = (float*)take(n * D * 4);
+  a.arrived = (uint32_t*)take(kTileCUs * 4);
+  a.part = (float*)take((size_t)kTileCUs * T128::BM * T128::BN * 4);
   return off;
 }
 
@@ -857,23 +1002,18 @@ static void launch_few(const ExpertsArgs& a, hipStream_t s) {
 
 // XP: x is a pair; HP: silu(gate) * up is.
 template <class S, bool BF, bool XP, bool HP>
-static void launch_shape(const ExpertsArgs& a, hipStream_t s) {
+static void launch_products(const ExpertsArgs& a, hipStream_t s) {
   const int n = a.T * a.k, tiles = n / S::BM + std::min(n, a.w.E);  // at most: whole tiles, and a ragged one per expert
   const int cg = (2 * a.w.F + S::BN - 1) / S::BN, cd = (a.w.D + S::BN - 1) / S::BN;
-  hvd_launch((experts_tiled<S, true, BF, XP, HP>), dim3(tiles * cg), dim3(64 * S::NW), 0, s, a, cg);
+  // (shared tiles: less than a round of workgroups more)
+  hvd_launch((experts_tiled<S, true, BF, XP, HP>), dim3(tiles * cg + (S::SPLIT ? kTileCUs : 0)), dim3(64 * S::NW), 0, s, a, cg);
   hvd_launch((experts_tiled<S, false, BF, HP, false>), dim3(tiles * cd), dim3(64 * S::NW), 0, s, a, cd);
 }
 template <bool BF, bool XP>
 static void launch_tiled(const ExpertsArgs& a, Form f, hipStream_t s) {
-  using T64 = TileShape<1, 4, 2, 2>;   // 64 x 256
-  using T128 = TileShape<2, 4, 2, 2>;  // 128 x 256
-  using T256 = TileShape<4, 2, 2, 4>;  // 256 x 256
-  switch (f) {
-    case FORM_T64_PAIR: return launch_shape<T64, BF, XP, true>(a, s);
-    case FORM_T128_PAIR: return launch_shape<T128, BF, XP, true>(a, s);
-    case FORM_T128: return launch_shape<T128, BF, XP, XP>(a, s);
-    default: return launch_shape<T256, BF, XP, XP>(a, s);
-  }
+  if (f == FORM_T64_PAIR) launch_products<T64, BF, XP, true>(a, s);
+  else if (XP || f == FORM_T128_PAIR) launch_products<T128, BF, XP, true>(a, s);
+  else launch_products<T128, BF, XP, XP>(a, s);
 }
 
 hipError_t launch_experts(const ExpertsArgs& a, hipStream_t s) {

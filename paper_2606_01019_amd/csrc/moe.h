@@ -97,6 +97,8 @@ struct ExpertsArgs {
   uint16_t *hhi, *hlo;  // silu(gate) * up, [places][F]
   uint16_t *xhi, *xlo;  // the activations' pair (ET_F32), [T][D]
   float* y;          // [T*k][D] expert outputs by place
+  uint32_t* arrived;  // parts of each shared tile that are done (cleared by every call)
+  float* part;        // shared tiles' partial sums
 };
 // Bytes of the workspace of a call, and its layout over `base`.
 size_t experts_carve(ExpertsArgs& a, void* base);
