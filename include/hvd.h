@@ -351,7 +351,8 @@ int hvd_measure_mfma_peak(void* stream, double* tflops);
  * row stride given in elements.  Calls enqueue on `stream` (hipStream_t,
  * NULL = default stream) and return without waiting; they allocate nothing
  * and may be captured into a graph.  They hold no state between calls, so
- * any number may run at once on buffers of their own.  rows = 0 does nothing.
+ * any number may run at once on buffers of their own.  rows = 0 does nothing;
+ * hvd_route and hvd_block_norm take at most 8388608 rows.
  * Bad arguments are HVD_ERR_ARG, and nothing is enqueued. */
 typedef enum { HVD_F16 = 0, HVD_BF16 = 1, HVD_F32 = 2 } hvd_dtype;
 typedef enum { HVD_SCORE_SOFTMAX = 0, HVD_SCORE_SIGMOID = 1 } hvd_score;
@@ -383,8 +384,7 @@ hvd_status hvd_route(const hvd_route_config* cfg, int32_t rows, const void* logi
 
 /* Experts of one layer: n_experts SwiGLU MLPs d_model -> ffn_dim -> d_model.
  * 1 <= n_experts <= 512, d_model % 64 == 0, ffn_dim % 32 == 0, both at most
- * 131072; dtype HVD_F16
- * or HVD_BF16. */
+ * 131072; dtype HVD_F16 or HVD_BF16. */
 typedef struct {
   int32_t n_experts;
   int32_t d_model;

@@ -890,9 +890,9 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void experts_down_few(ExpertsArg
 // The activations' fp16 pair, 8 elements per thread.
 __global__ __launch_bounds__(256) void experts_split(ExpertsArgs a) {
   const int D = a.w.D, per = D / 8;
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= a.T * per) return;
-  const int t = i / per, c = (i - t * per) * 8;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (int64_t)a.T * per) return;
+  const int t = (int)(i / per), c = (int)(i - (int64_t)t * per) * 8;
   const float4* p = (const float4*)((const float*)a.x + t * a.x_stride + c);
   const float4 u = p[0], q = p[1];
   const float v[8] = {u.x, u.y, u.z, u.w, q.x, q.y, q.z, q.w};
@@ -1025,7 +1025,7 @@ hipError_t launch_experts(const ExpertsArgs& a, hipStream_t s) {
     return hipGetLastError();
   }
   hvd_launch(experts_sort, dim3(a.w.E), dim3(256), 0, s, a);
-  if (pair) hvd_launch(experts_split, dim3((a.T * (a.w.D / 8) + 255) / 256), dim3(256), 0, s, a);
+  if (pair) hvd_launch(experts_split, dim3((unsigned)(((int64_t)a.T * (a.w.D / 8) + 255) / 256)), dim3(256), 0, s, a);
   pair ? launch_tiled<false, true>(a, f, s) : bf ? launch_tiled<true, false>(a, f, s) : launch_tiled<false, false>(a, f, s);
   hvd_launch(experts_combine, dim3(a.T, (a.w.D / 4 + 255) / 256), dim3(256), 0, s, a);
   return hipGetLastError();

@@ -20,6 +20,7 @@ constexpr int kMaxExperts = 512;
 constexpr int kMaxTopK = 16;
 constexpr int kMaxGroups = 64;
 constexpr int kMaxNormDim = 16384;
+constexpr int kMaxOpRows = 1 << 23;         // rows of one routing or norm call
 constexpr int kFewRows = 32;               // most rows of the experts' few-row form
 constexpr int kMaxExpertRows = 1 << 18;  // rows of one call of the experts
 

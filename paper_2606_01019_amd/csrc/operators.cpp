@@ -80,7 +80,7 @@ hvd_status check_forward(hvd_experts e, int rows, int top_k, int x_dtype) {
 extern "C" hvd_status hvd_route(const hvd_route_config* cfg, int32_t rows, const void* logits, int32_t logits_dtype,
                                 int64_t logits_stride, const float* bias, int32_t* ids, float* weights, void* stream) {
   if (hvd_status st = check_route_config(cfg); st != HVD_OK) return st;
-  if (rows < 0) return set_err(HVD_ERR_ARG, "rows must be >= 0");
+  if (rows < 0 || rows > kMaxOpRows) return set_err(HVD_ERR_ARG, "rows must be in [0, 8388608]");
   if (!float_type(logits_dtype)) return set_err(HVD_ERR_ARG, "unknown logits dtype");
   if (rows == 0) return HVD_OK;
   if (!logits || !ids || !weights) return set_err(HVD_ERR_ARG, "null logits, ids or weights");
@@ -175,7 +175,7 @@ extern "C" hvd_status hvd_experts_forward(hvd_experts e, int32_t rows, int32_t t
 
 extern "C" hvd_status hvd_block_norm(const hvd_block_norm_args* g, int32_t rows, int32_t dim, void* stream) {
   if (!g) return set_err(HVD_ERR_ARG, "null arguments");
-  if (rows < 0) return set_err(HVD_ERR_ARG, "rows must be >= 0");
+  if (rows < 0 || rows > kMaxOpRows) return set_err(HVD_ERR_ARG, "rows must be in [0, 8388608]");
   if (dim < 1 || dim > kMaxNormDim) return set_err(HVD_ERR_ARG, "dim must be in [1, 16384]");
   if (rows == 0) return HVD_OK;
   if (!g->x || (!g->x_out && !g->h)) return set_err(HVD_ERR_ARG, "null x, or neither x_out nor h");

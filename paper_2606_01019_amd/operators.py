@@ -3,7 +3,8 @@ the products of the chosen experts, and the norms around a block.
 
 Each call enqueues hand-written HIP kernels on torch's current stream of its
 tensors' device and returns without waiting; results are new tensors unless
-``out``-style arguments are given.  Calls may be captured into a graph.
+``out``-style arguments are given.  Calls may be captured into a graph.  There
+is no backward pass: arguments that require a gradient are refused.
 """
 
 import ctypes
@@ -58,6 +59,8 @@ def _matrix(t, what, device=None, rows=None, cols=None):
     """Checks a [rows, cols] tensor with unit column stride; returns its row stride."""
     if t.dim() != 2 or not t.is_cuda or (device is not None and t.device != device):
         _refuse(f"{what} must be a matrix on the GPU, on one device with the other arguments")
+    if t.requires_grad and torch.is_grad_enabled():
+        _refuse(f"{what} requires a gradient: these operators have no backward pass (use torch.no_grad())")
     n, m = t.shape
     if (rows is not None and n != rows) or (cols is not None and m != cols):
         _refuse(f"{what} has shape {tuple(t.shape)}, not ({rows}, {cols})")

@@ -425,6 +425,33 @@ def test_experts_strides(hvd, dtype, T):
     check_experts(hvd, W, odd, ids, w, layer=layer)
 
 
+def test_experts_past_32_bits(hvd):
+    """Expert outputs of more than 4 GiB; rows further apart than 2^31 elements."""
+    g = gen(2)
+    W = make(g, 8, 4096, 32, torch.bfloat16)
+    T = 17000
+    x = rnd(g, T, 4096, dtype=torch.bfloat16)
+    ids = torch.randint(0, 8, (T, 16), generator=g, device="cuda", dtype=torch.int32)
+    check_experts(hvd, W, x, ids, rnd(g, T, 16))
+    del x
+    far = torch.empty(8 * (1 << 29) + 4096, dtype=torch.bfloat16, device="cuda")
+    x = torch.as_strided(far, (9, 4096), (1 << 29, 1))
+    x.copy_(rnd(g, 9, 4096))
+    ids, w = choose(g, 9, 8, 2)
+    got, layer = check_experts(hvd, W, x, ids, w)
+    y, h = hvd.block_norm(x, got, gain=torch.ones(4096, device="cuda"))
+    y2, h2 = hvd.block_norm(x.contiguous(), got, gain=torch.ones(4096, device="cuda"))
+    assert torch.equal(y, y2) and torch.equal(h, h2)
+    a, b = hvd.route(x[:, :64], 8), hvd.route(x[:, :64].contiguous(), 8)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_experts_many_small_rows(hvd):
+    g = gen(6)
+    W = make(g, 24, 64, 32, torch.float16)
+    check_experts(hvd, W, rnd(g, 60001, 64, dtype=torch.float16), *choose(g, 60001, 24, 3, 2.0))
+
+
 def test_experts_are_the_same_bits_again(hvd):
     g = gen(1)
     for dtype in DT:
@@ -435,6 +462,30 @@ def test_experts_are_the_same_bits_again(hvd):
             a = layer.forward(x, ids, w)
             for _ in range(3):
                 assert torch.equal(layer.forward(x, ids, w), a)
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("T,E,k,F", [(40, 6, 2, 512), (300, 40, 3, 512), (900, 30, 2, 96)])
+def test_experts_shared_tiles_replayed(hvd, dtype, T, E, k, F):
+    """Tiles whose K range several workgroups share: right, and the same bits
+    from a graph replayed between eager calls."""
+    g = gen(T + 3)
+    W = make(g, E, 2048, F, dtype)
+    xs = [rnd(g, T, 2048, dtype=dtype) for _ in range(2)]
+    ids, w = choose(g, T, E, k, 0.5)
+    want, layer = check_experts(hvd, W, xs[0], ids, w)
+    other = layer.forward(xs[1], ids, w)
+    buf = xs[0].clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        res = layer.forward(buf, ids, w)
+    for i in range(5):
+        buf.copy_(xs[i % 2])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(res, (want, other)[i % 2])
+        assert torch.equal(layer.forward(xs[1 - i % 2], ids, w), (other, want)[i % 2])
 
 
 def test_experts_refusals(hvd):
@@ -451,11 +502,15 @@ def test_experts_refusals(hvd):
                 lambda: layer.forward(x, torch.zeros(3, 17, dtype=torch.int32, device="cuda"), torch.zeros(3, 17, device="cuda")),
                 lambda: layer.forward(x.cpu(), ids, w), lambda: hvd.Experts(W[0], W[1][:2], W[2]),
                 lambda: hvd.Experts(W[0].half(), W[1], W[2]), lambda: hvd.Experts(*(t.float() for t in W)),
+                lambda: layer.forward(x.clone().requires_grad_(), ids, w), lambda: hvd.route(rnd(g, 3, 8).requires_grad_(), 2),
+                lambda: hvd.block_norm(rnd(g, 3, 8), rnd(g, 3, 8).requires_grad_()),
                 lambda: hvd.route(rnd(g, 3, 8), 9), lambda: hvd.route(rnd(g, 3, 8), 2, bias=rnd(g, 7)),
                 lambda: hvd.block_norm(rnd(g, 3, 8), rnd(g, 3, 7)), lambda: hvd.block_norm(rnd(g, 3, 8).t()),
                 lambda: hvd.block_norm(rnd(g, 3, 8), rnd(g, 3, 8), gate=rnd(g, 2, 8))):
         with pytest.raises(hvd.HvdError):
             bad()
+    with torch.no_grad():
+        assert torch.equal(layer.forward(x.clone().requires_grad_(), ids, w), layer.forward(x, ids, w))
     assert layer.forward(x[:0], ids[:0], w[:0]).shape == (0, 128)
     assert hvd.route(rnd(g, 3, 8)[:0], 2)[0].shape == (0, 2)
     layer.close()

@@ -34,7 +34,7 @@ def test_route_config(lib, kw):
 
 
 @pytest.mark.parametrize("rows,logits,dtype,stride,bias,ids,w", [
-    (-1, A, 2, 64, None, A, A), (1, None, 2, 64, None, A, A), (1, A, 3, 64, None, A, A), (1, A, -1, 64, None, A, A),
+    (-1, A, 2, 64, None, A, A), ((1 << 23) + 1, A, 2, 64, None, A, A), (1, None, 2, 64, None, A, A), (1, A, 3, 64, None, A, A), (1, A, -1, 64, None, A, A),
     (2, A, 2, 63, None, A, A), (1, A + 2, 2, 64, None, A, A), (1, A + 1, 0, 64, None, A, A), (1, A, 2, 64, A + 1, A, A),
     (1, A, 2, 64, None, None, A), (1, A, 2, 64, None, A, None), (1, A, 2, 64, None, A + 2, A)])
 def test_route_arguments(lib, rows, logits, dtype, stride, bias, ids, w):
@@ -91,7 +91,7 @@ def test_block_norm_arguments(lib, kw):
     assert lib.hvd_block_norm(ctypes.byref(norm_args(**kw)), 2, 64, None) == HVD_ERR_ARG
 
 
-@pytest.mark.parametrize("rows,dim", [(-1, 64), (1, 0), (1, 16385)])
+@pytest.mark.parametrize("rows,dim", [(-1, 64), (1, 0), (1, 16385), ((1 << 23) + 1, 64)])
 def test_block_norm_sizes(lib, rows, dim):
     assert lib.hvd_block_norm(ctypes.byref(norm_args()), rows, dim, None) == HVD_ERR_ARG
 
