@@ -8,6 +8,7 @@ is no backward pass: arguments that require a gradient are refused.
 """
 
 import ctypes
+import struct
 
 from .hvd import HVD_ERR_ARG, SCORES, HvdError, RouteConfig, _check, load_library
 
@@ -25,6 +26,11 @@ class BlockNormArgs(ctypes.Structure):
                 ("h_stride", ctypes.c_int64), ("x_dtype", ctypes.c_int32), ("y_dtype", ctypes.c_int32),
                 ("gate_dtype", ctypes.c_int32), ("h_dtype", ctypes.c_int32), ("scale", ctypes.c_float),
                 ("eps", ctypes.c_float)]
+
+
+# the same structure as bytes: a microsecond faster to fill than its fields
+_pack_norm = struct.Struct("@PqPqPqqPPPqPqiiiiff").pack
+assert len(_pack_norm(*[0] * 19)) == ctypes.sizeof(BlockNormArgs)
 
 
 def _refuse(msg):
@@ -220,7 +226,8 @@ def block_norm(x, y=None, *, gain=None, post_gain=None, gate=None, scale=1.0, ep
     xs, xc = _matrix(x, "x"), _dtype(x.dtype, "x")
     rows, dim = x.shape
     dev = x.device
-    yp, ys, yc, gp, gr, gs, gc = None, 0, 0, None, 0, 0, 0
+    yp = ys = yc = gp = gr = gs = gc = op = os_ = hp = gainp = hc = 0
+    h = None
     if y is not None:
         yp, ys, yc = y.data_ptr(), _matrix(y, "y", dev, rows, dim), _dtype(y.dtype, "y")
         if x_out is None:
@@ -232,8 +239,6 @@ def block_norm(x, y=None, *, gain=None, post_gain=None, gate=None, scale=1.0, ep
         op = x_out.data_ptr()
     elif gate is not None or post_gain is not None or x_out is not None:
         _refuse("gate, post_gain and x_out belong to a y")
-    else:
-        op, os_ = None, 0
     if gate is not None:
         if gate.device != dev:
             _refuse("gate must be on the arguments' device")
@@ -247,12 +252,11 @@ def block_norm(x, y=None, *, gain=None, post_gain=None, gate=None, scale=1.0, ep
         elif gs not in (0, 1):
             _refuse("gate must have unit column stride")
         gp, gc = g.data_ptr(), _dtype(gate.dtype, "gate")
-    h, hp, gainp, hc = None, None, None, 0
     if gain is not None:
         gainp = _vector(gain, "gain", dim, dev)
         h = torch.empty((rows, dim), dtype=h_dtype or x.dtype, device=dev)
         hp, hc = h.data_ptr(), _dtype(h.dtype, "h")
-    a = BlockNormArgs(x.data_ptr(), xs, yp, ys, gp, gr, gs, _vector(post_gain, "post_gain", dim, dev) if post_gain is not None else None,
-                      gainp, op, os_, hp, dim, xc, yc, gc, hc, scale, eps)
-    _call(dev, lib.hvd_block_norm, ctypes.byref(a), rows, dim)
+    pp = _vector(post_gain, "post_gain", dim, dev) if post_gain is not None else 0
+    _call(dev, lib.hvd_block_norm, _pack_norm(x.data_ptr(), xs, yp, ys, gp, gr, gs, pp, gainp, op, os_, hp, dim, xc, yc,
+                                              gc, hc, scale, eps), rows, dim)
     return (x if y is None else x_out), h
