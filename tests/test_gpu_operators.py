@@ -203,6 +203,17 @@ def test_norm_widths(hvd, dim):
     check_norm(hvd, x, y)
 
 
+@pytest.mark.parametrize("dim", [2, 9, 519, 575, 576, 577, 1088, 1089, 2303, 2304, 2305, 4100, 4352, 4353, 6400, 6401, 8448, 8449,
+                                 16383])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_norm_leftover_columns(hvd, dim, dtype):
+    """Widths around the steps' ends, where columns go one to a lane."""
+    g = gen(dim + 1)
+    x, y = rnd(g, 6, dim, dtype=dtype, std=2.0), rnd(g, 6, dim, dtype=dtype)
+    check_norm(hvd, x, y, gain=rnd(g, dim), post=rnd(g, dim), gate=rnd(g, 6, dim, dtype=dtype), scale=0.5)
+    check_norm(hvd, x, y, gain=rnd(g, dim), h_dtype=torch.float16)
+
+
 @pytest.mark.parametrize("xt", TYPES)
 @pytest.mark.parametrize("yt", TYPES)
 @pytest.mark.parametrize("ht", TYPES)
