@@ -471,7 +471,8 @@ typedef struct {
  *   attn_norm [D], wq, wk, wv, wo, mlp_norm [D] as before, router [E, D],
  *   router_bias [E] (the bias of hvd_route; may be NULL), gate [E, F, D],
  *   up [E, F, D], down [E, D, F], post_norm [D] (NULL without post_norm);
- * count = 3 + 9 * first_layer + 12 * (n_layers - first_layer).  Handles from
+ * count = 3 + 9 * first_layer + 12 * (n_layers - first_layer).  cfg->ffn_dim is
+ * the dense layers' and has to be valid even without one.  Handles from
  * here work with every call of this header; HVD_OPT_FLOW has no effect on
  * them. */
 size_t hvd_model_bytes_moe(const hvd_config* cfg, const hvd_moe_config* moe);
