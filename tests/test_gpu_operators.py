@@ -402,6 +402,19 @@ def test_experts_same_id_twice(hvd, dtype, T):
     check_experts(hvd, W, rnd(g, T, 128, dtype=dtype), ids, w)
 
 
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("E,row", [(2, [1, 0, -1, 1, 5, 0, 1, 1, 0, 0, -7, 1, 0, 1, 2, 0]), (9, [-1, 8, 9, 0, -1, 4]), (1, [0] * 16),
+                                   (300, [299, -1, 255, 0, 256, 64, 63, 300])])
+def test_experts_one_row_with_empty_and_repeated_slots(hvd, dtype, E, row):
+    g = gen(E)
+    W = make(g, E, 128, 64, dtype)
+    x, ids = rnd(g, 1, 128, dtype=dtype), torch.tensor([row], dtype=torch.int32, device="cuda")
+    ok = (ids >= 0) & (ids < E)
+    w = rnd(g, 1, len(row)).abs()
+    got, layer = check_experts(hvd, W, x, ids, torch.where(ok, w, torch.zeros_like(w)))
+    assert torch.equal(layer.forward(x, ids, torch.where(ok, w, torch.full_like(w, math.nan))), got)
+
+
 @pytest.mark.parametrize("T", [3, 30, 300])
 def test_experts_infinite_weights_stay_in_their_rows(hvd, T):
     """An expert with infinities in its matrices spoils only the rows that chose it."""
