@@ -61,12 +61,17 @@ def _dtype(t, what):
     return c
 
 
+def _no_grad(t, what):
+    if t.requires_grad and torch.is_grad_enabled():
+        _refuse(f"{what} requires a gradient: these operators have no backward pass (use torch.no_grad())")
+
+
 def _matrix(t, what, device=None, rows=None, cols=None):
     """Checks a [rows, cols] tensor with unit column stride; returns its row stride."""
     if t.dim() != 2 or not t.is_cuda or (device is not None and t.device != device):
         _refuse(f"{what} must be a matrix on the GPU, on one device with the other arguments")
-    if t.requires_grad and torch.is_grad_enabled():
-        _refuse(f"{what} requires a gradient: these operators have no backward pass (use torch.no_grad())")
+    if t.requires_grad:
+        _no_grad(t, what)
     n, m = t.shape
     if (rows is not None and n != rows) or (cols is not None and m != cols):
         _refuse(f"{what} has shape {tuple(t.shape)}, not ({rows}, {cols})")
@@ -79,12 +84,16 @@ def _matrix(t, what, device=None, rows=None, cols=None):
 def _vector(t, what, n, device):
     if t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != n or t.device != device or not t.is_contiguous():
         _refuse(f"{what} must be a contiguous float32 vector of {n} on the arguments' device")
+    if t.requires_grad:
+        _no_grad(t, what)
     return t.data_ptr()
 
 
 def _exact(t, what, shape, dtype, device):
     if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
         _refuse(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on the arguments' device")
+    if t.requires_grad:
+        _no_grad(t, what)
     return t.data_ptr()
 
 
@@ -242,6 +251,7 @@ def block_norm(x, y=None, *, gain=None, post_gain=None, gate=None, scale=1.0, ep
     if gate is not None:
         if gate.device != dev:
             _refuse("gate must be on the arguments' device")
+        _no_grad(gate, "gate")
         try:
             g = gate.expand(rows, dim)
         except RuntimeError:

@@ -544,6 +544,29 @@ def test_experts_refusals(hvd):
 
 # ------------------------------------------------------------------- together
 
+def test_gradients_are_refused_for_every_argument(hvd):
+    """No backward pass: a gradient that would get lost is an error, whichever
+    argument asks for it; without autograd the same calls run."""
+    g = gen(3)
+    x, y, gate, gain = rnd(g, 3, 128), rnd(g, 3, 128), rnd(g, 3, 128), rnd(g, 128)
+    W = make(g, 4, 128, 64, torch.float16)
+    layer = hvd.Experts(*W)
+    ids, w = choose(g, 3, 4, 2)
+    logits, bias = rnd(g, 3, 8), rnd(g, 8)
+    p = lambda t: t.clone().requires_grad_()
+    calls = [lambda: hvd.block_norm(p(x), gain=gain), lambda: hvd.block_norm(x, p(y), gain=gain),
+             lambda: hvd.block_norm(x, gain=p(gain)), lambda: hvd.block_norm(x, y, post_gain=p(gain)),
+             lambda: hvd.block_norm(x, y, gate=p(gate)), lambda: hvd.block_norm(x, y, gate=p(gate[:1, :1])),
+             lambda: hvd.route(p(logits), 2), lambda: hvd.route(logits, 2, bias=p(bias)),
+             lambda: layer.forward(p(x), ids, w), lambda: layer.forward(x, ids, p(w))]
+    calls += [lambda i=i: hvd.Experts(*(p(t) if i == j else t for j, t in enumerate(W))) for i in range(3)]
+    for i, call in enumerate(calls):
+        with pytest.raises(hvd.HvdError, match="gradient"):
+            call()
+        with torch.no_grad():
+            call()
+
+
 def block(hvd, layer, x, gain, k):
     """The MLP block of an expert layer on a 32-bit residual stream."""
     _, h = hvd.block_norm(x, None, gain=gain)
