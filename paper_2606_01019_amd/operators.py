@@ -8,6 +8,8 @@ is no backward pass: arguments that require a gradient are refused.
 """
 
 import ctypes
+import math
+import operator
 import struct
 
 from .hvd import HVD_ERR_ARG, SCORES, HvdError, RouteConfig, _check, load_library
@@ -66,6 +68,28 @@ def _no_grad(t, what):
         _refuse(f"{what} requires a gradient: these operators have no backward pass (use torch.no_grad())")
 
 
+def _number(v, what):
+    """v as the float that a config or an argument block holds.  A tensor's value
+    is taken now; one that requires a gradient is refused like any other."""
+    if type(v) is not float:
+        if isinstance(v, torch.Tensor):
+            _no_grad(v, what)
+        try:
+            v = float(v)
+        except (TypeError, ValueError, RuntimeError, OverflowError):
+            _refuse(f"{what} must be a number")
+    if abs(v) > 3.4028234663852886e38 and not math.isinf(v):
+        _refuse(f"{what} must be in the range of a float")
+    return v
+
+
+def _integer(v, what):
+    try:
+        return operator.index(v)
+    except TypeError:
+        _refuse(f"{what} must be an integer")
+
+
 def _matrix(t, what, device=None, rows=None, cols=None):
     """Checks a [rows, cols] tensor with unit column stride; returns its row stride."""
     if t.dim() != 2 or not t.is_cuda or (device is not None and t.device != device):
@@ -119,6 +143,16 @@ def route(logits, top_k, *, score="softmax", bias=None, n_groups=1, top_groups=1
     code = _dtype(logits.dtype, "logits")
     rows, E = logits.shape
     dev = logits.device
+    # the key holds plain numbers: equal keys are equal configs, whatever becomes
+    # of the objects they came from
+    if type(top_k) is not int:
+        top_k = _integer(top_k, "top_k")
+    if type(n_groups) is not int:
+        n_groups = _integer(n_groups, "n_groups")
+    if type(top_groups) is not int:
+        top_groups = _integer(top_groups, "top_groups")
+    scale = _number(scale, "scale")
+    renorm = bool(renorm)
     key = (E, top_k, score, n_groups, top_groups, renorm, scale)
     cfg = _configs.get(key)
     if cfg is None:
@@ -127,7 +161,7 @@ def route(logits, top_k, *, score="softmax", bias=None, n_groups=1, top_groups=1
         if len(_configs) >= 256:
             _configs.clear()
         # (an address that stays: the library reads the config during the call only)
-        cfg = _configs[key] = ctypes.pointer(RouteConfig(E, top_k, SCORES[score], n_groups, top_groups, bool(renorm), scale))
+        cfg = _configs[key] = ctypes.pointer(RouteConfig(E, top_k, SCORES[score], n_groups, top_groups, renorm, scale))
     if not 1 <= top_k <= 16:
         _refuse("top_k must be in [1, 16]")
     bp = _vector(bias, "bias", E, dev) if bias is not None else None
@@ -235,6 +269,7 @@ def block_norm(x, y=None, *, gain=None, post_gain=None, gate=None, scale=1.0, ep
     xs, xc = _matrix(x, "x"), _dtype(x.dtype, "x")
     rows, dim = x.shape
     dev = x.device
+    scale, eps = _number(scale, "scale"), _number(eps, "eps")
     yp = ys = yc = gp = gr = gs = gc = op = os_ = hp = gainp = hc = 0
     h = None
     if y is not None:

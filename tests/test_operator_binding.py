@@ -1,0 +1,98 @@
+"""The torch binding of the expert-layer operators, on the CPU: what it hands to
+the library, which is stubbed here, and what it refuses."""
+
+import ctypes
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2606_01019_amd as hvd
+from paper_2606_01019_amd import operators as ops
+from paper_2606_01019_amd.hvd import RouteConfig
+
+
+class OnGpu(torch.Tensor):
+    """A host tensor that passes for one on the GPU."""
+    is_cuda = True
+
+
+def gpu(*shape, dtype=torch.float32):
+    return torch.ones(*shape, dtype=dtype).as_subclass(OnGpu)
+
+
+class Library:
+    """Records the calls; every one succeeds."""
+
+    def __init__(self):
+        self.routed, self.normed, self.calls = [], [], 0
+
+    def hvd_route(self, cfg, rows, *args):
+        c = ctypes.cast(cfg, ctypes.POINTER(RouteConfig)).contents
+        self.routed.append({f: getattr(c, f) for f, _ in RouteConfig._fields_})
+        return 0
+
+    def hvd_block_norm(self, args, rows, dim, stream):
+        a = ops.BlockNormArgs.from_buffer_copy(args)
+        self.normed.append((a.scale, a.eps))
+        return 0
+
+
+@pytest.fixture
+def lib(monkeypatch):
+    ops._library()
+    L = Library()
+    monkeypatch.setattr(ops, "_library", lambda: L)
+    monkeypatch.setattr(ops, "_call", lambda device, fn, *args: fn(*args, 0))
+    monkeypatch.setattr(ops, "_configs", {})
+    return L
+
+
+def test_a_changed_scale_is_the_scale(lib):
+    """A 0-dimensional tensor or array counts by its value at the call."""
+    for s in (torch.tensor(2.0), np.array(2.0)):
+        hvd.route(gpu(3, 8), 2, scale=s)
+        s += 1.0
+        hvd.route(gpu(3, 8), 2, scale=s)
+        assert [c["scale"] for c in lib.routed[-2:]] == [2.0, 3.0]
+        hvd.block_norm(gpu(3, 8), gpu(3, 8), scale=s, eps=s)
+        assert lib.normed[-1] == (3.0, 3.0)
+
+
+def test_equal_options_of_other_types(lib):
+    """Whatever holds a number, the library gets that number."""
+    want = dict(n_experts=8, top_k=2, score=0, n_groups=4, top_groups=2, renorm=1, scale=1.0)
+    for k, g, t, renorm, scale in ((2, 4, 2, True, 1.0), (np.int64(2), np.int32(4), torch.tensor(2), 1, 1),
+                                   (2, 4, 2, 7, np.float32(1)), (2, 4, 2, "yes", True)):
+        hvd.route(gpu(3, 8), k, n_groups=g, top_groups=t, renorm=renorm, scale=scale)
+        assert lib.routed[-1] == want
+    hvd.route(gpu(3, 8), 2, n_groups=4, top_groups=2, renorm=0)
+    assert lib.routed[-1]["renorm"] == 0
+    assert len(ops._configs) == 2
+
+
+@pytest.mark.parametrize("kw", [dict(top_k=2.0), dict(top_k=None), dict(n_groups=1.0), dict(top_groups="1"),
+                                dict(scale="a"), dict(scale=None), dict(scale=torch.ones(2)), dict(scale=1e39)])
+def test_options_that_are_no_numbers(lib, kw):
+    hvd.route(gpu(3, 8), 2)  # (a config that would compare equal is known)
+    args = dict(top_k=2, **kw) if "top_k" not in kw else kw
+    with pytest.raises(hvd.HvdError):
+        hvd.route(gpu(3, 8), args.pop("top_k"), **args)
+    if "scale" in kw:
+        for name in ("scale", "eps"):
+            with pytest.raises(hvd.HvdError):
+                hvd.block_norm(gpu(3, 8), gpu(3, 8), **{name: kw["scale"]})
+    assert len(lib.routed) == 1 and not lib.normed
+
+
+def test_numbers_that_require_a_gradient(lib):
+    p = torch.nn.Parameter(torch.tensor(2.0))
+    calls = (lambda: hvd.route(gpu(3, 8), 2, scale=p), lambda: hvd.block_norm(gpu(3, 8), gpu(3, 8), scale=p),
+             lambda: hvd.block_norm(gpu(3, 8), gpu(3, 8), eps=p))
+    for call in calls:
+        with pytest.raises(hvd.HvdError, match="gradient"):
+            call()
+        with torch.no_grad():
+            call()
+    assert lib.routed[-1]["scale"] == 2.0 and lib.normed == [(2.0, pytest.approx(1e-5)), (1.0, 2.0)]
