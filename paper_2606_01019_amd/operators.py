@@ -4,7 +4,8 @@ the products of the chosen experts, and the norms around a block.
 Each call enqueues hand-written HIP kernels on torch's current stream of its
 tensors' device and returns without waiting; results are new tensors unless
 ``out``-style arguments are given.  Calls may be captured into a graph.  There
-is no backward pass: arguments that require a gradient are refused.
+is no derivative: arguments that require a gradient or have a tangent are
+refused.
 """
 
 import ctypes
@@ -42,15 +43,16 @@ def _refuse(msg):
 # The calls below are a few microseconds of host time each, of which a decode
 # step makes dozens: torch is looked up once, configs are built once, and the
 # current device and raw stream are asked for without making objects.
-torch = None
+torch = _forward_ad = None
 _codes, _configs = {}, {}
 
 
 def _library():
-    global torch
+    global torch, _forward_ad
     lib = load_library()
     if torch is None:
         import torch as t
+        import torch.autograd.forward_ad as _forward_ad
         _codes.update({t.float16: 0, t.bfloat16: 1, t.float32: 2})
         torch = t
     return lib
@@ -66,6 +68,8 @@ def _dtype(t, what):
 def _no_grad(t, what):
     if t.requires_grad and torch.is_grad_enabled():
         _refuse(f"{what} requires a gradient: these operators have no backward pass (use torch.no_grad())")
+    if _forward_ad._current_level >= 0 and _forward_ad.unpack_dual(t).tangent is not None:
+        _refuse(f"{what} has a tangent: these operators have no forward-mode derivative")
 
 
 def _number(v, what):
@@ -94,7 +98,7 @@ def _matrix(t, what, device=None, rows=None, cols=None):
     """Checks a [rows, cols] tensor with unit column stride; returns its row stride."""
     if t.dim() != 2 or not t.is_cuda or (device is not None and t.device != device):
         _refuse(f"{what} must be a matrix on the GPU, on one device with the other arguments")
-    if t.requires_grad:
+    if t.requires_grad or _forward_ad._current_level >= 0:
         _no_grad(t, what)
     n, m = t.shape
     if (rows is not None and n != rows) or (cols is not None and m != cols):
@@ -108,7 +112,7 @@ def _matrix(t, what, device=None, rows=None, cols=None):
 def _vector(t, what, n, device):
     if t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != n or t.device != device or not t.is_contiguous():
         _refuse(f"{what} must be a contiguous float32 vector of {n} on the arguments' device")
-    if t.requires_grad:
+    if t.requires_grad or _forward_ad._current_level >= 0:
         _no_grad(t, what)
     return t.data_ptr()
 
@@ -116,7 +120,7 @@ def _vector(t, what, n, device):
 def _exact(t, what, shape, dtype, device):
     if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
         _refuse(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on the arguments' device")
-    if t.requires_grad:
+    if t.requires_grad or _forward_ad._current_level >= 0:
         _no_grad(t, what)
     return t.data_ptr()
 

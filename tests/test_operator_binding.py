@@ -96,3 +96,30 @@ def test_numbers_that_require_a_gradient(lib):
         with torch.no_grad():
             call()
     assert lib.routed[-1]["scale"] == 2.0 and lib.normed == [(2.0, pytest.approx(1e-5)), (1.0, 2.0)]
+
+
+def test_tangents_are_refused_for_every_argument(lib):
+    """No forward-mode derivative: a tangent that would get lost is an error,
+    whichever argument has it."""
+    import torch.autograd.forward_ad as fwd
+    x, y, gain, gate = gpu(3, 8), gpu(3, 8), gpu(8), gpu(3, 8)
+    plain = [lambda: hvd.route(x, 2), lambda: hvd.block_norm(x, y, gain=gain, post_gain=gain, gate=gate)]
+    with fwd.dual_level():
+        p = lambda t: fwd.make_dual(t, torch.ones_like(t))
+        calls = [lambda: hvd.block_norm(p(x), gain=gain), lambda: hvd.block_norm(x, p(y), gain=gain),
+                 lambda: hvd.block_norm(x, gain=p(gain)), lambda: hvd.block_norm(x, y, post_gain=p(gain)),
+                 lambda: hvd.block_norm(x, y, gate=p(gate)), lambda: hvd.block_norm(x, y, gate=p(gate[:1, :1])),
+                 lambda: hvd.block_norm(x, y, scale=p(torch.tensor(1.0))), lambda: hvd.route(x, 2, scale=p(torch.tensor(1.0))),
+                 lambda: hvd.route(p(x), 2), lambda: hvd.route(x, 2, bias=p(gain))]
+        for call in calls:
+            with pytest.raises(hvd.HvdError, match="tangent"):
+                call()
+            with torch.no_grad(), pytest.raises(hvd.HvdError, match="tangent"):  # (which stops gradients, not tangents)
+                call()
+            with fwd._set_fwd_grad_enabled(False):
+                call()
+        for t in (torch.ones(3, 64), torch.ones(3, 2)):
+            with pytest.raises(hvd.HvdError, match="tangent"):
+                ops._exact(p(t), "weights", t.shape, torch.float32, t.device)
+        for call in plain:  # tensors without one run inside a level too
+            call()
