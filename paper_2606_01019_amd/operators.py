@@ -178,7 +178,9 @@ def route(logits, top_k, *, score="softmax", bias=None, n_groups=1, top_groups=1
 class Experts:
     """The experts of one layer (hvd_experts_*): gate and up
     [n_experts, ffn_dim, d_model], down [n_experts, d_model, ffn_dim], float16
-    or bfloat16, packed once."""
+    or bfloat16, packed once.  Weights that require a gradient are packed under
+    torch.no_grad() only, and such a layer runs under it only; detached ones are
+    plain data."""
 
     def __init__(self, gate, up, down):
         self.handle = None
@@ -202,6 +204,7 @@ class Experts:
         self.handle = h
         self.home = torch.cuda.current_stream(self.device)
         self.home.synchronize()  # packed: later calls may run on any stream
+        self.grads = gate.requires_grad or up.requires_grad or down.requires_grad
         self.sizes = {}
 
     def forward(self, x, ids, weights, out=None):
@@ -211,6 +214,9 @@ class Experts:
         [0, n_experts) adds nothing."""
         if self.handle is None:
             _refuse("the experts are closed")
+        if self.grads and torch.is_grad_enabled():
+            _refuse("the experts were packed from weights that require a gradient: these operators have no backward pass "
+                    "(use torch.no_grad(), or pack detached weights)")
         code = _dtype(x.dtype, "x")
         dev, D = self.device, self.d_model
         xs = _matrix(x, "x", dev, None, D)
