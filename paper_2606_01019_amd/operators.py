@@ -9,7 +9,6 @@ refused.
 """
 
 import ctypes
-import math
 import operator
 import struct
 
@@ -68,23 +67,24 @@ def _dtype(t, what):
 def _no_grad(t, what):
     if t.requires_grad and torch.is_grad_enabled():
         _refuse(f"{what} requires a gradient: these operators have no backward pass (use torch.no_grad())")
-    if _forward_ad._current_level >= 0 and _forward_ad.unpack_dual(t).tangent is not None:
-        _refuse(f"{what} has a tangent: these operators have no forward-mode derivative")
+
+
+def _no_tangents(*args):
+    """For calls inside a forward-mode level: a tangent would get lost."""
+    for t in args:
+        if isinstance(t, torch.Tensor) and _forward_ad.unpack_dual(t).tangent is not None:
+            _refuse("an argument has a tangent: these operators have no forward-mode derivative")
 
 
 def _number(v, what):
-    """v as the float that a config or an argument block holds.  A tensor's value
-    is taken now; one that requires a gradient is refused like any other."""
-    if type(v) is not float:
-        if isinstance(v, torch.Tensor):
-            _no_grad(v, what)
-        try:
-            v = float(v)
-        except (TypeError, ValueError, RuntimeError, OverflowError):
-            _refuse(f"{what} must be a number")
-    if abs(v) > 3.4028234663852886e38 and not math.isinf(v):
-        _refuse(f"{what} must be in the range of a float")
-    return v
+    """The float that an argument other than one stands for.  A tensor's value is
+    taken now; one that requires a gradient is refused like any other."""
+    if isinstance(v, torch.Tensor):
+        _no_grad(v, what)
+    try:
+        return float(v)
+    except (TypeError, ValueError, RuntimeError, OverflowError):
+        _refuse(f"{what} must be a number")
 
 
 def _integer(v, what):
@@ -98,7 +98,7 @@ def _matrix(t, what, device=None, rows=None, cols=None):
     """Checks a [rows, cols] tensor with unit column stride; returns its row stride."""
     if t.dim() != 2 or not t.is_cuda or (device is not None and t.device != device):
         _refuse(f"{what} must be a matrix on the GPU, on one device with the other arguments")
-    if t.requires_grad or _forward_ad._current_level >= 0:
+    if t.requires_grad:
         _no_grad(t, what)
     n, m = t.shape
     if (rows is not None and n != rows) or (cols is not None and m != cols):
@@ -112,7 +112,7 @@ def _matrix(t, what, device=None, rows=None, cols=None):
 def _vector(t, what, n, device):
     if t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != n or t.device != device or not t.is_contiguous():
         _refuse(f"{what} must be a contiguous float32 vector of {n} on the arguments' device")
-    if t.requires_grad or _forward_ad._current_level >= 0:
+    if t.requires_grad:
         _no_grad(t, what)
     return t.data_ptr()
 
@@ -120,7 +120,7 @@ def _vector(t, what, n, device):
 def _exact(t, what, shape, dtype, device):
     if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
         _refuse(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on the arguments' device")
-    if t.requires_grad or _forward_ad._current_level >= 0:
+    if t.requires_grad:
         _no_grad(t, what)
     return t.data_ptr()
 
@@ -143,6 +143,8 @@ def route(logits, top_k, *, score="softmax", bias=None, n_groups=1, top_groups=1
     Returns (ids int32 [rows, top_k], weights float32 [rows, top_k]): best
     first, id -1 and weight 0 where no unmasked expert is left."""
     lib = _library()
+    if _forward_ad._current_level >= 0:
+        _no_tangents(logits, bias, scale)
     stride = _matrix(logits, "logits")
     code = _dtype(logits.dtype, "logits")
     rows, E = logits.shape
@@ -155,13 +157,17 @@ def route(logits, top_k, *, score="softmax", bias=None, n_groups=1, top_groups=1
         n_groups = _integer(n_groups, "n_groups")
     if type(top_groups) is not int:
         top_groups = _integer(top_groups, "top_groups")
-    scale = _number(scale, "scale")
-    renorm = bool(renorm)
+    if type(scale) is not float:
+        scale = _number(scale, "scale")
+    if renorm is not True:
+        renorm = bool(renorm)
     key = (E, top_k, score, n_groups, top_groups, renorm, scale)
     cfg = _configs.get(key)
     if cfg is None:
         if score not in SCORES:
             _refuse(f"score must be one of {sorted(SCORES)}")
+        if not abs(scale) <= 3.4028234663852886e38:
+            _refuse("scale must be finite")
         if len(_configs) >= 256:
             _configs.clear()
         # (an address that stays: the library reads the config during the call only)
@@ -187,6 +193,8 @@ class Experts:
         self.lib = _library()
         if gate.dim() != 3 or not gate.is_cuda:
             _refuse("gate must be [n_experts, ffn_dim, d_model] on the GPU")
+        if _forward_ad._current_level >= 0:
+            _no_tangents(gate, up, down)
         E, F, D = gate.shape
         self.n_experts, self.ffn_dim, self.d_model = E, F, D
         self.dtype, self.device = gate.dtype, gate.device
@@ -217,6 +225,8 @@ class Experts:
         if self.grads and torch.is_grad_enabled():
             _refuse("the experts were packed from weights that require a gradient: these operators have no backward pass "
                     "(use torch.no_grad(), or pack detached weights)")
+        if _forward_ad._current_level >= 0:
+            _no_tangents(x, ids, weights, out)
         code = _dtype(x.dtype, "x")
         dev, D = self.device, self.d_model
         xs = _matrix(x, "x", dev, None, D)
@@ -276,10 +286,15 @@ def block_norm(x, y=None, *, gain=None, post_gain=None, gate=None, scale=1.0, ep
     Returns (x', h).  Without a y, x' is x itself; without a gain, h is None.
     ``x_out`` (which may be x) receives x'; ``h_dtype`` defaults to x's."""
     lib = _library()
+    if _forward_ad._current_level >= 0:
+        _no_tangents(x, y, gain, post_gain, gate, scale, eps, x_out)
     xs, xc = _matrix(x, "x"), _dtype(x.dtype, "x")
     rows, dim = x.shape
     dev = x.device
-    scale, eps = _number(scale, "scale"), _number(eps, "eps")
+    if type(scale) is not float:
+        scale = _number(scale, "scale")
+    if type(eps) is not float:
+        eps = _number(eps, "eps")
     yp = ys = yc = gp = gr = gs = gc = op = os_ = hp = gainp = hc = 0
     h = None
     if y is not None:

@@ -34,3 +34,19 @@ def test_packed_weights_keep_their_need_of_a_gradient(hvd, which):
     with torch.no_grad():
         assert torch.equal(layer.forward(x, ids, w), want)
     assert torch.equal(hvd.Experts(*(t.detach() for t in W)).forward(x, ids, w), want)
+
+
+def test_tangents_of_the_experts_arguments(hvd):
+    import torch.autograd.forward_ad as fwd
+    W = weights()
+    x, ids, w = torch.ones(3, 128, device="cuda"), torch.zeros(3, 1, dtype=torch.int32, device="cuda"), torch.ones(3, 1, device="cuda")
+    layer = hvd.Experts(*W)
+    want = layer.forward(x, ids, w)
+    with fwd.dual_level():
+        p = lambda t: fwd.make_dual(t, torch.ones_like(t))
+        calls = [lambda: layer.forward(p(x), ids, w), lambda: layer.forward(x, ids, p(w)), lambda: layer.forward(x, ids, w, out=p(x))]
+        calls += [lambda i=i: hvd.Experts(*(p(t) if i == j else t for j, t in enumerate(W))) for i in range(3)]
+        for call in calls:
+            with pytest.raises(hvd.HvdError, match="tangent"):
+                call()
+        assert torch.equal(hvd.Experts(*W).forward(x, ids, w), want)
