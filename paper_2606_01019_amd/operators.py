@@ -30,6 +30,10 @@ class BlockNormArgs(ctypes.Structure):
                 ("eps", ctypes.c_float)]
 
 
+# Limits of include/hvd.h that are checked here too: a size that is handed over as
+# 32 bits would come out as another one, within them.
+MAX_ROWS, MAX_EXPERT_ROWS, MAX_EXPERTS, MAX_DIM = 1 << 23, 1 << 18, 512, 16384
+
 # the same structure as bytes: a microsecond faster to fill than its fields
 _pack_norm = struct.Struct("@PqPqPqqPPPqPqiiiiff").pack
 assert len(_pack_norm(*[0] * 19)) == ctypes.sizeof(BlockNormArgs)
@@ -148,6 +152,8 @@ def route(logits, top_k, *, score="softmax", bias=None, n_groups=1, top_groups=1
     stride = _matrix(logits, "logits")
     code = _dtype(logits.dtype, "logits")
     rows, E = logits.shape
+    if rows > MAX_ROWS or E > MAX_EXPERTS:
+        _refuse(f"logits may have up to {MAX_ROWS} rows of up to {MAX_EXPERTS} experts")
     dev = logits.device
     # the key holds plain numbers: equal keys are equal configs, whatever becomes
     # of the objects they came from
@@ -168,12 +174,14 @@ def route(logits, top_k, *, score="softmax", bias=None, n_groups=1, top_groups=1
             _refuse(f"score must be one of {sorted(SCORES)}")
         if not abs(scale) <= 3.4028234663852886e38:
             _refuse("scale must be finite")
+        if not 1 <= top_groups <= n_groups <= E:
+            _refuse("n_groups must be in [1, n_experts], top_groups in [1, n_groups]")
+        if not 1 <= top_k <= 16:
+            _refuse("top_k must be in [1, 16]")
         if len(_configs) >= 256:
             _configs.clear()
         # (an address that stays: the library reads the config during the call only)
         cfg = _configs[key] = ctypes.pointer(RouteConfig(E, top_k, SCORES[score], n_groups, top_groups, renorm, scale))
-    if not 1 <= top_k <= 16:
-        _refuse("top_k must be in [1, 16]")
     bp = _vector(bias, "bias", E, dev) if bias is not None else None
     ids = torch.empty((rows, top_k), dtype=torch.int32, device=dev)
     w = torch.empty((rows, top_k), dtype=torch.float32, device=dev)
@@ -196,6 +204,8 @@ class Experts:
         if _forward_ad._current_level >= 0:
             _no_tangents(gate, up, down)
         E, F, D = gate.shape
+        if max(E, F, D) >= 1 << 31:
+            _refuse("n_experts must be in [1, 512], ffn_dim and d_model at most 131072")
         self.n_experts, self.ffn_dim, self.d_model = E, F, D
         self.dtype, self.device = gate.dtype, gate.device
         for t, what, shape in ((gate, "gate", (E, F, D)), (up, "up", (E, F, D)), (down, "down", (E, D, F))):
@@ -234,6 +244,8 @@ class Experts:
             _refuse("ids must be [rows, top_k]")
         shape = ids.shape
         T, k = shape
+        if T > MAX_EXPERT_ROWS or k > 16:
+            _refuse(f"ids may have up to {MAX_EXPERT_ROWS} rows of up to 16 experts")
         if T != x.shape[0]:
             _refuse("ids must have x's rows")
         ip = _exact(ids, "ids", shape, torch.int32, dev)
@@ -290,6 +302,8 @@ def block_norm(x, y=None, *, gain=None, post_gain=None, gate=None, scale=1.0, ep
         _no_tangents(x, y, gain, post_gain, gate, scale, eps, x_out)
     xs, xc = _matrix(x, "x"), _dtype(x.dtype, "x")
     rows, dim = x.shape
+    if rows > MAX_ROWS or dim > MAX_DIM:
+        _refuse(f"x may have up to {MAX_ROWS} rows of up to {MAX_DIM} columns")
     dev = x.device
     if type(scale) is not float:
         scale = _number(scale, "scale")

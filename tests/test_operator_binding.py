@@ -120,3 +120,23 @@ def test_tangents_are_refused_for_every_argument(lib):
                 call()
         for call in plain:  # tensors without one run inside a level too
             call()
+
+
+def wide(rows, cols):
+    """Any number of rows and columns, without memory."""
+    return torch.empty(rows, cols, device="meta").as_subclass(OnGpu)
+
+
+W = 1 << 32
+
+
+@pytest.mark.parametrize("call", [
+    lambda: hvd.route(wide(W + 1, 8), 1), lambda: hvd.route(wide(1, W + 8), 1),
+    lambda: hvd.route(gpu(3, 8), 2, n_groups=W + 1), lambda: hvd.route(gpu(3, 8), 2, n_groups=4, top_groups=W + 2),
+    lambda: hvd.route(gpu(3, 8), W + 2), lambda: hvd.route(gpu(3, 8), 2, n_groups=1 - W),
+    lambda: hvd.block_norm(wide(W + 1, 8), wide(W + 1, 8)), lambda: hvd.block_norm(wide(3, W + 1), wide(3, W + 1))])
+def test_sizes_past_32_bits(lib, call):
+    """They would arrive as small ones, and leave outputs unwritten."""
+    with pytest.raises(hvd.HvdError):
+        call()
+    assert not lib.routed and not lib.normed
