@@ -80,6 +80,11 @@ def _no_tangents(*args):
             _refuse("an argument has a tangent: these operators have no forward-mode derivative")
 
 
+def _written(t):
+    """t was written in place: autograd refuses a backward pass that saved it."""
+    torch.autograd.graph.increment_version(t)
+
+
 def _number(v, what):
     """The float that an argument other than one stands for.  A tensor's value is
     taken now; one that requires a gradient is refused like any other."""
@@ -273,6 +278,8 @@ class Experts:
               work.data_ptr(), n)
         if torch._C._cuda_getCurrentRawStream(dev.index) != self.home.cuda_stream and not torch.cuda.is_current_stream_capturing():
             self.buf.record_stream(torch.cuda.current_stream(dev))  # close() may give the weights back while this call runs
+        if out is not None:
+            _written(out)
         return dst
 
     __call__ = forward
@@ -311,6 +318,7 @@ def block_norm(x, y=None, *, gain=None, post_gain=None, gate=None, scale=1.0, ep
         eps = _number(eps, "eps")
     yp = ys = yc = gp = gr = gs = gc = op = os_ = hp = gainp = hc = 0
     h = None
+    given = x_out is not None
     if y is not None:
         yp, ys, yc = y.data_ptr(), _matrix(y, "y", dev, rows, dim), _dtype(y.dtype, "y")
         if x_out is None:
@@ -343,4 +351,6 @@ def block_norm(x, y=None, *, gain=None, post_gain=None, gate=None, scale=1.0, ep
     pp = _vector(post_gain, "post_gain", dim, dev) if post_gain is not None else 0
     _call(dev, lib.hvd_block_norm, _pack_norm(x.data_ptr(), xs, yp, ys, gp, gr, gs, pp, gainp, op, os_, hp, dim, xc, yc,
                                               gc, hc, scale, eps), rows, dim)
+    if given:
+        _written(x_out)
     return (x if y is None else x_out), h

@@ -50,3 +50,15 @@ def test_tangents_of_the_experts_arguments(hvd):
             with pytest.raises(hvd.HvdError, match="tangent"):
                 call()
         assert torch.equal(hvd.Experts(*W).forward(x, ids, w), want)
+
+
+def test_an_output_that_is_given_counts_as_changed(hvd):
+    """A backward pass that saved the output's buffer notices that it was written."""
+    layer = hvd.Experts(*weights())
+    x, ids, w = torch.ones(3, 128, device="cuda"), torch.zeros(3, 1, dtype=torch.int32, device="cuda"), torch.ones(3, 1, device="cuda")
+    for write in (lambda o: layer.forward(x, ids, w, out=o), lambda o: hvd.block_norm(x, x, x_out=o)):
+        out, a = torch.zeros(3, 128, device="cuda"), torch.ones(3, 128, device="cuda", requires_grad=True)
+        z = (a * out).sum()
+        write(out)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            z.backward()

@@ -140,3 +140,19 @@ def test_sizes_past_32_bits(lib, call):
     with pytest.raises(hvd.HvdError):
         call()
     assert not lib.routed and not lib.normed
+
+
+def test_an_output_that_is_given_counts_as_changed(lib):
+    """A backward pass that saved x notices that x_out overwrote it."""
+    a, y = torch.ones(3, 8, requires_grad=True), gpu(3, 8)
+    x = gpu(3, 8)
+    z = (a * x).sum()
+    hvd.block_norm(x, y)
+    version = x._version
+    hvd.block_norm(x, y, x_out=x)
+    assert x._version > version
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        z.backward()
+    with torch.inference_mode():
+        t = gpu(3, 8)
+        hvd.block_norm(t, t, x_out=t)
