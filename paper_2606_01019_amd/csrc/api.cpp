@@ -1217,12 +1217,12 @@ hvd_status forward(hvd_kv_s* k, const std::vector<SeqMeta>& seqs, std::vector<Ro
       ns = 2;
       splits = std::max(1, std::min((kGemmSplitTarget + nb2 - 1) / nb2, KT / 64));
     }
-    if (family <= PF_LM && k->gemm_force[family][0]) {
-      const int fns = k->gemm_force[family][0];
+    if (const int* force = forced_shape(k->gemm_force, family); force[0]) {
+      const int fns = force[0];
       const bool ok = NT % fns == 0 && !(fns == 1 && epi == EPI_SILU) && !(fns == 8 && (mt_block > 2 || N % 128));
       if (ok) {
         ns = fns;
-        splits = std::min(k->gemm_force[family][1], KT);
+        splits = std::min(force[1], KT);
       }
     }
     while (splits > 1 && (size_t)(N / 16) * 16 * splits * mt_block * 16 * mblocks * 4 > sx.gemm_part_bytes) --splits;
@@ -1468,8 +1468,8 @@ hvd_status forward(hvd_kv_s* k, const std::vector<SeqMeta>& seqs, std::vector<Ro
       const bool mlp = epi == EPI_SILU || family == PF_DOWN;
       const bool single = lm_head && ((mlp && (epi == EPI_SILU ? k->mlp_single_gu : k->mlp_single_down)) ||
                                       (family == PF_LM && k->lm_single));
-      const int* force = k->tiled_force[family <= PF_LM ? family : 0];
-      const bool forced = family <= PF_LM && force[0] && N % kTileBN[force[0] - 1] == 0;
+      const int* force = forced_shape(k->tiled_force, family);
+      const bool forced = force[0] && N % kTileBN[force[0] - 1] == 0;
       const TiledPlan plan = forced ? tiled_plan_forced(force[0] - 1, std::max(1, std::min(force[1], a.KT / 32)), MT, N,
                                                         a.KT, sx.gemm_part_bytes)
                                     : tiled_plan(MT, N, a.KT, single, kCUs, sx.gemm_part_bytes);
@@ -1488,7 +1488,8 @@ hvd_status forward(hvd_kv_s* k, const std::vector<SeqMeta>& seqs, std::vector<Ro
                         ((epi == EPI_SILU && k->mlp_single_gu) || (family == PF_DOWN && k->mlp_single_down) ||
                          (k->lm_single && family == PF_LM));
     if (mid_takes(MT, N, K)) {
-      const MidPlan plan = mid_plan(MT, a.NT, a.KT, k->gemm_min_blocks, k->ns8_mt3, sx.gemm_part_bytes, k->gemm_force[family]);
+      const MidPlan plan = mid_plan(MT, a.NT, a.KT, k->gemm_min_blocks, k->ns8_mt3, sx.gemm_part_bytes,
+                                    forced_shape(k->gemm_force, family));
       if (epi == EPI_LM) {
         lm_parts = a.NT / plan.strips;
         a.n_part = lm_parts;

@@ -72,6 +72,14 @@ int hvdh_mid_plan(int32_t mtiles, int32_t N, int32_t K, int32_t wide, int64_t pa
   out4[3] = p.mt_block;
   return hvd::mid_takes(mtiles, N, K);
 }
+// Forced shape of a GEMM family, of five that hold {10 f + 1, 10 f + 2}
+void hvdh_forced_shape(int32_t family, int32_t* out2) {
+  int force[5][2];
+  for (int f = 0; f < 5; ++f) force[f][0] = 10 * f + 1, force[f][1] = 10 * f + 2;
+  const int* p = hvd::forced_shape(force, family);
+  out2[0] = p[0];
+  out2[1] = p[1];
+}
 // Work plan of a large-batch GEMM: tile, workgroups, shared tiles, sharing workgroups
 void hvdh_tiled_plan(int32_t mtiles, int32_t N, int32_t KT, int32_t single, int32_t cus, int64_t part_bytes, int32_t* out4) {
   const hvd::TiledPlan p = hvd::tiled_plan(mtiles, N, KT, single != 0, cus, (size_t)part_bytes);

@@ -15,6 +15,14 @@ constexpr int kGemmSplitTarget = 256;        // workgroups a K split aims for (o
 constexpr int kGemmLongK = 256;              // K steps above which a K split pays for its reduction
 constexpr int kGemmCounters = 16384;         // split-K arrival counters (output blocks of one launch)
 
+// The shape a caller forced on the GEMMs of a family, {0, 0} = none; GEMMs outside
+// the N families that can be forced (an expert layer's router) have none.
+template <int N>
+const int* forced_shape(const int (&force)[N][2], int family) {
+  static constexpr int none[2] = {0, 0};
+  return family >= 0 && family < N ? force[family] : none;
+}
+
 // strips of 16 columns per workgroup (4 or 8), K splits, row blocks and their row tiles
 struct MidPlan {
   int strips, splits, mblocks, mt_block;
