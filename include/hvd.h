@@ -405,7 +405,8 @@ hvd_status hvd_experts_load(const hvd_experts_config* cfg, const void* gate, con
                             void* dev_buf, size_t dev_bytes, void* stream, hvd_experts* out);
 void hvd_experts_free(hvd_experts e);
 
-/* Workspace bytes of a forward call (0 for arguments it would refuse). */
+/* Workspace bytes that serve every forward call of up to `rows` rows (0 for
+ * arguments it would refuse); they grow with rows. */
 size_t hvd_experts_workspace(hvd_experts e, int32_t rows, int32_t top_k, int32_t x_dtype);
 
 /* out[t] = sum over j of weights[t][j] * down(silu(gate x[t]) * (up x[t])) of

@@ -538,20 +538,14 @@ size_t meta_capacity_ints(const hvd_config& c, int max_rows, int max_seqs, int p
          item_ints * (4 * units + 4 * kPartSlots + kAttnClasses * (64 + 16)) + 3 * (size_t)max_seqs * pt_stride + 64;
 }
 
-// Workspace of the experts for any forward of at most `rows` rows: the few-row
-// forms have sizes of their own, above them it grows with the rows.
-size_t experts_bytes_for(int d_model, const hvd_moe_config& m, int rows) {
+// Workspace of the experts for any forward of at most `rows` rows.
+size_t experts_work_bytes(const hvd_config& c, const hvd_moe_config& m, int rows) {
   ExpertsArgs a{};
-  a.w = ExpertsW{nullptr, nullptr, m.route.n_experts, d_model, m.ffn_dim, ET_F16};
+  a.w = ExpertsW{nullptr, nullptr, m.route.n_experts, c.d_model, m.ffn_dim, ET_F16};
   a.x_type = ET_F32;
   a.T = rows;
   a.k = m.route.top_k;
-  return experts_carve(a, nullptr);
-}
-size_t experts_work_bytes(const hvd_config& c, const hvd_moe_config& m, int rows) {
-  size_t most = 0;
-  for (int T = 1; T <= std::min(rows, kFewRows); ++T) most = std::max(most, experts_bytes_for(c.d_model, m, T));
-  return std::max(most, experts_bytes_for(c.d_model, m, rows));
+  return experts_workspace(a);
 }
 
 size_t carve_kv(hvd_kv_s* k, const hvd_config& c, const hvd_moe_config* moe, int max_seqs, int n_pages, void* base) {

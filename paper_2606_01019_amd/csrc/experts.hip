@@ -1010,6 +1010,20 @@ static Form form_of(const ExpertsArgs& a) {
   return fills ? FORM_T64_PAIR : FORM_T128_PAIR;
 }
 
+size_t experts_workspace(ExpertsArgs a) {
+  // A form's workspace grows with the rows, so the most that up to a.T rows take
+  // is at a.T or at the last rows of a form.
+  const int rows = a.T, E = a.w.E, k = a.k, full = 128 * kTileCUs;
+  const int ends[] = {1, 16, kFewRows, kFewSlots / k, (int)std::min<int64_t>(rows, ((int64_t)kPairRows * E - 1) / k),
+                      (full - 1) / a.w.F / k, rows};
+  size_t most = 0;
+  for (int T : ends) {
+    a.T = std::min(T, rows);
+    most = std::max(most, experts_carve(a, nullptr));
+  }
+  return most;
+}
+
 size_t experts_carve(ExpertsArgs& a, void* base) {
   size_t off = 0;
   auto take = [&](size_t bytes) {

@@ -101,7 +101,9 @@ struct ExpertsArgs {
   uint32_t* arrived;  // parts of each shared tile that are done (cleared by every call)
   float* part;        // shared tiles' partial sums
 };
-// Bytes of the workspace of a call, and its layout over `base`.
+// Bytes of the workspace of a call with up to a.T rows.
+size_t experts_workspace(ExpertsArgs a);
+// Bytes of the workspace of a call of exactly a.T rows, and its layout over `base`.
 size_t experts_carve(ExpertsArgs& a, void* base);
 hipError_t launch_experts(const ExpertsArgs& a, hipStream_t s);
 // Packs the weights of n experts: src row-major [n][rows][cols] on the device,

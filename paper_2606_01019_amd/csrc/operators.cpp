@@ -143,7 +143,7 @@ extern "C" size_t hvd_experts_workspace(hvd_experts e, int32_t rows, int32_t top
   a.T = rows;
   a.k = top_k;
   a.x_type = x_dtype;
-  return std::max<size_t>(experts_carve(a, nullptr), 256);  // (0 is a refusal)
+  return std::max<size_t>(experts_workspace(a), 256);  // (0 is a refusal)
 }
 
 extern "C" hvd_status hvd_experts_forward(hvd_experts e, int32_t rows, int32_t top_k, const void* x, int32_t x_dtype,
