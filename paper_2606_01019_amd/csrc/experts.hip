@@ -1051,7 +1051,8 @@ size_t experts_carve(ExpertsArgs& a, void* base) {
   a.xlo = pair ? (uint16_t*)take((size_t)a.T * D * 2) : nullptr;
   a.y = (float*)take(n * D * 4);
   a.arrived = (uint32_t*)take(kTileCUs * 4);
-  a.part = (float*)take((size_t)kTileCUs * T128::BM * T128::BN * 4);
+  // (64-row tiles are not shared)
+  a.part = f != FORM_T64_PAIR ? (float*)take((size_t)kTileCUs * T128::BM * T128::BN * 4) : nullptr;
   return off;
 }
 

@@ -44,3 +44,15 @@ def test_one_workspace_for_all_row_counts(hvd, E, k, D, F, dtype):
     assert lib.hvd_experts_forward(h, N, k, x.data_ptr(), code, D, ids.data_ptr(), w.data_ptr(), out.data_ptr(), D,
                                    work.data_ptr(), 255, s) != 0  # too small
     assert size(0) > 0 and size(-1) == 0
+
+
+def test_no_partial_sums_where_no_tile_is_shared(hvd):
+    """Calls of few rows per expert: slots, products and outputs, without the 32 MiB
+    of partial sums that 128-row tiles share."""
+    E, k, D, F = 64, 8, 64, 1024
+    layer = hvd.Experts(*(torch.zeros(s, dtype=torch.float16, device="cuda") for s in ((E, F, D), (E, F, D), (E, D, F))))
+    for T in (33, 64, 127):
+        need = layer.lib.hvd_experts_workspace(layer.handle, T, k, 0)
+        few = 2 * E * 16 * F * 2  # (the largest few-row call)
+        assert need <= max(few, T * k * (2 * 4 + 2 * F * 2 + D * 4)) + 16384, (T, need)
+    assert layer.lib.hvd_experts_workspace(layer.handle, 128, k, 0) > 32 << 20
