@@ -412,12 +412,14 @@ size_t hvd_experts_workspace(hvd_experts e, int32_t rows, int32_t top_k, int32_t
 /* out[t] = sum over j of weights[t][j] * down(silu(gate x[t]) * (up x[t])) of
  * expert ids[t][j], for rows of x [rows][d_model]; 1 <= top_k <= 16, rows <=
  * 262144.  x_dtype is the weights' type, or HVD_F32 with HVD_F16 weights: then
- * activations run as fp16 hi + lo pairs (about 22 bits).  out [rows][d_model]
- * has x's type.  ids outside [0, n_experts) (hvd_route's -1) add nothing,
+ * x and the product silu * up run as fp16 hi + lo pairs, each row of them scaled
+ * by a power of two, so that about 22 bits hold whatever their size.  out
+ * [rows][d_model] has x's type.  ids outside [0, n_experts) (hvd_route's -1) add nothing,
  * whatever their weight; a row without an expert is written 0; an id that
- * comes twice counts twice.  The product silu * up is rounded to 16 bits (to
- * the pair with HVD_F32); with HVD_F16 and HVD_F32 it and the activations must
- * stay within fp16's range.  x, out and work are 16-byte aligned, their row
+ * comes twice counts twice.  With HVD_F16 and HVD_BF16 the product is rounded to
+ * that type (calls of few rows per expert may keep more bits of it); with HVD_F16
+ * it has to stay within fp16's range: above 65504 it is infinite, below 2^-14 it
+ * loses bits.  x, out and work are 16-byte aligned, their row
  * strides multiples of 16 bytes; out may not overlap x.  work holds
  * hvd_experts_workspace bytes and belongs to this call until it is done:
  * calls that may overlap, and graphs that may run at once, need one each. */

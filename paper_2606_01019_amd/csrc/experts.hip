@@ -13,6 +13,14 @@
 // tile, about 22 bits).  The activation silu(gate) * up is rounded to that
 // form, which is what the matrix instructions take; everything that is summed
 // is 32-bit.
+//
+// 32-bit values have a larger range than the pair, so each row of x, and of
+// silu(gate) * up each row (of 32 columns in the few-row form), is scaled by
+// the power of two that brings its largest magnitude to [2^14, 2^15): the pair
+// keeps 22 bits of values down to 2^-17 of the largest, and 2^-39 of the
+// largest below.  The scale is undone on 32-bit sums.  (silu * up is about
+// quadratic in x: unscaled, x of size 1e-2 left 11 bits of it, 1e-4 none, and 1e3
+// overflowed.)
 #include "common.h"
 #include "kernels.h"
 #include "moe.h"
@@ -74,6 +82,29 @@ __device__ __forceinline__ uint16_t to16(float v) {
 }
 // (exp through the hardware exp2: 1 + exp(-v) is good to a few 2^-24; v below -88 gives v / inf = -0)
 __device__ __forceinline__ float silu(float v) { return v / (1.f + __expf(-v)); }
+
+// ---------------------------------------------------------------- scaled pairs
+
+// The power of two of values up to m in magnitude, as a biased exponent b in
+// [1, 240]: v * pow2_down(b) is below 2^15, pow2_up(b) undoes it.
+__device__ __forceinline__ int scale_exp(float m) { return max((int)(__float_as_uint(m) >> 23) - 14, 1); }
+__device__ __forceinline__ float pow2_up(int b) { return __uint_as_float((uint32_t)b << 23); }
+__device__ __forceinline__ float pow2_down(int b) { return __uint_as_float((uint32_t)(254 - b) << 23); }
+// Infinities and NaN do not count: they stay what they are under any scale.
+__device__ __forceinline__ float max_finite(float m, float v) {
+  const float a = fabsf(v);
+  return a <= 3.402823466e38f ? fmaxf(m, a) : m;
+}
+// The max over the 16 lanes of a row, by data-parallel permutes.
+__device__ __forceinline__ float row16_max(float v) {
+  auto dpp = [](float x, auto ctrl) __attribute__((always_inline)) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), decltype(ctrl)::value, 0xf, 0xf, false));
+  };
+  v = fmaxf(v, dpp(v, std::integral_constant<int, 0xB1>{}));
+  v = fmaxf(v, dpp(v, std::integral_constant<int, 0x4E>{}));
+  v = fmaxf(v, dpp(v, std::integral_constant<int, 0x141>{}));
+  return fmaxf(v, dpp(v, std::integral_constant<int, 0x140>{}));
+}
 
 // ---------------------------------------------------------------- slots in expert order
 
@@ -224,7 +255,8 @@ __device__ __forceinline__ Tile find_tile(const ExpertsArgs& a, int CB, int KT) 
 // Places past the list repeat its last one and are not stored; a tile belongs
 // to one expert.
 // GU: rows of x, silu(gate) * up out (OP: as a pair); else rows of that
-// product, the expert's output out.  AP: the row operand is a pair.
+// product, the expert's output out.  AP: the row operand is a pair; GU's is then
+// scaled (xs), and its product goes out in 32 bits, to be scaled by whole rows.
 template <int WY_, int WX_, int WM_, int WN_>
 struct TileShape {
   static constexpr int WY = WY_, WX = WX_, WM = WM_, WN = WN_, NW = WY * WX;
@@ -448,6 +480,13 @@ __global__ __launch_bounds__(64 * S::NW, 2) void experts_tiled(ExpertsArgs a, in
   };
   if (RPW > 1 && tl.rows <= BM / 2) with_blocks(std::integral_constant<int, RPW / 2>{});
   else with_blocks(std::integral_constant<int, RPW>{});
+  float row_up[WM][2];  // what undoes the scale of the rows this lane stores
+  if constexpr (GU && AP)
+#pragma unroll
+    for (int i = 0; i < WM; ++i)
+#pragma unroll
+      for (int it = 0; it < 2; ++it)
+        row_up[i][it] = a.xs[a.perm[tl.row0 + min(wy * 32 * WM + 32 * i + (lane >> 2) + 16 * it, tl.rows - 1)] / a.k];
   vm_wait<0>();  // no copy may land after the ring is reused or released
   __syncthreads();
 
@@ -531,18 +570,29 @@ __global__ __launch_bounds__(64 * S::NW, 2) void experts_tiled(ExpertsArgs a, in
           float g[8], u[8];
           oct(row, c, g);
           oct(row, c + 16, u);
+          if constexpr (AP)
+#pragma unroll
+            for (int n = 0; n < 8; ++n) {
+              g[n] *= row_up[i][it];
+              u[n] *= row_up[i][it];
+            }
 #pragma unroll
           for (int n = 0; n < 8; ++n) g[n] = silu(g[n]) * u[n];
           if (row0 + row < tl.rows) {
             const size_t at = (size_t)(tl.row0 + row0 + row) * F + (col0 >> 1) + o * 8;
-            uint4 hi, lo;
-            if constexpr (OP) {
-              pair8<BF>(g, hi, lo);
-              *(uint4*)(a.hlo + at) = lo;
+            if constexpr (AP) {
+              *(float4*)(a.y + at) = float4{g[0], g[1], g[2], g[3]};
+              *(float4*)(a.y + at + 4) = float4{g[4], g[5], g[6], g[7]};
             } else {
-              to16x8<BF>(g, hi);
+              uint4 hi, lo;
+              if constexpr (OP) {
+                pair8<BF>(g, hi, lo);
+                *(uint4*)(a.hlo + at) = lo;
+              } else {
+                to16x8<BF>(g, hi);
+              }
+              *(uint4*)(a.hhi + at) = hi;
             }
-            *(uint4*)(a.hhi + at) = hi;
           }
         }
       } else {
@@ -633,7 +683,13 @@ struct RowChoice {
 // expert; its 8 waves deal the K steps among themselves, so that the workgroup
 // reads one contiguous window, and sum in LDS.  h of expert y, row t goes to
 // row y * 16 MT + t, as a pair.
-// XF: x is 32-bit and becomes the fp16 pair here.  ONE: a single row.
+// XF: x is 32-bit and multiplied as the scaled pair.  A launch before this one
+// makes it, except for ONE, a single row: a workgroup reads that once ahead for its
+// scale, while the first weights are on their way.  (With more rows x is up to half
+// as many bytes as the weights to a workgroup: all of them reading 9 rows ahead, top 8 of 64
+// experts of 4096 x 1024, took this kernel from 94 to 113 us.)  The 32 columns of h
+// that a workgroup makes are one K step of the down product; their scale goes to hx
+// by (expert, step, row).
 template <int MT, int NS, bool BF, bool XF, bool ONE>
 __global__ __launch_bounds__(64 * kFewWaves, MT == 1 ? 4 : 2) void experts_gu_few(ExpertsArgs a) {
   constexpr int U = MT == 1 ? (XF ? 3 : 4) : (XF ? 3 : 4);
@@ -664,36 +720,58 @@ __global__ __launch_bounds__(64 * kFewWaves, MT == 1 ? 4 : 2) void experts_gu_fe
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     const int t = min(m * 16 + (lane & 15), a.T - 1);
-    xp[m] = (const char*)a.x + (t * a.x_stride + (lane >> 4) * 8) * (XF ? 4 : 2);
+    if constexpr (XF && !ONE) xp[m] = (const char*)(a.xhi + (size_t)t * D * 2 + (lane >> 4) * 8);
+    else xp[m] = (const char*)a.x + (t * a.x_stride + (lane >> 4) * 8) * (XF ? 4 : 2);
   }
+  constexpr int xq = XF && !ONE ? 64 : 16;  // from a lane's first 16 bytes of a step to its second
   f32x4 acc[MT][NS];
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
     for (int s = 0; s < NS; ++s) acc[m][s] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float x_down = 1.f, x_up[MT];  // a single row's scale; what undoes the scales of the rows this thread finishes
+  if constexpr (XF && !ONE)
+#pragma unroll
+    for (int m = 0; m < MT; ++m) x_up[m] = a.xs[min(m * 16 + (int)(threadIdx.x >> 4 & 15), a.T - 1)];
   u32x4 qw[U][NS], qx[U][MT][XQ];
-  auto load = [&](int u, int j) __attribute__((always_inline)) {
+  auto load_w = [&](int u, int j) __attribute__((always_inline)) {
     const int kt = wave + j * kFewWaves;
 #pragma unroll
     for (int s = 0; s < NS; ++s) qw[u][s] = __builtin_nontemporal_load(wp[s] + (size_t)kt * 256);
+  };
+  auto load_x = [&](int u, int j) __attribute__((always_inline)) {
+    const int kt = wave + j * kFewWaves;
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int q = 0; q < XQ; ++q) qx[u][m][q] = *(const u32x4*)(xp[m] + (size_t)kt * (XF ? 128 : 64) + q * 16);
+      for (int q = 0; q < XQ; ++q) qx[u][m][q] = *(const u32x4*)(xp[m] + (size_t)kt * (XF ? 128 : 64) + q * xq);
+  };
+  auto load = [&](int u, int j) __attribute__((always_inline)) {
+    load_w(u, j);
+    load_x(u, j);
   };
   auto consume = [&](int u) __attribute__((always_inline)) {
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
       if constexpr (XF) {
-        float v[8];
+        u32x4 h, l;
+        if constexpr (ONE) {
+          // (scaling the next steps' values early would hold them twice, and spill)
+          __builtin_amdgcn_sched_barrier(0);
+          float v[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v[i] = __uint_as_float(qx[u][m][0][i]);
-          v[4 + i] = __uint_as_float(qx[u][m][1][i]);
+          for (int i = 0; i < 4; ++i) {
+            v[i] = __uint_as_float(qx[u][m][0][i]) * x_down;
+            v[4 + i] = __uint_as_float(qx[u][m][1][i]) * x_down;
+          }
+          uint4 hi, lo;
+          pair8<false>(v, hi, lo);
+          h = u32x4{hi.x, hi.y, hi.z, hi.w};
+          l = u32x4{lo.x, lo.y, lo.z, lo.w};
+        } else {
+          h = qx[u][m][0];
+          l = qx[u][m][1];
         }
-        uint4 hi, lo;
-        pair8<false>(v, hi, lo);
-        const u32x4 h{hi.x, hi.y, hi.z, hi.w}, l{lo.x, lo.y, lo.z, lo.w};
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
           acc[m][s] = mfma16<BF>(h, qw[u][s], acc[m][s]);
@@ -705,9 +783,35 @@ __global__ __launch_bounds__(64 * kFewWaves, MT == 1 ? 4 : 2) void experts_gu_fe
       }
     }
   };
+  if constexpr (XF && ONE) {
+    if (nsteps >= U)
+#pragma unroll
+      for (int u = 0; u < U; ++u) load_w(u, u);
+    __builtin_amdgcn_sched_barrier(0);
+    __shared__ float s_max[kFewWaves];
+    const float* p = (const float*)a.x;
+    float mx = 0.f;
+    for (int c = threadIdx.x * 4; c < D; c += 64 * kFewWaves * 4) {
+      const f32x4 v = *(const f32x4*)(p + c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mx = max_finite(mx, v[i]);
+    }
+    mx = rows_max(row16_max(mx));
+    if (lane == 0) s_max[wave] = mx;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) mx = fmaxf(mx, s_max[w]);
+    const int b = scale_exp(mx);
+    x_down = pow2_down(b);
+    x_up[0] = pow2_up(b);
+    __builtin_amdgcn_sched_barrier(0);
+  }
   if (nsteps >= U) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) load(u, u);
+    for (int u = 0; u < U; ++u) {
+      if constexpr (!(XF && ONE)) load_w(u, u);
+      load_x(u, u);
+    }
     int j = 0;
     for (; j + 2 * U <= nsteps; j += U) {
 #pragma unroll
@@ -736,6 +840,40 @@ __global__ __launch_bounds__(64 * kFewWaves, MT == 1 ? 4 : 2) void experts_gu_fe
     for (int s = 0; s < NS; ++s) *(f32x4*)&red[wave][m][s][lane * 4] = acc[m][s];
   __syncthreads();
   // element (row, col) of a 16 x 16 tile is at [16 (row/4) + col] * 4 + row%4
+  if constexpr (XF) {
+    // 16 lanes per row and (gate strip, up strip) pair; the row's scale is both pairs'
+    static_assert(NS == 4, "a workgroup makes one K step of the down product");
+    __shared__ float s_top[MT][2][16];
+    const int c = threadIdx.x & 15, row = threadIdx.x >> 4 & 15, sp = threadIdx.x >> 8;
+    const int at = ((row >> 2) * 16 + c) * 4 + (row & 3);
+    float v[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      float g = 0.f, u = 0.f;
+#pragma unroll
+      for (int w = 0; w < kFewWaves; ++w) {
+        g += red[w][m][2 * sp][at];
+        u += red[w][m][2 * sp + 1][at];
+      }
+      v[m] = silu(g * x_up[m]) * (u * x_up[m]);
+      const float top = row16_max(max_finite(0.f, v[m]));
+      if (c == 0) s_top[m][sp][row] = top;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      const int t = m * 16 + row, b = scale_exp(fmaxf(s_top[m][0][row], s_top[m][1][row]));
+      if (t < a.T) {
+        const float h = v[m] * pow2_down(b);
+        const uint16_t hi = f2h(h);
+        const size_t o = ((size_t)blockIdx.y * (16 * MT) + t) * F + (blockIdx.x * 2 + sp) * 16 + c;
+        a.hhi[o] = hi;
+        a.hlo[o] = f2h(h - h2f(hi));
+        if (c == 0 && sp == 0) a.hx[((size_t)blockIdx.y * gridDim.x + blockIdx.x) * (16 * MT) + t] = (uint8_t)b;
+      }
+    }
+    return;
+  }
   for (int i = threadIdx.x; i < MT * (NS / 2) * 256; i += 64 * kFewWaves) {
     const int c = i & 15, row = i >> 4 & 15, sp = (i >> 8) % (NS / 2), m = (i >> 8) / (NS / 2);
     const int at = ((row >> 2) * 16 + c) * 4 + (row & 3);
@@ -763,7 +901,9 @@ __global__ __launch_bounds__(64 * kFewWaves, MT == 1 ? 4 : 2) void experts_gu_fe
 // alike, however the rows chose, the sums over k need no further pass, and a
 // row's result does not depend on the other rows of the call (alone, a row that
 // has an id twice adds the two products, not the weights: a rounding apart).
-template <int MT, int NS, bool BF, bool ONE>
+// XF: h is scaled by (row, K step): each step's products are scaled back into the
+// expert's sum.
+template <int MT, int NS, bool BF, bool XF, bool ONE>
 __global__ __launch_bounds__(64 * kFewWaves, 2) void experts_down_few(ExpertsArgs a) {
   constexpr int U = MT == 1 ? 8 : 4;
   __shared__ Distinct ds;
@@ -823,14 +963,17 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void experts_down_few(ExpertsArg
   const int total = spw * nd;
   if (total > 0) {
     u32x4 qw[U][NS], qh[U][MT], ql[U][MT];
+    uint32_t qe[U][MT];  // XF: the scales of this lane's four output rows, a byte each
     // the loader's place: expert ld, step li of it
     int ld = 0, li = 0;
     const u32x4* wp;
     uint32_t hoff[MT];  // halves; rows that did not choose the expert read its first row that did
+    const uint8_t* xe;
     auto enter = [&]() __attribute__((always_inline)) {
       const int e = ONE ? rc.expert(ld) : __builtin_amdgcn_readfirstlane(ds.list[ld]);
       const uint32_t vm = ONE ? 1u : __builtin_amdgcn_readfirstlane(vmask[ld]);
       wp = (const u32x4*)a.w.dn + (size_t)e * (D / 64) * KT * 256 + lane;
+      if constexpr (XF) xe = a.hx + (size_t)ld * KT * (16 * MT) + 4 * (lane >> 4);
       const int any = __builtin_ctz(vm);
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
@@ -850,6 +993,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void experts_down_few(ExpertsArg
       for (int m = 0; m < MT; ++m) {
         qh[u][m] = *(const u32x4*)(a.hhi + hoff[m] + kt * 32);
         ql[u][m] = *(const u32x4*)(a.hlo + hoff[m] + kt * 32);
+        if constexpr (XF) qe[u][m] = *(const uint32_t*)(xe + (size_t)kt * (16 * MT) + m * 16);
       }
       if (++li == spw) {
         li = 0;
@@ -863,8 +1007,16 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void experts_down_few(ExpertsArg
       for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-          acc[m][s] = mfma16<BF>(qh[u][m], qw[u][s], acc[m][s]);
-          acc[m][s] = mfma16<BF>(ql[u][m], qw[u][s], acc[m][s]);
+          if constexpr (XF) {
+            f32x4 z{0.f, 0.f, 0.f, 0.f};
+            z = mfma16<BF>(qh[u][m], qw[u][s], z);
+            z = mfma16<BF>(ql[u][m], qw[u][s], z);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[m][s][r] += z[r] * pow2_up(qe[u][m] >> 8 * r & 255u);
+          } else {
+            acc[m][s] = mfma16<BF>(qh[u][m], qw[u][s], acc[m][s]);
+            acc[m][s] = mfma16<BF>(ql[u][m], qw[u][s], acc[m][s]);
+          }
         }
       if (++ci == spw) {
         const uint32_t vm = ONE ? ~0u : vmask[cd];
@@ -935,22 +1087,50 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void experts_down_few(ExpertsArg
   }
 }
 
-// The activations' fp16 pair, 8 elements per thread.
-__global__ __launch_bounds__(256) void experts_split(ExpertsArgs a) {
-  const int D = a.w.D, per = D / 8;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= (int64_t)a.T * per) return;
-  const int t = (int)(i / per), c = (int)(i - (int64_t)t * per) * 8;
-  const float4* p = (const float4*)((const float*)a.x + t * a.x_stride + c);
-  const float4 u = p[0], q = p[1];
-  const float v[8] = {u.x, u.y, u.z, u.w, q.x, q.y, q.z, q.w};
-  uint4 hi, lo;
-  split8(v, hi, lo);
-  *(uint4*)(a.xhi + (size_t)t * D + c) = hi;
-  *(uint4*)(a.xlo + (size_t)t * D + c) = lo;
+// Rows of 32-bit values as the scaled fp16 pair, LANES threads per row (64: a
+// wave; 256: the workgroup), 8 columns per thread and step: one pass for the largest
+// magnitude, one (of a row that is in cache now; held in registers instead it took
+// as long) for the pair.  up[row] undoes the scale.  lo null: hi and lo of 32 columns
+// side by side, a cache line per row and K step, as the few-row form reads them (its
+// call of 16 rows, top 8 of 64 experts of 4096 x 1024: 222 us with 64 bytes of each
+// apart, 218 so).
+template <int LANES>
+__global__ __launch_bounds__(256) void experts_pair(const float* __restrict__ src, int64_t stride, int rows, int cols,
+                                                    uint16_t* __restrict__ hi, uint16_t* __restrict__ lo, float* __restrict__ up) {
+  __shared__ float s_max[4];
+  const int t = threadIdx.x & (LANES - 1), row = blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+  if (row >= rows) return;  // (whole waves; no row past the last with LANES 256)
+  const float* p = src + row * stride;
+  float mx = 0.f;
+#pragma unroll 4
+  for (int c = t * 8; c < cols; c += LANES * 8) {
+    const f32x4 u = *(const f32x4*)(p + c), v = *(const f32x4*)(p + c + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mx = max_finite(max_finite(mx, u[i]), v[i]);
+  }
+  mx = rows_max(row16_max(mx));
+  if constexpr (LANES > 64) {
+    if ((threadIdx.x & 63) == 0) s_max[threadIdx.x >> 6] = mx;
+    __syncthreads();
+    mx = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
+  }
+  const int b = scale_exp(mx);
+  const float down = pow2_down(b);
+#pragma unroll 4
+  for (int c = t * 8; c < cols; c += LANES * 8) {
+    const f32x4 u = *(const f32x4*)(p + c), v = *(const f32x4*)(p + c + 4);
+    const float w[8] = {u[0] * down, u[1] * down, u[2] * down, u[3] * down, v[0] * down, v[1] * down, v[2] * down, v[3] * down};
+    uint4 h, l;
+    pair8<false>(w, h, l);
+    uint16_t* const d = hi + (size_t)row * cols * (lo ? 1 : 2) + (lo ? c : c + (c & ~31));
+    *(uint4*)d = h;
+    *(uint4*)(lo ? lo + (size_t)row * cols + c : d + 32) = l;
+  }
+  if (t == 0) up[row] = pow2_up(b);
 }
 
-// out[t] = sum_j w[t][j] y[pos[t][j]], 4 columns per thread.
+// out[t] = sum_j w[t][j] y[pos[t][j]] (up[place] undoes the scale of its product),
+// 4 columns per thread.
 __global__ __launch_bounds__(256) void experts_combine(ExpertsArgs a) {
   const int D = a.w.D, c = (blockIdx.y * 256 + threadIdx.x) * 4, t = blockIdx.x;
   if (c >= D) return;
@@ -959,7 +1139,14 @@ __global__ __launch_bounds__(256) void experts_combine(ExpertsArgs a) {
     const int p = a.pos[t * a.k + j];
     if (p < 0) continue;
     const float w = a.weights[t * a.k + j];
-    const float4 y = *(const float4*)(a.y + (size_t)p * D + c);
+    float4 y = *(const float4*)(a.y + (size_t)p * D + c);
+    if (a.hs) {
+      const float up = a.hs[p];
+      y.x *= up;
+      y.y *= up;
+      y.z *= up;
+      y.w *= up;
+    }
     v.x += w * y.x;
     v.y += w * y.y;
     v.z += w * y.z;
@@ -1037,6 +1224,13 @@ size_t experts_carve(ExpertsArgs& a, void* base) {
     const size_t rows = std::min(n, (size_t)(a.T == 1 ? kMaxTopK : a.w.E)) * (f == FORM_FEW16 ? 16 : 32);  // (one row: an entry per slot)
     a.hhi = (uint16_t*)take(rows * F * 2);
     a.hlo = (uint16_t*)take(rows * F * 2);
+    if (a.x_type == ET_F32) {
+      a.hx = (uint8_t*)take(rows * (F / 32));
+      if (a.T > 1) {
+        a.xhi = (uint16_t*)take((size_t)a.T * D * 4);
+        a.xs = (float*)take((size_t)a.T * 4);
+      }
+    }
     return off;
   }
   const bool pair = a.x_type == ET_F32;
@@ -1049,18 +1243,26 @@ size_t experts_carve(ExpertsArgs& a, void* base) {
   a.hlo = pair || f <= FORM_T128_PAIR ? (uint16_t*)take(n * F * 2 + 64) : nullptr;
   a.xhi = pair ? (uint16_t*)take((size_t)a.T * D * 2) : nullptr;
   a.xlo = pair ? (uint16_t*)take((size_t)a.T * D * 2) : nullptr;
-  a.y = (float*)take(n * D * 4);
+  a.xs = pair ? (float*)take((size_t)a.T * 4) : nullptr;
+  a.hs = pair ? (float*)take(n * 4) : nullptr;
+  a.y = (float*)take(n * (pair ? std::max(D, F) : D) * 4);
   a.arrived = (uint32_t*)take(kTileCUs * 4);
   // (64-row tiles are not shared)
   a.part = f != FORM_T64_PAIR ? (float*)take((size_t)kTileCUs * T128::BM * T128::BN * 4) : nullptr;
   return off;
 }
 
+// (a wave per row leaves CUs without work below a thousand rows)
+static void launch_pair(const float* src, int64_t stride, int rows, int cols, uint16_t* hi, uint16_t* lo, float* up, hipStream_t s) {
+  if (rows < 4 * kTileCUs) hvd_launch(experts_pair<256>, dim3(rows), dim3(256), 0, s, src, stride, rows, cols, hi, lo, up);
+  else hvd_launch(experts_pair<64>, dim3((rows + 3) / 4), dim3(256), 0, s, src, stride, rows, cols, hi, lo, up);
+}
 template <int MT, bool BF, bool XF, bool ONE>
 static void launch_few(const ExpertsArgs& a, hipStream_t s) {
   const int n = std::min(a.T * a.k, ONE ? kMaxTopK : a.w.E);
+  if (XF && !ONE) launch_pair((const float*)a.x, a.x_stride, a.T, a.w.D, a.xhi, nullptr, a.xs, s);
   hvd_launch((experts_gu_few<MT, 4, BF, XF, ONE>), dim3(2 * a.w.F / 64, n), dim3(64 * kFewWaves), 0, s, a);
-  hvd_launch((experts_down_few<MT, 1, BF, ONE>), dim3(a.w.D / 16), dim3(64 * kFewWaves), 0, s, a);
+  hvd_launch((experts_down_few<MT, 1, BF, XF, ONE>), dim3(a.w.D / 16), dim3(64 * kFewWaves), 0, s, a);
 }
 template <int MT, bool ONE>
 static void launch_few_types(const ExpertsArgs& a, hipStream_t s) {
@@ -1076,6 +1278,7 @@ static void launch_products(const ExpertsArgs& a, hipStream_t s) {
   const int cg = (2 * a.w.F + S::BN - 1) / S::BN, cd = (a.w.D + S::BN - 1) / S::BN;
   // (shared tiles: less than a round of workgroups more)
   hvd_launch((experts_tiled<S, true, BF, XP, HP>), dim3(tiles * cg + (S::SPLIT ? kTileCUs : 0)), dim3(64 * S::NW), 0, s, a, cg);
+  if (XP) launch_pair(a.y, a.w.F, n, a.w.F, a.hhi, a.hlo, a.hs, s);
   hvd_launch((experts_tiled<S, false, BF, HP, false>), dim3(tiles * cd), dim3(64 * S::NW), 0, s, a, cd);
 }
 template <bool BF, bool XP>
@@ -1095,7 +1298,7 @@ hipError_t launch_experts(const ExpertsArgs& a, hipStream_t s) {
     return hipGetLastError();
   }
   hvd_launch(experts_sort, dim3(a.w.E), dim3(256), 0, s, a);
-  if (pair) hvd_launch(experts_split, dim3((unsigned)(((int64_t)a.T * (a.w.D / 8) + 255) / 256)), dim3(256), 0, s, a);
+  if (pair) launch_pair((const float*)a.x, a.x_stride, a.T, a.w.D, a.xhi, a.xlo, a.xs, s);
   pair ? launch_tiled<false, true>(a, f, s) : bf ? launch_tiled<true, false>(a, f, s) : launch_tiled<false, false>(a, f, s);
   hvd_launch(experts_combine, dim3(a.T, (a.w.D / 4 + 255) / 256), dim3(256), 0, s, a);
   return hipGetLastError();

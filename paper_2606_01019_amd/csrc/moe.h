@@ -97,7 +97,9 @@ struct ExpertsArgs {
   int32_t* off;      // [E] first place of each expert
   uint16_t *hhi, *hlo;  // silu(gate) * up, [places][F]
   uint16_t *xhi, *xlo;  // the activations' pair (ET_F32), [T][D]
-  float* y;          // [T*k][D] expert outputs by place
+  float *xs, *hs;       // ET_F32: what undoes the scales of x's rows [T] and the places' products [T*k]
+  uint8_t* hx;          // ET_F32, few rows: the scales of hhi and hlo as biased exponents [places][F/32][rows]
+  float* y;          // [T*k][D] expert outputs by place (ET_F32: before that, the places' products [T*k][F])
   uint32_t* arrived;  // parts of each shared tile that are done (cleared by every call)
   float* part;        // shared tiles' partial sums
 };
