@@ -290,17 +290,21 @@ __device__ __forceinline__ float from16(uint16_t b) {
   if constexpr (BF) return bf2f(b);
   else return h2f(b);
 }
+// What hi leaves over of v: nothing of an infinity, which would make NaN of it.
+template <bool BF>
+__device__ __forceinline__ uint16_t lo16(float v, uint16_t hi) {
+  const float h = from16<BF>(hi);
+  return to16<BF>(fabsf(h) == INFINITY ? 0.f : v - h);
+}
 template <bool BF>
 __device__ __forceinline__ void pair8(const float (&v)[8], uint4& hi, uint4& lo) {
   to16x8<BF>(v, hi);
   const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w};
-  float r[8];
+  uint32_t l[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    r[2 * i] = v[2 * i] - from16<BF>((uint16_t)(h[i] & 0xFFFFu));
-    r[2 * i + 1] = v[2 * i + 1] - from16<BF>((uint16_t)(h[i] >> 16));
-  }
-  to16x8<BF>(r, lo);
+  for (int i = 0; i < 4; ++i)
+    l[i] = lo16<BF>(v[2 * i], (uint16_t)(h[i] & 0xFFFFu)) | (uint32_t)lo16<BF>(v[2 * i + 1], (uint16_t)(h[i] >> 16)) << 16;
+  lo = uint4{l[0], l[1], l[2], l[3]};
 }
 
 // f(constant of value i), i clamped to [0, N)
@@ -868,7 +872,7 @@ __global__ __launch_bounds__(64 * kFewWaves, MT == 1 ? 4 : 2) void experts_gu_fe
         const uint16_t hi = f2h(h);
         const size_t o = ((size_t)blockIdx.y * (16 * MT) + t) * F + (blockIdx.x * 2 + sp) * 16 + c;
         a.hhi[o] = hi;
-        a.hlo[o] = f2h(h - h2f(hi));
+        a.hlo[o] = lo16<false>(h, hi);
         if (c == 0 && sp == 0) a.hx[((size_t)blockIdx.y * gridDim.x + blockIdx.x) * (16 * MT) + t] = (uint8_t)b;
       }
     }
@@ -889,7 +893,7 @@ __global__ __launch_bounds__(64 * kFewWaves, MT == 1 ? 4 : 2) void experts_gu_fe
       const uint16_t hi = to16<BF>(v);
       const size_t o = ((size_t)blockIdx.y * (16 * MT) + t) * F + (blockIdx.x * (NS / 2) + sp) * 16 + c;
       a.hhi[o] = hi;
-      a.hlo[o] = to16<BF>(v - from16<BF>(hi));
+      a.hlo[o] = lo16<BF>(v, hi);
     }
   }
 }
