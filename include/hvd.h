@@ -432,7 +432,7 @@ hvd_status hvd_experts_forward(hvd_experts e, int32_t rows, int32_t top_k, const
  *     v = rms(y) * post_gain,  x' = x + scale * gate * v,  h = rms(x') * gain.
  * y NULL: x' = x.  post_gain NULL: v = y.  gate NULL: 1; its strides may be 0
  * (one value for a row or a column).  x_out NULL: x' is not written; it has
- * x's type and may be x itself.  h NULL (or gain NULL with h NULL): no h.
+ * x's type and may be x itself; outputs overlap nothing else.  h NULL (or gain NULL with h NULL): no h.
  * gains are float [dim].  1 <= dim <= 16384, any alignment the types allow.
  * Sums are 32-bit, and h is computed from x' before its rounding to x's type. */
 typedef struct {
@@ -474,7 +474,8 @@ typedef struct {
  *   attn_norm [D], wq, wk, wv, wo, mlp_norm [D] as before, router [E, D],
  *   router_bias [E] (the bias of hvd_route; may be NULL), gate [E, F, D],
  *   up [E, F, D], down [E, D, F], post_norm [D] (NULL without post_norm);
- * count = 3 + 9 * first_layer + 12 * (n_layers - first_layer).  cfg->ffn_dim is
+ * count = 3 + 9 * first_layer + 12 * (n_layers - first_layer).  d_model is at
+ * most 16384, the experts' ffn_dim at most 131072.  cfg->ffn_dim is
  * the dense layers' and has to be valid even without one.  Handles from
  * here work with every call of this header; HVD_OPT_FLOW has no effect on
  * them. */

@@ -199,7 +199,8 @@ class Experts:
     [n_experts, ffn_dim, d_model], down [n_experts, d_model, ffn_dim], float16
     or bfloat16, packed once.  Weights that require a gradient are packed under
     torch.no_grad() only, and such a layer runs under it only; detached ones are
-    plain data."""
+    plain data.  A graph that captured calls reads the packed weights at every
+    replay: close the layer after its last one."""
 
     def __init__(self, gate, up, down):
         self.handle = None
@@ -213,6 +214,8 @@ class Experts:
             _refuse("n_experts must be in [1, 512], ffn_dim and d_model at most 131072")
         self.n_experts, self.ffn_dim, self.d_model = E, F, D
         self.dtype, self.device = gate.dtype, gate.device
+        if torch.cuda.is_current_stream_capturing():
+            _refuse("experts are packed outside of a graph's capture (the packing is waited for)")
         for t, what, shape in ((gate, "gate", (E, F, D)), (up, "up", (E, F, D)), (down, "down", (E, D, F))):
             _exact(t, what, shape, gate.dtype, gate.device)
         cfg = ExpertsConfig(E, D, F, _dtype(gate.dtype, "weights"))

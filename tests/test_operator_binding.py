@@ -156,3 +156,10 @@ def test_an_output_that_is_given_counts_as_changed(lib):
     with torch.inference_mode():
         t = gpu(3, 8)
         hvd.block_norm(t, t, x_out=t)
+
+
+def test_packing_inside_a_capture_is_refused(lib, monkeypatch):
+    """Its wait would end the capture with an error."""
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    with pytest.raises(hvd.HvdError, match="capture"):
+        ops.Experts(gpu(2, 32, 64), gpu(2, 32, 64), gpu(2, 64, 32))
