@@ -19,7 +19,7 @@
 // the power of two that brings its largest magnitude to [2^14, 2^15): the pair
 // keeps 22 bits of values down to 2^-17 of the largest, and 2^-39 of the
 // largest below.  The scale is undone on 32-bit sums.  (silu * up is about
-// quadratic in x: unscaled, x of size 1e-2 left 11 bits of it, 1e-4 none, and 1e3
+// quadratic in x: unscaled, x of size 1e-2 left 11 bits of it, 1e-4 none, and 100
 // overflowed.)
 #include "common.h"
 #include "kernels.h"
@@ -80,7 +80,8 @@ __device__ __forceinline__ uint16_t to16(float v) {
   if constexpr (BF) return __builtin_bit_cast(uint16_t, (__bf16)v);
   else return f2h(v);
 }
-// (exp through the hardware exp2: 1 + exp(-v) is good to a few 2^-24; v below -88 gives v / inf = -0)
+// (exp through the hardware exp2: its relative error is a few 2^-24 and |v| 2^-24 more
+// from the exponent's rounding, which counts where exp(-v) does, below 0; v below -88 gives v / inf = -0)
 __device__ __forceinline__ float silu(float v) { return v / (1.f + __expf(-v)); }
 
 // ---------------------------------------------------------------- scaled pairs
@@ -696,7 +697,7 @@ struct RowChoice {
 // by (expert, step, row).
 template <int MT, int NS, bool BF, bool XF, bool ONE>
 __global__ __launch_bounds__(64 * kFewWaves, MT == 1 ? 4 : 2) void experts_gu_few(ExpertsArgs a) {
-  constexpr int U = MT == 1 ? (XF ? 3 : 4) : (XF ? 3 : 4);
+  constexpr int U = XF ? 3 : 4;  // K steps in flight
   constexpr int XQ = XF ? 2 : 1;  // 16-byte loads per lane and row tile
   __shared__ float red[kFewWaves][MT][NS][256];
   int e;
