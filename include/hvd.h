@@ -474,8 +474,8 @@ typedef struct {
  *   attn_norm [D], wq, wk, wv, wo, mlp_norm [D] as before, router [E, D],
  *   router_bias [E] (the bias of hvd_route; may be NULL), gate [E, F, D],
  *   up [E, F, D], down [E, D, F], post_norm [D] (NULL without post_norm);
- * count = 3 + 9 * first_layer + 12 * (n_layers - first_layer).  d_model is at
- * most 16384, the experts' ffn_dim at most 131072.  cfg->ffn_dim is
+ * count = 3 + 9 * first_layer + 12 * (n_layers - first_layer).  n_layers is at
+ * most 65536, d_model 16384, the experts' ffn_dim 131072.  cfg->ffn_dim is
  * the dense layers' and has to be valid even without one.  Handles from
  * here work with every call of this header; HVD_OPT_FLOW has no effect on
  * them. */

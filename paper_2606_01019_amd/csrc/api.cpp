@@ -105,10 +105,14 @@ hvd_status check_config(const hvd_config* c) {
   return HVD_OK;
 }
 
+constexpr int kMaxExpertLayers = 1 << 16;
+
 // Checks a decoder with expert layers (moe null: a dense one).
 hvd_status check_moe(const hvd_config* c, const hvd_moe_config* moe) {
   if (hvd_status st = check_config(c); st != HVD_OK) return st;
   if (!moe) return HVD_OK;
+  // (the host keeps a block per layer, and counts tensors in 32 bits)
+  if (c->n_layers > kMaxExpertLayers) return set_err(HVD_ERR_ARG, "n_layers of a decoder with experts must be at most 65536");
   if (moe->first_layer < 0 || moe->first_layer >= c->n_layers) return set_err(HVD_ERR_ARG, "first_layer must be in [0, n_layers)");
   if (moe->ffn_dim < 32 || moe->ffn_dim % 32 || moe->ffn_dim > (1 << 17) || c->d_model > (1 << 17))
     return set_err(HVD_ERR_ARG, "the experts' ffn_dim must be a positive multiple of 32, it and d_model at most 131072");
