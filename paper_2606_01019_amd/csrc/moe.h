@@ -96,7 +96,7 @@ struct ExpertsArgs {
   int32_t* cnt;      // [E] slots of each expert
   int32_t* off;      // [E] first place of each expert
   uint16_t *hhi, *hlo;  // silu(gate) * up, [places][F]
-  uint16_t *xhi, *xlo;  // the activations' pair (ET_F32), [T][D]
+  uint16_t *xhi, *xlo;  // the activations' pair (ET_F32), [T][D]; few rows: xhi alone, [T][D/32][hi, lo][32]
   float *xs, *hs;       // ET_F32: what undoes the scales of x's rows [T] and the places' products [T*k]
   uint8_t* hx;          // ET_F32, few rows: the scales of hhi and hlo as biased exponents [places][F/32][rows]
   float* y;          // [T*k][D] expert outputs by place (ET_F32: before that, the places' products [T*k][F])
