@@ -453,6 +453,147 @@ typedef struct {
 } hvd_block_norm_args;
 hvd_status hvd_block_norm(const hvd_block_norm_args* args, int32_t rows, int32_t dim, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Operators on the rows of several sequences: what a verify step of a decoder
+ * that is not loaded here needs around its matrix products -- its keys and
+ * values into a paged cache, the attention over it, and the penalties and masks
+ * on its logits.  A step's rows are those of its sequences one after the other:
+ * the pending token and the drafts (a chain or a tree), a prompt's chunk, or one
+ * token.
+ *
+ * The conventions of the expert layer's operators hold: DEVICE buffers of the
+ * current device, calls that enqueue on `stream` and return without waiting,
+ * that allocate nothing, hold no state and may be captured into a graph; bad
+ * arguments are HVD_ERR_ARG and nothing is enqueued.  rows is at most 1048576
+ * (65536 for hvd_adjust_logits), rows = 0 does nothing.  What the device buffers
+ * of a batch hold is read when the call runs, so a captured call follows them;
+ * their values are bounded by the kernels: rows, keys and pages that do not
+ * exist are neither read nor written. */
+typedef struct {
+  const int32_t* starts;   /* [n_seqs + 1], nondecreasing from 0: sequence s has rows starts[s] .. starts[s + 1] - 1;
+                              rows from starts[n_seqs] on belong to none */
+  const int32_t* lengths;  /* [n_seqs] keys of each sequence, those of this step's n rows included: row i of a
+                              sequence is key ctx + i, ctx = length - n */
+  const int32_t* pages;    /* [n_seqs][max_pages]: key j lies on page pages[s][j / page_size]; an id outside
+                              [0, n_pages) is no page: its keys are neither written nor seen */
+  const int64_t* tree;     /* nullable [rows]: bit j of a row says that row j of its sequence lies on its path (its own
+                              bit included; a parent before its children; at most 64 rows a sequence).
+                              The row then stands at position ctx + (bits set) - 1.  NULL: chains, row i at
+                              position ctx + i */
+  int64_t pages_stride;    /* elements from one sequence's pages to the next one's */
+  int32_t n_seqs;          /* at most 4096 */
+  int32_t max_pages;       /* max_pages * page_size at most 2^29 */
+} hvd_row_batch;
+
+/* A paged cache of one layer: keys and values [n_pages][n_heads][page_size][head_dim]
+ * of dtype HVD_F16 or HVD_BF16, the four dimensions at any strides that do not
+ * overlap (elements, multiples of 8, token strides at most 2^28; head_dim itself
+ * contiguous), 16-byte aligned.  page_size is a power of two from 16 to 1024,
+ * head_dim a multiple of 8 from 8 to 256, n_heads at most 256. */
+typedef struct {
+  void* k;
+  int64_t k_page_stride, k_head_stride, k_token_stride;
+  void* v;
+  int64_t v_page_stride, v_head_stride, v_token_stride;
+  int32_t n_pages, n_heads, page_size, head_dim, dtype;
+} hvd_paged_kv;
+
+/* Writes the rows' keys and values to their places in the cache, keys (and
+ * queries) rotated: with the angle t = position * freqs[j], pair j of the first
+ * `rot` columns of a head becomes (a cos t - b sin t, b cos t + a sin t); pairs
+ * are columns (j, j + rot / 2), or (2j, 2j + 1) if interleaved.  Angles are
+ * 64-bit, the rotation 32-bit, and each output is rounded once to the cache's
+ * type.  The other columns, and values, are rounded alone.  q_out
+ * [rows][q_heads][head_dim], contiguous, of the cache's type, receives the
+ * queries (0 for rows of no sequence). */
+typedef struct {
+  const void* k;           /* [rows][n_heads][head_dim] at any strides, head_dim contiguous; type `dtype` */
+  int64_t k_row_stride, k_head_stride;
+  const void* v;
+  int64_t v_row_stride, v_head_stride;
+  const void* q;           /* nullable [rows][q_heads][head_dim] */
+  int64_t q_row_stride, q_head_stride;
+  void* q_out;             /* 16-byte aligned; NULL with q NULL */
+  const double* freqs;     /* [rot / 2] radians per position; NULL with rot = 0 */
+  const int32_t* positions; /* nullable [rows]: in place of the batch's positions */
+  int32_t q_heads, rot, interleaved, dtype; /* rot even, at most head_dim; dtype HVD_F16, HVD_BF16 or HVD_F32 */
+} hvd_append_args;
+hvd_status hvd_append_kv(const hvd_row_batch* batch, const hvd_paged_kv* kv, const hvd_append_args* args, int32_t rows,
+                         void* stream);
+
+/* Attention of the rows over the cache, their own keys included (appended
+ * before).  q_heads is a multiple of n_heads: query head h reads key head
+ * h / (q_heads / n_heads).  A row at position p sees the key at position j if
+ *     (j <= p or j < prefix of its sequence),  p - j < window,  key >= first of the row;
+ * with a tree, of this step's keys the row sees those on its path, at the
+ * positions of their depth, whatever the prefix.  With
+ *     x = scale * q.k,  x = cap * tanh(x / cap),  x = x - slopes[h] * |p - j|
+ * out = sum exp(x) v / sum exp(x), 0 for a row that sees no key (or whose scores
+ * are all -inf) and for rows of no sequence.  What a key or value holds that a
+ * row does not see does not reach it, infinities and NaNs included.  q and out
+ * have the cache's type; scores, sums and outputs are 32-bit, weights are
+ * rounded to the cache's type for the product with the values. */
+typedef struct {
+  const void* q;           /* [rows][q_heads][head_dim], strides multiples of 8, 16-byte aligned */
+  int64_t q_row_stride, q_head_stride;
+  void* out;               /* the same; may be q itself */
+  int64_t out_row_stride, out_head_stride;
+  const float* slopes;     /* nullable [q_heads] */
+  const int32_t* first;    /* nullable [rows]: keys before it belong to another document */
+  const int32_t* prefix;   /* nullable [n_seqs]: keys that all rows of the sequence see */
+  float scale;
+  float cap;               /* 0: none */
+  int32_t q_heads;
+  int32_t window;          /* 0: none */
+} hvd_attend_args;
+/* Workspace bytes of a call with these sizes (0 for ones it would refuse).  The
+ * workspace belongs to the call until it is done: calls that may overlap, and
+ * graphs that may run at once, need one each. */
+size_t hvd_attend_workspace(const hvd_row_batch* batch, const hvd_paged_kv* kv, int32_t q_heads, int32_t rows);
+hvd_status hvd_attend(const hvd_row_batch* batch, const hvd_paged_kv* kv, const hvd_attend_args* args, int32_t rows,
+                      void* work, size_t work_bytes, void* stream);
+
+/* Penalties, biases and a mask on the rows' logits, and each row's best token.
+ * Of a batch, starts, n_seqs and tree are read.  For token v let n be how often
+ * it was generated: in the sequence's history from prompt_lengths on, and in
+ * `tokens` on the row's own path (rows up to itself, or its tree mask's); it was
+ * seen if n > 0 or the history has it at all.  Then, each step rounded to 32 bits:
+ *     x = seen ? (x > 0 ? x / repetition : x * repetition) : x
+ *     x = x - frequency * n,  x = x - presence (if n > 0),  x = x + bias(v)
+ *     x = allowed(v) ? x : -inf
+ * out receives x rounded to the logits' type; best the lowest token with the
+ * largest x (before that rounding), -1 where every x is -inf or NaN.  Rows of no
+ * sequence are copied and have best -1.  Tokens outside [0, vocab) count to
+ * nothing. */
+typedef struct {
+  const void* logits;      /* [rows][vocab], unit column stride, aligned to its elements; type `dtype` */
+  int64_t logits_stride;
+  void* out;               /* nullable; may be logits itself (with its stride) */
+  int64_t out_stride;
+  int32_t* best;           /* nullable [rows]; out or best is wanted */
+  const int32_t* tokens;   /* nullable [rows] */
+  const int32_t* history;  /* nullable [n_seqs][max_history] */
+  int64_t history_stride;
+  const int32_t* history_lengths; /* [n_seqs]; with history */
+  const int32_t* prompt_lengths;  /* nullable [n_seqs] (all generated) */
+  const float* repetition; /* nullable [n_seqs], and so the next two */
+  const float* frequency;
+  const float* presence;
+  const int32_t* bias_ids; /* nullable [n_seqs][n_bias]; an id that comes twice has its last bias */
+  int64_t bias_ids_stride;
+  const float* bias;       /* [n_seqs][n_bias] */
+  int64_t bias_stride;
+  const int32_t* allowed;  /* nullable [rows][(vocab + 31) / 32]: bit v % 32 of word v / 32 */
+  int64_t allowed_stride;  /* 0: one mask for all rows */
+  int32_t vocab;           /* at most 2^24 */
+  int32_t max_history;     /* at most 983039 */
+  int32_t n_bias;          /* at most 2046 */
+  int32_t dtype;
+} hvd_adjust_args;
+size_t hvd_adjust_workspace(const hvd_row_batch* batch, const hvd_adjust_args* args, int32_t rows);
+hvd_status hvd_adjust_logits(const hvd_row_batch* batch, const hvd_adjust_args* args, int32_t rows, void* work,
+                             size_t work_bytes, void* stream);
+
 /* Decoders with expert layers.  Layers first_layer .. n_layers - 1 have
  * route.n_experts SwiGLU experts of ffn_dim (% 32 == 0) each in place of the
  * dense MLP: with h the normalised MLP input,

@@ -19,3 +19,9 @@ from .operators import (  # noqa: F401
     block_norm,
     route,
 )
+from .rows import (  # noqa: F401
+    RowBatch,
+    adjust_logits,
+    append_kv,
+    attend,
+)

@@ -23,8 +23,8 @@ DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 COMMON = ["-O3", "-std=c++17", "-fPIC", f"-I{INCLUDE}", "-Wall", "-Wno-unused-function"]
 
 HIP_SOURCES = ["gemm_mid.hip", "gemm.hip", "gemm_tiled.hip", "attn.hip", "attn_o.hip", "misc.hip", "scratch.hip", "flow.hip", "peak.hip",
-               "route.hip", "block_norm.hip", "experts.hip"]
-HOST_SOURCES = ["api.cpp", "operators.cpp", "host_state.cpp"]
+               "route.hip", "block_norm.hip", "experts.hip", "append_kv.hip", "attend.hip", "adjust_logits.hip"]
+HOST_SOURCES = ["api.cpp", "operators.cpp", "row_operators.cpp", "host_state.cpp"]
 
 
 def _run(cmd):

@@ -1,0 +1,878 @@
+// Attention of a step's rows over a paged cache (gfx950).
+//
+// A row r of sequence s at position p sees a key at position j of the cache if
+//   j < len(s),  (j <= p or j < prefix(s)),  p - j < window,  j >= first(r),
+// and with a tree mask, of the keys that this step appended (from ctx on),
+// those of its mask's bits, which stand at the positions of their depth.  With
+//   x = scale * q.k,  x = cap * tanh(x / cap),  x = x - slope(h) * |p - j|
+// the row's output is sum_j exp(x_j) v_j / sum_j exp(x_j), 0 where it sees none.
+//
+// Scores, their maximum, sums and outputs are 32-bit; the weights are rounded to
+// the cache's type for the product with V (an fp16 weight is scaled by 2^7, so
+// that weights down to 2^-21 of the largest keep all its bits), not for the sum.
+//
+// The G query heads of a key head and the rows of a sequence are one list of
+// columns, column m = row m / G, head m % G: the products are transposed,
+//   S^T = K Q^T (keys x columns),  O^T = V^T P^T (head dim x columns),
+// so that a lane holds one column: its maximum, sum and rescaling need no other
+// lane but the one 32 away, and S^T's accumulators are, rounded, P^T's operand
+// as they lie (a 32x32 accumulator's lane has keys 8i + 4h + 0..3; V's operand
+// takes its keys in that order, by LDS reads that transpose).
+//
+// K and V go from the cache to LDS without registers (global_load_lds), in
+// tiles whose 16-byte pieces are XOR-swizzled by key for both kinds of read.
+#include "common.h"
+#include "kernels.h"
+#include "rows.h"
+
+#include <algorithm>
+#include <atomic>
+
+namespace hvd {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLazy = 8.f;     // the running maximum may lag by this (base 2)
+constexpr int kNoKey = 0x7fffffff;
+
+template <bool BF16>
+struct Half;
+template <>
+struct Half<false> {
+  static constexpr float kShift = 7.f;
+  static constexpr uint32_t kInf = 0x04000400u;  // 0x8000 - the exponent of infinities and NaNs
+  __device__ static f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+  __device__ static uint16_t bits(float v) { return f2h(v); }
+  __device__ static float value(uint16_t b) { return h2f(b); }
+};
+template <>
+struct Half<true> {
+  static constexpr float kShift = 0.f;
+  static constexpr uint32_t kInf = 0x00800080u;
+  __device__ static f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+  __device__ static uint16_t bits(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
+  __device__ static float value(uint16_t b) { return bf2f(b); }
+};
+
+// A value of the lane 32 away.
+__device__ __forceinline__ float other_half_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float other_half_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// How the work is cut: columns per tile; `target` items wanted, or 0: a tile's
+// keys are not split.
+struct Cut {
+  int cols, target, min_chunk;
+};
+
+// One item: columns [col0, col0 + cols) of sequence s over the keys of split
+// `split` of its tile.
+struct Item {
+  int s, row0, n, len, tile, split, splits, chunk, first_item;
+};
+
+// How many keys a tile of sequence s may see at most, and its tiles.
+__device__ __forceinline__ void seq_load(const AttendArgs& a, const Cut& c, int s, int& row0, int& n, int& len, int& tiles,
+                                         int& range) {
+  row0 = n = len = tiles = range = 0;
+  if (s > a.b.S) return;
+  int e;
+  seq_rows(a.b, s, row0, e);
+  n = e - row0;
+  if (s < a.b.S) len = min(max(a.b.lengths[s], 0), a.b.P << a.page_shift);
+  tiles = (int)(((int64_t)n * (a.Hq / a.H) + c.cols - 1) / c.cols);
+  range = len;
+  if (a.window > 0 && !a.prefix && !a.b.tree) range = min(len, a.window + min(n, a.b.T));
+  if (range < 0) range = len;
+}
+
+// The keys of one split: the same in every workgroup.
+__device__ __forceinline__ int chunk_of(const AttendArgs& a, const Cut& c) {
+  if (c.target == 0) return 1 << 30;
+  const int lane = threadIdx.x & 63;
+  float total = 0.f;
+  for (int s = 0; s <= a.b.S; s += 64) {
+    int row0, n, len, tiles, range;
+    seq_load(a, c, s + lane, row0, n, len, tiles, range);
+    total += (float)tiles * (float)range;
+  }
+  total = wave_sum(total) * (float)a.H;
+  int k = (int)fminf(total / (float)c.target, 1.0e9f);
+  k = (k + 127) & ~63;
+  return __builtin_amdgcn_readfirstlane(max(k, c.min_chunk));
+}
+
+__device__ __forceinline__ int splits_of(int range, int chunk) { return max(1, (int)(((int64_t)range + 63 + chunk - 1) / chunk)); }
+
+// Item number `idx`; false past the last one.
+__device__ __forceinline__ bool find_item(const AttendArgs& a, const Cut& c, int idx, Item& it) {
+  const int lane = threadIdx.x & 63;
+  it.chunk = chunk_of(a, c);
+  int base = 0;
+  for (int s = 0; s <= a.b.S; s += 64) {
+    int row0, n, len, tiles, range;
+    seq_load(a, c, s + lane, row0, n, len, tiles, range);
+    const int splits = splits_of(range, it.chunk), mine = tiles * splits;
+    const int upto = wave_scan(mine);
+    const uint64_t past = __builtin_amdgcn_ballot_w64(base + upto > idx);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      it.s = s + l;
+      it.row0 = __builtin_amdgcn_readlane(row0, l);
+      it.n = __builtin_amdgcn_readlane(n, l);
+      it.len = __builtin_amdgcn_readlane(len, l);
+      it.splits = __builtin_amdgcn_readlane(splits, l);
+      const int at = idx - base - __builtin_amdgcn_readlane(upto - mine, l);
+      // the last tiles of a sequence see the most keys: they go first
+      const int t = at / it.splits;
+      it.tile = __builtin_amdgcn_readlane(tiles, l) - 1 - t;
+      it.split = at - t * it.splits;
+      it.first_item = idx - it.split;
+      return true;
+    }
+    base += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
+
+// What a column sees: keys [lo, hi), and of the keys from ctx on (tree only)
+// those of `see`.
+struct Column {
+  int row, head;  // row of the batch (-1: none)
+  int pos, lo, hi, ctx;
+  uint64_t path;  // the tree mask
+  uint64_t see;   // its bits that window, first and len leave
+};
+__device__ __forceinline__ Column column_of(const AttendArgs& a, const Item& it, int m, int head0) {
+  Column c;
+  const int G = a.Hq / a.H;
+  const int i = m / G;
+  const bool on = i < it.n, in_seq = it.s < a.b.S;
+  c.row = on ? it.row0 + i : -1;
+  c.head = head0 + (m - i * G);
+  c.ctx = (in_seq ? a.b.lengths[it.s] : 0) - it.n;
+  c.path = c.see = 0;
+  c.pos = c.ctx + i;
+  const int first = on && a.first ? max(a.first[c.row], 0) : 0;
+  if (a.b.tree) {
+    if (on && in_seq) c.path = (uint64_t)a.b.tree[c.row];
+    const int depth = __builtin_popcountll(c.path);
+    c.pos = c.ctx + depth - 1;
+    c.see = c.path;
+    if (a.window > 0)
+      for (int drop = depth - a.window; drop > 0; --drop) c.see &= c.see - 1;  // positions rise with the bits
+    const int64_t from = max((int64_t)first - c.ctx, (int64_t)-c.ctx), to = (int64_t)it.len - c.ctx;
+    if (from > 0) c.see = from < 64 ? c.see >> from << from : 0;
+    if (to < 64) c.see = to > 0 ? c.see & ((1ull << to) - 1) : 0;
+  }
+  c.lo = first;
+  if (a.window > 0) c.lo = max(c.lo, c.pos - a.window + 1);
+  c.hi = c.pos + 1;
+  if (a.b.tree) c.hi = c.ctx;
+  else if (a.prefix && in_seq) c.hi = max(c.hi, a.prefix[it.s]);
+  c.hi = min(c.hi, it.len);
+  if (!on || !in_seq || c.hi <= c.lo) c.hi = c.lo = 0;
+  if (!on || !in_seq) c.see = 0;
+  return c;
+}
+
+template <int CTRL>
+__device__ __forceinline__ int dpp(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, false);
+}
+// f over all lanes of a wave (one that does not mind a value twice)
+template <class F>
+__device__ __forceinline__ int wave_all(int v, F f) {
+  v = f(v, dpp<0xB1>(v));
+  v = f(v, dpp<0x4E>(v));
+  v = f(v, dpp<0x141>(v));
+  v = f(v, dpp<0x140>(v));
+  const auto x = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+  v = f((int)x[0], (int)x[1]);
+  const auto y = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+  return __builtin_amdgcn_readfirstlane(f((int)y[0], (int)y[1]));
+}
+
+// The keys that some column of a wave sees lie in [lo, hi); all columns (that
+// exist) see all keys of [all_lo, all_hi).
+struct Span {
+  int lo, hi, all_lo, all_hi;
+};
+__device__ __forceinline__ Span span_of(const AttendArgs& a, const Column& c) {
+  const auto least = [](int x, int y) { return x < y ? x : y; };
+  const auto most = [](int x, int y) { return x > y ? x : y; };
+  int lo = c.hi > c.lo ? c.lo : kNoKey, hi = c.hi;
+  if (c.see) {
+    lo = min(lo, c.ctx + __builtin_ctzll(c.see));
+    hi = max(hi, c.ctx + 64 - __builtin_clzll(c.see));
+  }
+  Span s;
+  s.lo = wave_all(lo, least);
+  s.hi = wave_all(hi, most);
+  s.all_lo = wave_all(c.row >= 0 ? c.lo : 0, most);
+  s.all_hi = wave_all(c.row >= 0 ? c.hi : kNoKey, least);
+  return s;
+}
+
+template <int DHP>
+struct Geo {
+  static constexpr int CH = DHP / 8;   // 16-byte pieces of a key
+  static constexpr int KPI = 64 / CH;  // keys of one copy instruction
+  static constexpr int ROW = DHP * 2;  // bytes of a key
+  // Piece c of key k lies at piece c ^ swz(k): four successive keys (a transposing
+  // read takes 64 bytes of each) and sixteen keys (a row read takes one piece
+  // of each) fall on different banks; with 8 pieces two keys share 256 bytes.
+  __device__ static constexpr int swz(int k) {
+    return CH == 8 ? ((k >> 1 & 1) << 2) | (k >> 2 & 3) : ((k & 3) << 2) | (k >> 2 & 3);
+  }
+};
+
+// The cache pages of 64 groups of 16 keys, one per lane: group l starts at key
+// `key` of lane l.  -1: past `end`, or not a page of the cache.
+__device__ __forceinline__ int page_ids(const AttendArgs& a, const int32_t* table, int key, int end) {
+  const int pi = key >> a.page_shift;
+  int p = key < end && pi < a.b.P ? table[pi] : -1;
+  return (unsigned)p < (unsigned)a.n_pages ? p : -1;
+}
+
+// Which of a tile's NK keys have a page: group g0 is the tile's first.
+template <int NK>
+__device__ __forceinline__ uint64_t good_keys(int ids, int g0, int key0, int end) {
+  uint64_t good = 0;
+#pragma unroll
+  for (int g = 0; g < NK / 16; ++g)
+    if (__builtin_amdgcn_readlane(ids, g0 + g) >= 0) good |= 0xffffull << (16 * g);
+  const int n = end - key0;
+  if (n < NK) good &= n > 0 ? (1ull << n) - 1 : 0;
+  return good;
+}
+
+// Copies of keys [k0, k0 + N * KPI) of a tile to LDS, K and V.  Returns false if
+// fewer than 2 N copies were asked for.
+template <int DHP, int N>
+__device__ __forceinline__ bool stage(const AttendArgs& a, const uint16_t* kb, const uint16_t* vb, int key0, int k0, int ids, int g0,
+                                      uint64_t good, unsigned char* lk, unsigned char* lv) {
+  using G = Geo<DHP>;
+  const int lane = threadIdx.x & 63;
+  const int kk = lane / G::CH, piece = lane % G::CH;
+  const int in_page = (1 << a.page_shift) - 1;
+  constexpr uint64_t kMine = N * G::KPI >= 64 ? ~0ull : (1ull << (N * G::KPI & 63)) - 1;
+  const bool whole = (good >> k0 & kMine) == kMine && a.D == DHP;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int kf = k0 + i * G::KPI;  // wave-uniform
+    const int64_t p = __builtin_amdgcn_readlane(ids, g0 + (kf >> 4));
+    const int k = kf + kk;
+    const int c = piece ^ G::swz(k);
+    const int64_t tok = (key0 + kf) & in_page;
+    // (a wave-uniform address and 32 bits of each lane's own)
+    const char* kp = (const char*)(kb + (p * a.k.page + tok * a.k.tok)) + (uint32_t)(kk * (int)a.k.tok + c * 8) * 2u;
+    const char* vp = (const char*)(vb + (p * a.v.page + tok * a.v.tok)) + (uint32_t)(kk * (int)a.v.tok + c * 8) * 2u;
+    unsigned char *dk = lk + kf * G::ROW, *dv = lv + kf * G::ROW;
+    if (whole) {
+      __builtin_amdgcn_global_load_lds((const void*)kp, (lds_void*)dk, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((const void*)vp, (lds_void*)dv, 16, 0, 0);
+    } else {
+      // pieces past the head dimension stay zero, keys without a page become it
+      const bool in = c * 8 < a.D, ok = good >> k & 1;
+      if (in && ok) {
+        __builtin_amdgcn_global_load_lds((const void*)kp, (lds_void*)dk, 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((const void*)vp, (lds_void*)dv, 16, 0, 0);
+      }
+      if (in && !ok) {
+        *(uint4*)(dk + lane * 16) = uint4{0, 0, 0, 0};
+        *(uint4*)(dv + lane * 16) = uint4{0, 0, 0, 0};
+      }
+    }
+  }
+  if (!whole) __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the zeros are there before the barrier
+  return whole;
+}
+
+// The lowest n bits (none for n <= 0, all for n >= 64).
+__device__ __forceinline__ uint64_t below(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
+
+__device__ __forceinline__ s16x8 join4(s16x4 x, s16x4 y) {
+  return s16x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+}
+
+// The state of a wave's 32 columns; NB blocks of 32 keys per step.
+template <int DHP, bool BF16, int NB>
+struct Wave {
+  using G = Geo<DHP>;
+  using H = Half<BF16>;
+  s16x8 q[DHP / 16];
+  f32x16 o[DHP / 32];
+  float m, l;   // of the scores times `c`; l of this lane's half of the keys
+  float c;      // the scores' factor to base-2 exponents
+  bool turned;  // the scores are made exponents one by one
+
+  __device__ __forceinline__ void init(const AttendArgs& a, const Column& col, int h) {
+    m = -INFINITY;
+    l = 0.f;
+    turned = a.cap > 0.f || a.slopes || !(a.scale > 0.f);
+    c = turned ? 1.f : a.scale * kLog2e;
+#pragma unroll
+    for (int d = 0; d < DHP / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+    const uint16_t* src = (const uint16_t*)a.q + (int64_t)max(col.row, 0) * a.q_row + (col.row >= 0 ? col.head : 0) * a.q_head;
+#pragma unroll
+    for (int s = 0; s < DHP / 16; ++s) {
+      const int d = s * 16 + h * 8;
+      q[s] = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+      if (col.row >= 0 && d < a.D) q[s] = *(const s16x8*)(src + d);
+    }
+  }
+
+  // One tile: keys key0 .. key0 + 32 NB - 1.  masked: some column does not see some
+  // key of it.
+  __device__ __forceinline__ void step(const AttendArgs& a, const Column& col, const unsigned char* lk, const unsigned char* lv,
+                                       int key0, uint64_t good, bool masked, float slope) {
+    const int lane = threadIdx.x & 63, h = lane >> 5, r = lane & 31;
+    f32x16 s[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+    // (piece 2t + h of key 32b + r: the key's swizzle does not depend on b, nor its low bit on t)
+    const unsigned char* kr = lk + r * G::ROW;
+    const int kx = (h ^ G::swz(r)) * 16;
+#pragma unroll
+    for (int t = 0; t < DHP / 16; ++t)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+        s[b] = H::mfma(*(const s16x8*)(kr + (kx ^ (32 * t)) + 32 * b * G::ROW), q[t], s[b]);
+    if (turned) {
+      const float f = a.scale * kLog2e, cl = a.cap * kLog2e, inv = a.cap > 0.f ? a.scale / a.cap : 0.f;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float x = s[b][i] * f;
+          if (a.cap > 0.f) {
+            // tanh y = 1 - 2 / (exp 2y + 1); near 0, where that cancels, its series
+            const float y = s[b][i] * inv, y2 = y * y;
+            const float far = 1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * (2.f * kLog2e)) + 1.f);
+            const float near = y * (1.f + y2 * (-1.f / 3.f + y2 * (2.f / 15.f - y2 * (17.f / 315.f))));
+            x = cl * (fabsf(y) < 0.25f ? near : far);
+          }
+          s[b][i] = x;
+        }
+      if (a.slopes) {
+        const float apart = (float)(col.pos - key0 - 4 * h);
+        if (a.b.tree && key0 + 32 * NB > col.ctx) {  // this step's keys stand at the positions of their depth
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int k = 32 * b + 8 * (i >> 2) + (i & 3), j = key0 + 4 * h + k - col.ctx;
+              const int d = col.pos - col.ctx - __builtin_popcountll(col.path & below(j));
+              s[b][i] -= slope * fabsf(j >= 0 ? (float)d : apart - (float)k);
+            }
+        } else {
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[b][i] -= slope * fabsf(apart - (float)(32 * b + 8 * (i >> 2) + (i & 3)));
+        }
+      }
+    }
+    if (masked) {
+      // bit k: key k of the tile is seen
+      uint64_t see = below(col.hi - key0) & ~below(col.lo - key0);
+      if (a.b.tree) {
+        const int from = key0 - col.ctx;
+        see |= from >= 64 || from <= -64 ? 0 : from >= 0 ? col.see >> from : col.see << -from;
+      }
+      see = (see & good) >> (4 * h);
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          s[b][i] = ((uint32_t)(see >> (32 * b)) & 1u << (8 * (i >> 2) + (i & 3))) ? s[b][i] : -INFINITY;
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+    top = other_half_max(top);
+    // The maximum lags until a weight would pass 2^kLazy: most tiles rescale nothing
+    if (__builtin_amdgcn_ballot_w64(top * c > m * c + kLazy || (m == -INFINITY && top > -INFINITY))) {
+      const float mn = fmaxf(m, top);
+      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * c);
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < DHP / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] *= f;
+      m = mn;
+    }
+    const float mc = (m == -INFINITY ? 0.f : m * c) - H::kShift;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], c, -mc));
+        l += s[b][i];
+      }
+    s16x8 p[2 * NB];
+#pragma unroll
+    for (int t = 0; t < 2 * NB; ++t)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) p[t][j] = (short)H::bits(s[t >> 1][8 * (t & 1) + j]);
+    if (masked && values_not_finite(lv)) {
+      add_not_finite(lv, p, h);
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2 * NB; ++t)
+#pragma unroll
+        for (int d = 0; d < DHP / 32; ++d) o[d] = H::mfma(read_v8(lv, t, h, d), p[t], o[d]);
+    }
+  }
+
+  // V's operand of 32 dimensions (from 32 d) for the 16 keys of P's operand t: keys
+  // 16t + 4h .. + 3 and the four 8 further on.  Sixteen lanes read four keys' 16
+  // dimensions, and each gets one dimension's four keys.  (The keys' swizzle
+  // does not depend on t.)
+  __device__ __forceinline__ s16x8 read_v8(const unsigned char* lv, int t, int h, int d) {
+    const int lane = threadIdx.x & 63;
+    const int key = 4 * h + (lane >> 2 & 3), dim = (lane & 16) + (lane & 3) * 4;
+    const unsigned char* p = lv + key * G::ROW + (dim & 7) * 2 + 16 * t * G::ROW;
+    const int x = ((dim >> 3) ^ G::swz(key)) * 16, y = ((dim >> 3) ^ G::swz(key + 8)) * 16;
+    return join4(__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (x ^ (64 * d)))),
+                 __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (y ^ (64 * d)) + 8 * G::ROW)));
+  }
+
+  // A value that a column does not see must not reach it, and 0 times an infinity
+  // or a NaN would.  In a tile with hidden keys and such values these are taken
+  // out of V and counted, by weight, where they are; a dimension's count makes
+  // it infinite, both signs' (a NaN is both) a NaN.
+  __device__ __forceinline__ bool values_not_finite(const unsigned char* lv) {
+    const int lane = threadIdx.x & 63;
+    uint32_t bad = 0;
+#pragma unroll
+    for (int i = 0; i < 32 * NB / G::KPI; ++i) {
+      const uint4 v = *(const uint4*)(lv + (i * 64 + lane) * 16);
+      bad |= ((v.x & 0x7fff7fffu) + H::kInf) | ((v.y & 0x7fff7fffu) + H::kInf) | ((v.z & 0x7fff7fffu) + H::kInf) |
+             ((v.w & 0x7fff7fffu) + H::kInf);
+    }
+    return __builtin_amdgcn_ballot_w64(bad & 0x80008000u) != 0;
+  }
+  __device__ __forceinline__ void add_not_finite(const unsigned char* lv, const s16x8 (&p)[2 * NB], int h) {
+#pragma unroll
+    for (int d = 0; d < DHP / 32; ++d) {
+#pragma unroll
+      for (int sign = 0; sign < 2; ++sign) {
+        f32x16 there;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) there[i] = 0.f;
+#pragma unroll
+        for (int t = 0; t < 2 * NB; ++t) {
+          __builtin_amdgcn_sched_barrier(0);  // one operand at a time: this path may not cost the other one registers
+          const u32x4 v = __builtin_bit_cast(u32x4, read_v8(lv, t, h, d));
+          u32x4 finite, u;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t mag = (v[j] & 0x7fff7fffu) + H::kInf;  // bit 15 of a half: not finite
+            const uint32_t not_finite = mag & 0x80008000u, nan = (mag - 0x00010001u) & 0x80008000u;
+            finite[j] = v[j] & ~(not_finite | (not_finite - (not_finite >> 15)));
+            u[j] = (nan | (not_finite & (sign ? v[j] : ~v[j]))) >> 1;  // 2 in either type
+          }
+          if (sign == 0) o[d] = H::mfma(__builtin_bit_cast(s16x8, finite), p[t], o[d]);
+          there = H::mfma(__builtin_bit_cast(s16x8, u), p[t], there);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] += there[i] > 0.f ? (sign ? -INFINITY : INFINITY) : 0.f;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+};
+
+// Four successive dimensions of a row's result.
+template <bool BF16>
+__device__ __forceinline__ void store_out(const AttendArgs& a, int row, int head, int dim, float x, float y, float z, float w) {
+  if (dim >= a.D) return;
+  using H = Half<BF16>;
+  uint16_t* p = (uint16_t*)a.out + (int64_t)row * a.out_row + head * a.out_head + dim;
+  *(uint2*)p = uint2{(uint32_t)H::bits(x) | (uint32_t)H::bits(y) << 16, (uint32_t)H::bits(z) | (uint32_t)H::bits(w) << 16};
+}
+
+// Partial results of an item (a.part): [blocks][cols][DHP] sums, [blocks][cols][2]
+// maxima (base 2) and weights' sums, [blocks] how many splits of the tile are live.
+struct Part {
+  float *o, *ml;
+  int* live;
+};
+__device__ __forceinline__ Part part_of(const AttendArgs& a, int blocks, int cols, int dhp) {
+  Part p;
+  p.o = a.part;
+  p.ml = a.part + (size_t)blocks * cols * dhp;
+  p.live = (int*)(p.ml + (size_t)blocks * cols * 2);
+  return p;
+}
+
+// This block's item cut down to the keys [k0, k1) it is to look at; false: none.
+__device__ __forceinline__ bool cut_keys(const AttendArgs& a, const Item& it, const Part& part, int lo, int hi, int& k0, int& k1,
+                                         bool& alone) {
+  const int base = lo == kNoKey ? 0 : lo & ~63;
+  hi = max(hi, base);
+  const int live = (int)(((int64_t)hi - base + it.chunk - 1) / it.chunk);
+  if (it.split > 0 && it.split >= live) return false;
+  alone = live <= 1;
+  if (it.splits > 1 && it.split == 0 && threadIdx.x == 0) part.live[blockIdx.x] = live;
+  k0 = base + it.split * it.chunk;
+  k1 = (int)min((int64_t)hi, (int64_t)k0 + it.chunk);
+  return true;
+}
+
+// Many columns: four waves of 32 share the tiles of 64 keys (32 where a key is 256
+// wide: registers), one being copied while one is worked on.
+constexpr int kWideCols = 128;
+template <int DHP>
+constexpr int wide_blocks() { return DHP == 256 ? 1 : 2; }
+template <int DHP>
+constexpr int wide_lds() { return 2 * 2 * 32 * wide_blocks<DHP>() * DHP * 2; }
+
+template <int DHP, bool BF16>
+__global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArgs a, Cut cut, int blocks) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ int red[4][2];
+  using G = Geo<DHP>;
+  constexpr int NB = wide_blocks<DHP>(), KT = 32 * NB, TILE = KT * G::ROW;
+  constexpr uint64_t kAll = KT == 64 ? ~0ull : 0xffffffffull;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int idx = blockIdx.x / a.H, kvh = blockIdx.x - idx * a.H;
+  Item it;
+  if (!find_item(a, cut, idx, it)) return;
+  const int m = it.tile * kWideCols + wave * 32 + (lane & 31);
+  const Column col = column_of(a, it, m, kvh * (a.Hq / a.H));
+  const Span sp = span_of(a, col);
+  if (lane == 0) {
+    red[wave][0] = sp.lo;
+    red[wave][1] = sp.hi;
+  }
+  __syncthreads();
+  const int lo = min(min(red[0][0], red[1][0]), min(red[2][0], red[3][0]));
+  const int hi = max(max(red[0][1], red[1][1]), max(red[2][1], red[3][1]));
+  const Part part = part_of(a, blocks, kWideCols, DHP);
+  int k0, k1;
+  bool alone;
+  if (!cut_keys(a, it, part, lo, hi, k0, k1, alone)) return;
+  Wave<DHP, BF16, NB> w;
+  w.init(a, col, lane >> 5);
+  const float slope = a.slopes && col.row >= 0 ? a.slopes[col.head] * kLog2e : 0.f;
+  if (k0 < k1) {
+    if (a.D < DHP) {
+      for (int i = tid; i < 4 * TILE / 16; i += 256) ((uint4*)smem)[i] = uint4{0, 0, 0, 0};
+      __syncthreads();
+    }
+    const uint16_t* kb = (const uint16_t*)a.k.p + kvh * a.k.head;
+    const uint16_t* vb = (const uint16_t*)a.v.p + kvh * a.v.head;
+    const int32_t* table = a.b.pages + (it.s < a.b.S ? it.s : 0) * a.b.pages_stride;
+    const int end = min(hi, it.len);
+    constexpr int N = KT / G::KPI / 4;
+    const int mine = wave * N * G::KPI;
+    int ids = page_ids(a, table, k0 + lane * 16, end);
+    uint64_t good = good_keys<KT>(ids, 0, k0, end), next_good = 0;
+    stage<DHP, N>(a, kb, vb, k0, mine, ids, 0, good, smem, smem + TILE);
+    for (int key = k0, t = 0; key < k1; key += KT, ++t) {
+      vm_wait<0>();
+      block_barrier();
+      unsigned char* now = smem + (t & 1) * 2 * TILE;
+      if (key + KT < k1) {
+        const int g = (t + 1) * (KT / 16) & 63;
+        if (g == 0) ids = page_ids(a, table, key + KT + lane * 16, end);
+        next_good = good_keys<KT>(ids, g, key + KT, end);
+        unsigned char* next = smem + ((t + 1) & 1) * 2 * TILE;
+        stage<DHP, N>(a, kb, vb, key + KT, mine, ids, g, next_good, next, next + TILE);
+      }
+      if (key < sp.hi && key + KT > sp.lo)
+        w.step(a, col, now, now + TILE, key, good, key < sp.all_lo || key + KT > sp.all_hi || good != kAll, slope);
+      good = next_good;
+    }
+  }
+  if (col.row < 0) return;
+  const float l = other_half_sum(w.l), mb = w.m == -INFINITY ? -INFINITY : w.m * w.c;
+  const int h = lane >> 5;
+  if (alone) {
+    const float f = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int d = 0; d < DHP / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        store_out<BF16>(a, col.row, col.head, 32 * d + 2 * i + 4 * h, w.o[d][i] * f, w.o[d][i + 1] * f, w.o[d][i + 2] * f,
+                        w.o[d][i + 3] * f);
+  } else {
+    const size_t at = (size_t)blockIdx.x * kWideCols + wave * 32 + (lane & 31);
+#pragma unroll
+    for (int d = 0; d < DHP / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *(float4*)(part.o + at * DHP + 32 * d + 2 * i + 4 * h) = float4{w.o[d][i], w.o[d][i + 1], w.o[d][i + 2], w.o[d][i + 3]};
+    if (h == 0) *(float2*)(part.ml + at * 2) = float2{mb, l};
+  }
+}
+
+// Few columns: the waves of a workgroup hold the same 32 columns and take the
+// tiles of 32 keys by turns, each with tiles of its own in LDS and no barrier;
+// their results are joined through LDS at the end.
+constexpr int kFewCols = 32;
+template <int DHP>
+constexpr int few_waves() { return DHP == 256 ? 2 : 4; }
+template <int DHP>
+constexpr int few_lds() { return few_waves<DHP>() * 2 * 2 * 32 * DHP * 2; }
+
+template <int DHP, bool BF16>
+__global__ __launch_bounds__(64 * few_waves<DHP>()) void attend_few(AttendArgs a, Cut cut, int blocks) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  constexpr int NW = few_waves<DHP>();
+  __shared__ float stat[NW][32][2];
+  using G = Geo<DHP>;
+  constexpr int TILE = 32 * G::ROW;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int idx = blockIdx.x / a.H, kvh = blockIdx.x - idx * a.H;
+  Item it;
+  if (!find_item(a, cut, idx, it)) return;
+  const Column col = column_of(a, it, it.tile * kFewCols + (lane & 31), kvh * (a.Hq / a.H));
+  const Span sp = span_of(a, col);
+  const Part part = part_of(a, blocks, kFewCols, DHP);
+  int k0, k1;
+  bool alone;
+  if (!cut_keys(a, it, part, sp.lo, sp.hi, k0, k1, alone)) return;
+  Wave<DHP, BF16, 1> w;
+  w.init(a, col, lane >> 5);
+  const float slope = a.slopes && col.row >= 0 ? a.slopes[col.head] * kLog2e : 0.f;
+  unsigned char* my = smem + wave * 4 * TILE;
+  if (a.D < DHP) {
+    for (int i = lane; i < 4 * TILE / 16; i += 64) ((uint4*)my)[i] = uint4{0, 0, 0, 0};
+    __syncthreads();
+  }
+  const uint16_t* kb = (const uint16_t*)a.k.p + kvh * a.k.head;
+  const uint16_t* vb = (const uint16_t*)a.v.p + kvh * a.v.head;
+  const int32_t* table = a.b.pages + (it.s < a.b.S ? it.s : 0) * a.b.pages_stride;
+  const int end = min(sp.hi, it.len);
+  constexpr int N = 32 / G::KPI, STEP = 32 * NW;
+  // lane l holds the page of half l & 1 of this wave's tile l / 2
+  const auto ids_from = [&](int key) { return page_ids(a, table, key + (lane >> 1) * STEP + (lane & 1) * 16, end); };
+  const int first = k0 + wave * 32;
+  if (first < k1) {
+    int ids = ids_from(first);
+    uint64_t good = good_keys<32>(ids, 0, first, end), next_good = 0;
+    stage<DHP, N>(a, kb, vb, first, 0, ids, 0, good, my, my + TILE);
+    for (int key = first, t = 0; key < k1; key += STEP, ++t) {
+      unsigned char *now = my + (t & 1) * 2 * TILE, *next = my + ((t + 1) & 1) * 2 * TILE;
+      bool all = false;
+      if (key + STEP < k1) {
+        const int g = (t + 1) * 2 & 63;
+        if (g == 0) ids = ids_from(key + STEP);
+        next_good = good_keys<32>(ids, g, key + STEP, end);
+        asm volatile("" ::: "memory");
+        all = stage<DHP, N>(a, kb, vb, key + STEP, 0, ids, g, next_good, next, next + TILE);
+      }
+      if (all) vm_wait<2 * N>();
+      else vm_wait<0>();
+      asm volatile("" ::: "memory");
+      w.step(a, col, now, now + TILE, key, good, key < sp.all_lo || key + 32 > sp.all_hi || good != 0xffffffffull, slope);
+      good = next_good;
+    }
+  }
+  // join the waves
+  const float l = other_half_sum(w.l), mb = w.m == -INFINITY ? -INFINITY : w.m * w.c;
+  if (lane < 32) {
+    stat[wave][lane][0] = mb;
+    stat[wave][lane][1] = l;
+  }
+  __syncthreads();  // (every wave has read its last tile)
+  float* so = (float*)smem;  // [NW][32][DHP], pieces of 4 swizzled by column
+  {
+    const int r = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int d = 0; d < DHP / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const int piece = 8 * d + (i >> 1) + h;
+        *(float4*)(so + (wave * 32 + r) * DHP + (piece ^ (r & 15)) * 4) =
+            float4{w.o[d][i], w.o[d][i + 1], w.o[d][i + 2], w.o[d][i + 3]};
+      }
+  }
+  __syncthreads();
+  const int G_ = a.Hq / a.H;
+  const int cols = (int)min((int64_t)kFewCols, (int64_t)it.n * G_ - (int64_t)it.tile * kFewCols);
+  for (int u = tid; u < cols * (DHP / 4); u += 64 * NW) {
+    const int r = u / (DHP / 4), piece = u - r * (DHP / 4);
+    float top = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < NW; ++v) top = fmaxf(top, stat[v][r][0]);
+    float sum = 0.f, x = 0.f, y = 0.f, z = 0.f, q = 0.f;
+#pragma unroll
+    for (int v = 0; v < NW; ++v) {
+      const float f = stat[v][r][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stat[v][r][0] - top);
+      const float4 t = *(const float4*)(so + (v * 32 + r) * DHP + (piece ^ (r & 15)) * 4);
+      if (stat[v][r][0] > -INFINITY || !(stat[v][r][1] == 0.f)) {
+        sum += f * stat[v][r][1];
+        x += f * t.x;
+        y += f * t.y;
+        z += f * t.z;
+        q += f * t.w;
+      }
+    }
+    if (alone) {
+      const float f = sum == 0.f ? 0.f : 1.f / sum;
+      const int mm = it.tile * kFewCols + r, i = mm / G_;
+      store_out<BF16>(a, it.row0 + i, kvh * G_ + (mm - i * G_), piece * 4, x * f, y * f, z * f, q * f);
+    } else {
+      const size_t at = (size_t)blockIdx.x * kFewCols + r;
+      *(float4*)(part.o + at * DHP + piece * 4) = float4{x, y, z, q};
+      if (piece == 0) *(float2*)(part.ml + at * 2) = float2{top, sum};
+    }
+  }
+}
+
+// Joins the splits of each row and head: a wave each, its lanes over the dimensions.
+template <int DHP, bool BF16>
+__global__ __launch_bounds__(256) void attend_join(AttendArgs a, Cut cut, int blocks) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t at = (int64_t)blockIdx.x * 4 + wave;
+  const int row = (int)(at / a.Hq), head = (int)(at - (int64_t)row * a.Hq);
+  if (row >= a.b.T) return;
+  const int sq = seq_of_row(a.b, row);
+  if (sq >= a.b.S) return;  // written by its only item
+  const int chunk = chunk_of(a, cut);
+  int base = 0, row0 = 0, tiles = 0, splits = 1;
+  for (int s = 0; s <= sq; s += 64) {
+    int r0, n, len, ts, range;
+    seq_load(a, cut, s + lane, r0, n, len, ts, range);
+    const int sp = splits_of(range, chunk), upto = wave_scan(ts * sp);
+    if (sq < s + 64) {
+      const int l = sq - s;
+      row0 = __builtin_amdgcn_readlane(r0, l);
+      tiles = __builtin_amdgcn_readlane(ts, l);
+      splits = __builtin_amdgcn_readlane(sp, l);
+      base += __builtin_amdgcn_readlane(upto, l) - tiles * splits;
+    } else {
+      base += __builtin_amdgcn_readlane(upto, 63);
+    }
+  }
+  if (splits <= 1) return;
+  const int G = a.Hq / a.H, kvh = head / G;
+  const int m = (row - row0) * G + head - kvh * G;
+  const int tile = m / cut.cols;
+  const int first = base + (tiles - 1 - tile) * splits;
+  const Part part = part_of(a, blocks, cut.cols, DHP);
+  const int live = part.live[(int64_t)first * a.H + kvh];
+  if (live <= 1) return;
+  const auto place = [&](int sp) { return ((size_t)(first + sp) * a.H + kvh) * cut.cols + (m - tile * cut.cols); };
+  float top = -INFINITY;
+  for (int i = lane; i < live; i += 64) top = fmaxf(top, part.ml[place(i) * 2]);
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  constexpr int VL = DHP >= 256 ? 4 : DHP / 64;  // dimensions per lane
+  float sum = 0.f, x[VL] = {};
+#pragma unroll 4
+  for (int i = 0; i < live; ++i) {
+    const size_t p = place(i);
+    const float mi = part.ml[p * 2], li = part.ml[p * 2 + 1];
+    const float f = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mi - top);
+    if (mi > -INFINITY || !(li == 0.f)) {
+      sum += f * li;
+#pragma unroll
+      for (int j = 0; j < VL; ++j) x[j] += f * part.o[p * DHP + lane * VL + j];
+    }
+  }
+  const float f = sum == 0.f ? 0.f : 1.f / sum;
+  uint16_t* out = (uint16_t*)a.out + (int64_t)row * a.out_row + head * a.out_head;
+#pragma unroll
+  for (int j = 0; j < VL; ++j)
+    if (lane * VL + j < a.D) out[lane * VL + j] = Half<BF16>::bits(x[j] * f);
+}
+
+// ------------------------------------------------------------------- launches
+
+struct Plan {
+  Cut cut;
+  int blocks;
+  bool few;
+};
+int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+
+Plan plan_of(const AttendArgs& a) {
+  Plan p{};
+  const int64_t cols = (int64_t)a.b.T * (a.Hq / a.H);
+  const int seqs = std::min(a.b.S, a.b.T);
+  p.few = cols <= (int64_t)32 * std::max(1, seqs);
+  p.cut.cols = p.few ? kFewCols : kWideCols;
+  const int64_t most = cols / p.cut.cols + std::min(a.b.S + 1, a.b.T);  // tiles there can be
+  const int64_t likely = std::max<int64_t>(seqs, (cols + p.cut.cols - 1) / p.cut.cols);
+  const int target = p.few ? 512 : 768;
+  p.cut.min_chunk = p.few ? 128 : 256;
+  p.cut.target = likely * a.H < target ? target : 0;
+  const int64_t items = p.cut.target ? 2 * most + target / a.H + 9 : most;
+  p.blocks = (int)(items * a.H);
+  return p;
+}
+
+template <class F>
+hipError_t allow_lds(F kernel, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess || (done.load(std::memory_order_acquire) >> (dev & 63) & 1)) return e;
+  e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess) done.fetch_or(1ull << (dev & 63), std::memory_order_release);
+  return e;
+}
+
+template <int DHP, bool BF16>
+hipError_t launch_dh(const AttendArgs& a, const Plan& p, hipStream_t s) {
+  static std::atomic<uint64_t> few_done{0}, wide_done{0};
+  if (p.few) {
+    hipError_t e = allow_lds(attend_few<DHP, BF16>, few_lds<DHP>(), few_done);
+    if (e != hipSuccess) return e;
+    hvd_launch((attend_few<DHP, BF16>), dim3(p.blocks), dim3(64 * few_waves<DHP>()), few_lds<DHP>(), s, a, p.cut, p.blocks);
+  } else {
+    hipError_t e = allow_lds(attend_wide<DHP, BF16>, wide_lds<DHP>(), wide_done);
+    if (e != hipSuccess) return e;
+    hvd_launch((attend_wide<DHP, BF16>), dim3(p.blocks), dim3(256), wide_lds<DHP>(), s, a, p.cut, p.blocks);
+  }
+  if (p.cut.target) {
+    const int64_t waves = (int64_t)a.b.T * a.Hq;
+    hvd_launch((attend_join<DHP, BF16>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, a, p.cut, p.blocks);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t attend_workspace(const AttendArgs& a) {
+  const Plan p = plan_of(a);
+  if (!p.cut.target) return 0;
+  return (size_t)p.blocks * (p.cut.cols * (padded_dim(a.D) + 2) + 1) * sizeof(float);
+}
+
+hipError_t launch_attend(const AttendArgs& a, hipStream_t s) {
+  const Plan p = plan_of(a);
+  const bool bf = a.type == ET_BF16;
+  switch (padded_dim(a.D)) {
+    case 64: return bf ? launch_dh<64, true>(a, p, s) : launch_dh<64, false>(a, p, s);
+    case 128: return bf ? launch_dh<128, true>(a, p, s) : launch_dh<128, false>(a, p, s);
+    default: return bf ? launch_dh<256, true>(a, p, s) : launch_dh<256, false>(a, p, s);
+  }
+}
+
+}  // namespace hvd

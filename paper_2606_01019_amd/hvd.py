@@ -23,7 +23,8 @@ EXPORTS = ("hvd_model_bytes", "hvd_model_load", "hvd_model_free", "hvd_kv_bytes"
            "hvd_async_begin", "hvd_async_step", "hvd_async_end", "hvd_verify_noalloc", "hvd_flow_trace",
            "hvd_measure_mfma_peak", "hvd_route", "hvd_experts_bytes", "hvd_experts_load", "hvd_experts_free",
            "hvd_experts_workspace", "hvd_experts_forward", "hvd_block_norm", "hvd_model_bytes_moe",
-           "hvd_kv_bytes_moe", "hvd_model_load_moe")
+           "hvd_kv_bytes_moe", "hvd_model_load_moe", "hvd_append_kv", "hvd_attend_workspace", "hvd_attend",
+           "hvd_adjust_workspace", "hvd_adjust_logits")
 HVD_OPT_GRAPHS = 1
 HVD_OPT_MLP_SINGLE = 2
 HVD_OPT_LM_SINGLE = 3
@@ -149,6 +150,11 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "hvd_model_bytes_moe": (SZ, [P, P]),
         "hvd_kv_bytes_moe": (SZ, [P, P, I32, I32]),
         "hvd_model_load_moe": (I32, [P, P, P, P, SZ, P, ctypes.POINTER(P)]),
+        "hvd_append_kv": (I32, [P, P, P, I32, P]),
+        "hvd_attend_workspace": (SZ, [P, P, I32, I32]),
+        "hvd_attend": (I32, [P, P, P, I32, P, SZ, P]),
+        "hvd_adjust_workspace": (SZ, [P, P, I32]),
+        "hvd_adjust_logits": (I32, [P, P, I32, P, SZ, P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
