@@ -487,7 +487,7 @@ typedef struct {
 
 /* A paged cache of one layer: keys and values [n_pages][n_heads][page_size][head_dim]
  * of dtype HVD_F16 or HVD_BF16, the four dimensions at any strides that do not
- * overlap (elements, multiples of 8, token strides at most 2^28; head_dim itself
+ * overlap (elements, multiples of 8, token strides at most 2^26; head_dim itself
  * contiguous), 16-byte aligned.  page_size is a power of two from 16 to 1024,
  * head_dim a multiple of 8 from 8 to 256, n_heads at most 256. */
 typedef struct {

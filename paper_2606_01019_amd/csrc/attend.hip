@@ -27,6 +27,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 namespace hvd {
 namespace {
@@ -241,77 +242,126 @@ struct Geo {
   }
 };
 
-// The cache pages of 64 groups of 16 keys, one per lane: group l starts at key
-// `key` of lane l.  -1: past `end`, or not a page of the cache.
-__device__ __forceinline__ int page_ids(const AttendArgs& a, const int32_t* table, int key, int end) {
+// Where 64 groups of 16 keys lie in the cache, one per lane (group l starts at key
+// `key` of lane l): byte offsets of their pages, and which of them have one --
+// none past `end`, and none that the cache does not have.
+struct Pages {
+  uint32_t k_lo, k_hi, v_lo, v_hi;
+  uint64_t has;
+};
+__device__ __forceinline__ Pages pages_of(const AttendArgs& a, const int32_t* table, int key, int end) {
   const int pi = key >> a.page_shift;
-  int p = key < end && pi < a.b.P ? table[pi] : -1;
-  return (unsigned)p < (unsigned)a.n_pages ? p : -1;
+  const int p = key < end && pi < a.b.P ? table[pi] : -1;
+  const bool in = (unsigned)p < (unsigned)a.n_pages;
+  const int64_t k = 2 * (in ? p : 0) * a.k.page, v = 2 * (in ? p : 0) * a.v.page;
+  return Pages{(uint32_t)k, (uint32_t)(k >> 32), (uint32_t)v, (uint32_t)(v >> 32), __builtin_amdgcn_ballot_w64(in)};
 }
 
 // Which of a tile's NK keys have a page: group g0 is the tile's first.
 template <int NK>
-__device__ __forceinline__ uint64_t good_keys(int ids, int g0, int key0, int end) {
+__device__ __forceinline__ uint64_t good_keys(uint64_t has, int g0, int key0, int end) {
+  constexpr uint64_t kAll = NK == 64 ? ~0ull : (1ull << NK) - 1, kGroups = (1 << (NK / 16)) - 1;
+  const uint64_t mine = has >> g0 & kGroups;
+  if (mine == kGroups && key0 + NK <= end) return kAll;
   uint64_t good = 0;
 #pragma unroll
-  for (int g = 0; g < NK / 16; ++g)
-    if (__builtin_amdgcn_readlane(ids, g0 + g) >= 0) good |= 0xffffull << (16 * g);
+  for (int g = 0; g < NK / 16; ++g) good |= mine >> g & 1 ? 0xffffull << (16 * g) : 0;
   const int n = end - key0;
-  if (n < NK) good &= n > 0 ? (1ull << n) - 1 : 0;
-  return good;
+  return n >= NK ? good : n > 0 ? good & ((1ull << n) - 1) : 0;
 }
 
-// Copies of keys [k0, k0 + N * KPI) of a tile to LDS, K and V.  Returns false if
-// fewer than 2 N copies were asked for.
+// The same value, which the compiler takes for a new one each time: addresses built
+// from it are not kept in registers (which the accumulators need) over the loop.
+__device__ __forceinline__ int afresh(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+// 16 bytes per lane from base + off (bytes; a wave-uniform base, 32 bits per lane)
+// to LDS at dst + 16 * lane.  In assembly because the compiler, which cannot tell
+// the tiles apart, would have a transposing read of one tile wait for the
+// copies to the other; the waits are the callers'.  (m0 takes a cycle to arrive;
+// nothing else here uses it.)
+__device__ __forceinline__ void copy_to_lds(const char* base, uint32_t off, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(off), "s"(base) : "memory");
+}
+
+// Copies of N * KPI keys of a tile to LDS, K and V: whole groups of 16, or a part
+// of one.
 template <int DHP, int N>
-__device__ __forceinline__ bool stage(const AttendArgs& a, const uint16_t* kb, const uint16_t* vb, int key0, int k0, int ids, int g0,
-                                      uint64_t good, unsigned char* lk, unsigned char* lv) {
+struct Copies {
   using G = Geo<DHP>;
-  const int lane = threadIdx.x & 63;
-  const int kk = lane / G::CH, piece = lane % G::CH;
-  const int in_page = (1 << a.page_shift) - 1;
-  constexpr uint64_t kMine = N * G::KPI >= 64 ? ~0ull : (1ull << (N * G::KPI & 63)) - 1;
-  const bool whole = (good >> k0 & kMine) == kMine && a.D == DHP;
+  static constexpr int PER = N * G::KPI < 16 ? N : 16 / G::KPI;  // copies per group
+  uint32_t k_off[PER], v_off[PER];  // of this lane, from the first key's place
+  int piece[PER];
+
+  // k0: the first key's place in the tile (of a group, or of this part of one)
+  __device__ __forceinline__ void init(const AttendArgs& a, int k0) {
+    const int lane = threadIdx.x & 63, kk = lane / G::CH;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int kf = k0 + i * G::KPI;  // wave-uniform
-    const int64_t p = __builtin_amdgcn_readlane(ids, g0 + (kf >> 4));
-    const int k = kf + kk;
-    const int c = piece ^ G::swz(k);
-    const int64_t tok = (key0 + kf) & in_page;
-    // (a wave-uniform address and 32 bits of each lane's own)
-    const char* kp = (const char*)(kb + (p * a.k.page + tok * a.k.tok)) + (uint32_t)(kk * (int)a.k.tok + c * 8) * 2u;
-    const char* vp = (const char*)(vb + (p * a.v.page + tok * a.v.tok)) + (uint32_t)(kk * (int)a.v.tok + c * 8) * 2u;
-    unsigned char *dk = lk + kf * G::ROW, *dv = lv + kf * G::ROW;
-    if (whole) {
-      __builtin_amdgcn_global_load_lds((const void*)kp, (lds_void*)dk, 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((const void*)vp, (lds_void*)dv, 16, 0, 0);
-    } else {
-      // pieces past the head dimension stay zero, keys without a page become it
-      const bool in = c * 8 < a.D, ok = good >> k & 1;
-      if (in && ok) {
-        __builtin_amdgcn_global_load_lds((const void*)kp, (lds_void*)dk, 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((const void*)vp, (lds_void*)dv, 16, 0, 0);
-      }
-      if (in && !ok) {
-        *(uint4*)(dk + lane * 16) = uint4{0, 0, 0, 0};
-        *(uint4*)(dv + lane * 16) = uint4{0, 0, 0, 0};
-      }
+    for (int i = 0; i < PER; ++i) {
+      const int k = i * G::KPI + kk;
+      piece[i] = (lane % G::CH) ^ G::swz(k0 + k);
+      k_off[i] = 2u * (uint32_t)(k * (int)a.k.tok + piece[i] * 8);
+      v_off[i] = 2u * (uint32_t)(k * (int)a.v.tok + piece[i] * 8);
     }
   }
-  if (!whole) __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the zeros are there before the barrier
-  return whole;
-}
 
-// The lowest n bits (none for n <= 0, all for n >= 64).
-__device__ __forceinline__ uint64_t below(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
+  // The tile begins with key0; group g0 of `pg` is its first, `good` its keys that
+  // have a page.  Returns false if fewer than 2 N copies were asked for.
+  __device__ __forceinline__ bool issue(const AttendArgs& a, const char* kb, const char* vb, int key0, int k0, const Pages& pg, int g0,
+                                        uint64_t good, unsigned char* smem, uint32_t lk, uint32_t lv) const {
+    constexpr uint64_t kMine = N * G::KPI >= 64 ? ~0ull : (1ull << (N * G::KPI & 63)) - 1;
+    const bool whole = (good >> k0 & kMine) == kMine && a.D == DHP;
+    const uint32_t base = (uint32_t)(uintptr_t)(lds_void*)smem;
+#pragma unroll
+    for (int f = 0; f < N; f += PER) {
+      const int first = k0 + f * G::KPI, g = g0 + (first >> 4);  // wave-uniform
+      const uint32_t tok = 2u * ((key0 + first) & ((1 << a.page_shift) - 1));
+      const char* kp = kb + (uint64_t)tok * (uint32_t)a.k.tok +
+                       ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(pg.k_hi, g) << 32 | (uint32_t)__builtin_amdgcn_readlane(pg.k_lo, g));
+      const char* vp = vb + (uint64_t)tok * (uint32_t)a.v.tok +
+                       ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(pg.v_hi, g) << 32 | (uint32_t)__builtin_amdgcn_readlane(pg.v_lo, g));
+      if (whole) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const uint32_t at = (first + i * G::KPI) * G::ROW;
+          copy_to_lds(kp, k_off[i], base + lk + at);
+          copy_to_lds(vp, v_off[i], base + lv + at);
+        }
+      } else {
+        // pieces past the head dimension stay zero, keys without a page become it
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const uint32_t at = (first + i * G::KPI) * G::ROW;
+          const bool in = piece[i] * 8 < a.D, ok = good >> (first + i * G::KPI + lane / G::CH) & 1;
+          if (in && ok) {
+            copy_to_lds(kp, k_off[i], base + lk + at);
+            copy_to_lds(vp, v_off[i], base + lv + at);
+          }
+          if (in && !ok) {
+            *(uint4*)(smem + lk + at + lane * 16) = uint4{0, 0, 0, 0};
+            *(uint4*)(smem + lv + at + lane * 16) = uint4{0, 0, 0, 0};
+          }
+        }
+      }
+    }
+    if (!whole) __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the zeros are there before the barrier
+    return whole;
+  }
+};
 
 __device__ __forceinline__ s16x8 join4(s16x4 x, s16x4 y) {
   return s16x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
 }
 
-// The state of a wave's 32 columns; NB blocks of 32 keys per step.
-template <int DHP, bool BF16, int NB>
+// The lowest n bits (none for n <= 0, all for n >= 64).
+__device__ __forceinline__ uint64_t below(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
+
+// The state of a wave's 32 columns; NB blocks of 32 keys per step.  TURN: scores
+// are made exponents one by one (a cap, a bias, a scale that is not positive).
+template <int DHP, bool BF16, int NB, bool TURN>
 struct Wave {
   using G = Geo<DHP>;
   using H = Half<BF16>;
@@ -319,17 +369,18 @@ struct Wave {
   f32x16 o[DHP / 32];
   float m, l;   // of the scores times `c`; l of this lane's half of the keys
   float c;      // the scores' factor to base-2 exponents
-  bool turned;  // the scores are made exponents one by one
 
-  __device__ __forceinline__ void init(const AttendArgs& a, const Column& col, int h) {
+  __device__ __forceinline__ void reset() {
     m = -INFINITY;
     l = 0.f;
-    turned = a.cap > 0.f || a.slopes || !(a.scale > 0.f);
-    c = turned ? 1.f : a.scale * kLog2e;
 #pragma unroll
     for (int d = 0; d < DHP / 32; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+  }
+  __device__ __forceinline__ void init(const AttendArgs& a, const Column& col, int h) {
+    reset();
+    c = TURN ? 1.f : a.scale * kLog2e;
     const uint16_t* src = (const uint16_t*)a.q + (int64_t)max(col.row, 0) * a.q_row + (col.row >= 0 ? col.head : 0) * a.q_head;
 #pragma unroll
     for (int s = 0; s < DHP / 16; ++s) {
@@ -340,24 +391,43 @@ struct Wave {
   }
 
   // One tile: keys key0 .. key0 + 32 NB - 1.  masked: some column does not see some
-  // key of it.
+  // key of it.  CAREFUL: with what is not finite in V taken care of.
+  // The operands of a product are read from LDS before it begins (and half of V
+  // before the softmax), which the barriers for the scheduler say: left to
+  // itself it reads each just before its use.
+  template <bool CAREFUL>
   __device__ __forceinline__ void step(const AttendArgs& a, const Column& col, const unsigned char* lk, const unsigned char* lv,
                                        int key0, uint64_t good, bool masked, float slope) {
     const int lane = threadIdx.x & 63, h = lane >> 5, r = lane & 31;
     f32x16 s[NB];
+    {
+      // (piece 2t + h of key 32b + r: the key's swizzle does not depend on b, nor its low bit on t)
+      const unsigned char* kr = lk + r * G::ROW;
+      const int kx = afresh((h ^ G::swz(r)) * 16);
+      s16x8 kf[DHP / 16][NB];
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+      for (int t = 0; t < DHP / 16; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
-    // (piece 2t + h of key 32b + r: the key's swizzle does not depend on b, nor its low bit on t)
-    const unsigned char* kr = lk + r * G::ROW;
-    const int kx = (h ^ G::swz(r)) * 16;
-#pragma unroll
-    for (int t = 0; t < DHP / 16; ++t)
+        for (int b = 0; b < NB; ++b) kf[t][b] = *(const s16x8*)(kr + (kx ^ (32 * t)) + 32 * b * G::ROW);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int b = 0; b < NB; ++b)
-        s[b] = H::mfma(*(const s16x8*)(kr + (kx ^ (32 * t)) + 32 * b * G::ROW), q[t], s[b]);
-    if (turned) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+#pragma unroll
+      for (int t = 0; t < DHP / 16; ++t)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) s[b] = H::mfma(kf[t][b], q[t], s[b]);
+    }
+    s16x8 vf[2 * NB][DHP / 32];
+    if constexpr (!CAREFUL) {
+#pragma unroll
+      for (int t = 0; t < NB; ++t)
+#pragma unroll
+        for (int d = 0; d < DHP / 32; ++d) vf[t][d] = read_v8(lv, t, h, d);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (TURN) {
       const float f = a.scale * kLog2e, cl = a.cap * kLog2e, inv = a.cap > 0.f ? a.scale / a.cap : 0.f;
 #pragma unroll
       for (int b = 0; b < NB; ++b)
@@ -413,7 +483,7 @@ struct Wave {
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
     top = other_half_max(top);
     // The maximum lags until a weight would pass 2^kLazy: most tiles rescale nothing
-    if (__builtin_amdgcn_ballot_w64(top * c > m * c + kLazy || (m == -INFINITY && top > -INFINITY))) {
+    if (__builtin_amdgcn_ballot_w64(top * c > m * c + kLazy)) {
       const float mn = fmaxf(m, top);
       const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * c);
       l *= f;
@@ -436,14 +506,30 @@ struct Wave {
     for (int t = 0; t < 2 * NB; ++t)
 #pragma unroll
       for (int j = 0; j < 8; ++j) p[t][j] = (short)H::bits(s[t >> 1][8 * (t & 1) + j]);
-    if (masked && values_not_finite(lv)) {
+    if constexpr (CAREFUL) {
       add_not_finite(lv, p, h);
     } else {
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int t = NB; t < 2 * NB; ++t)
+#pragma unroll
+        for (int d = 0; d < DHP / 32; ++d) vf[t][d] = read_v8(lv, t, h, d);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int t = 0; t < 2 * NB; ++t)
 #pragma unroll
-        for (int d = 0; d < DHP / 32; ++d) o[d] = H::mfma(read_v8(lv, t, h, d), p[t], o[d]);
+        for (int d = 0; d < DHP / 32; ++d) o[d] = H::mfma(vf[t][d], p[t], o[d]);
     }
+  }
+
+  // Whether some dimension of some column came out as a NaN.
+  __device__ __forceinline__ bool any_nan() const {
+    bool bad = false;
+#pragma unroll
+    for (int d = 0; d < DHP / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) bad = bad || o[d][i] != o[d][i];
+    return __builtin_amdgcn_ballot_w64(bad) != 0;
   }
 
   // V's operand of 32 dimensions (from 32 d) for the 16 keys of P's operand t: keys
@@ -454,26 +540,15 @@ struct Wave {
     const int lane = threadIdx.x & 63;
     const int key = 4 * h + (lane >> 2 & 3), dim = (lane & 16) + (lane & 3) * 4;
     const unsigned char* p = lv + key * G::ROW + (dim & 7) * 2 + 16 * t * G::ROW;
-    const int x = ((dim >> 3) ^ G::swz(key)) * 16, y = ((dim >> 3) ^ G::swz(key + 8)) * 16;
+    const int x = afresh(((dim >> 3) ^ G::swz(key)) * 16);  // (key + 8: another piece, two away)
     return join4(__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (x ^ (64 * d)))),
-                 __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (y ^ (64 * d)) + 8 * G::ROW)));
+                 __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (x ^ (64 * d) ^ 32) + 8 * G::ROW)));
   }
 
   // A value that a column does not see must not reach it, and 0 times an infinity
-  // or a NaN would.  In a tile with hidden keys and such values these are taken
-  // out of V and counted, by weight, where they are; a dimension's count makes
-  // it infinite, both signs' (a NaN is both) a NaN.
-  __device__ __forceinline__ bool values_not_finite(const unsigned char* lv) {
-    const int lane = threadIdx.x & 63;
-    uint32_t bad = 0;
-#pragma unroll
-    for (int i = 0; i < 32 * NB / G::KPI; ++i) {
-      const uint4 v = *(const uint4*)(lv + (i * 64 + lane) * 16);
-      bad |= ((v.x & 0x7fff7fffu) + H::kInf) | ((v.y & 0x7fff7fffu) + H::kInf) | ((v.z & 0x7fff7fffu) + H::kInf) |
-             ((v.w & 0x7fff7fffu) + H::kInf);
-    }
-    return __builtin_amdgcn_ballot_w64(bad & 0x80008000u) != 0;
-  }
+  // or a NaN would.  So where a result is a NaN, the item is done once more with
+  // this: such values are taken out of V and counted, by weight, where they are;
+  // a dimension's count makes it infinite, both signs' (a NaN is both) a NaN.
   __device__ __forceinline__ void add_not_finite(const unsigned char* lv, const s16x8 (&p)[2 * NB], int h) {
 #pragma unroll
     for (int d = 0; d < DHP / 32; ++d) {
@@ -551,7 +626,7 @@ constexpr int wide_blocks() { return DHP == 256 ? 1 : 2; }
 template <int DHP>
 constexpr int wide_lds() { return 2 * 2 * 32 * wide_blocks<DHP>() * DHP * 2; }
 
-template <int DHP, bool BF16>
+template <int DHP, bool BF16, bool TURN>
 __global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArgs a, Cut cut, int blocks) {
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ int red[4][2];
@@ -576,7 +651,7 @@ __global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArg
   int k0, k1;
   bool alone;
   if (!cut_keys(a, it, part, lo, hi, k0, k1, alone)) return;
-  Wave<DHP, BF16, NB> w;
+  Wave<DHP, BF16, NB, TURN> w;
   w.init(a, col, lane >> 5);
   const float slope = a.slopes && col.row >= 0 ? a.slopes[col.head] * kLog2e : 0.f;
   if (k0 < k1) {
@@ -584,29 +659,53 @@ __global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArg
       for (int i = tid; i < 4 * TILE / 16; i += 256) ((uint4*)smem)[i] = uint4{0, 0, 0, 0};
       __syncthreads();
     }
-    const uint16_t* kb = (const uint16_t*)a.k.p + kvh * a.k.head;
-    const uint16_t* vb = (const uint16_t*)a.v.p + kvh * a.v.head;
+    const char* kb = (const char*)a.k.p + 2 * kvh * a.k.head;
+    const char* vb = (const char*)a.v.p + 2 * kvh * a.v.head;
     const int32_t* table = a.b.pages + (it.s < a.b.S ? it.s : 0) * a.b.pages_stride;
     const int end = min(hi, it.len);
     constexpr int N = KT / G::KPI / 4;
     const int mine = wave * N * G::KPI;
-    int ids = page_ids(a, table, k0 + lane * 16, end);
-    uint64_t good = good_keys<KT>(ids, 0, k0, end), next_good = 0;
-    stage<DHP, N>(a, kb, vb, k0, mine, ids, 0, good, smem, smem + TILE);
-    for (int key = k0, t = 0; key < k1; key += KT, ++t) {
-      vm_wait<0>();
-      block_barrier();
-      unsigned char* now = smem + (t & 1) * 2 * TILE;
-      if (key + KT < k1) {
-        const int g = (t + 1) * (KT / 16) & 63;
-        if (g == 0) ids = page_ids(a, table, key + KT + lane * 16, end);
-        next_good = good_keys<KT>(ids, g, key + KT, end);
-        unsigned char* next = smem + ((t + 1) & 1) * 2 * TILE;
-        stage<DHP, N>(a, kb, vb, key + KT, mine, ids, g, next_good, next, next + TILE);
+    Copies<DHP, N> copies;
+    copies.init(a, mine);
+    const auto run = [&](auto careful) __attribute__((always_inline)) {
+      Pages pg = pages_of(a, table, k0 + lane * 16, end);
+      uint64_t good = good_keys<KT>(pg.has, 0, k0, end), next_good = 0;
+      copies.issue(a, kb, vb, k0, mine, pg, 0, good, smem, 0, TILE);
+      int key = k0, t = 0;
+      // waits for this tile and begins to copy the next one
+      const auto next = [&]() __attribute__((always_inline)) {
+        vm_wait<0>();
+        block_barrier();
+        if (key + KT < k1) {
+          const int g = (t + 1) * (KT / 16) & 63;
+          if (g == 0) pg = pages_of(a, table, key + KT + lane * 16, end);
+          next_good = good_keys<KT>(pg.has, g, key + KT, end);
+          const uint32_t to = ((t + 1) & 1) * 2 * TILE;
+          copies.issue(a, kb, vb, key + KT, mine, pg, g, next_good, smem, to, to + TILE);
+        }
+      };
+      const auto skip = [&](int until) __attribute__((always_inline)) {
+        for (; key < until; key += KT, ++t) {
+          next();
+          good = next_good;
+        }
+      };
+      // tiles that this wave's columns see, those before and after them only copied
+      // (three loops: a branch around the step has the compiler move its accumulators)
+      skip(min(k1, sp.lo - (KT - 1)));
+      for (; key < min(k1, sp.hi); key += KT, ++t) {
+        next();
+        unsigned char* now = smem + (t & 1) * 2 * TILE;
+        w.template step<decltype(careful)::value>(a, col, now, now + TILE, key, good,
+                                                  key < sp.all_lo || key + KT > sp.all_hi || good != kAll, slope);
+        good = next_good;
       }
-      if (key < sp.hi && key + KT > sp.lo)
-        w.step(a, col, now, now + TILE, key, good, key < sp.all_lo || key + KT > sp.all_hi || good != kAll, slope);
-      good = next_good;
+      skip(k1);
+    };
+    run(std::false_type{});
+    if (__syncthreads_or(w.any_nan())) {  // (all of them: the tiles are shared)
+      w.reset();
+      run(std::true_type{});
     }
   }
   if (col.row < 0) return;
@@ -640,8 +739,8 @@ constexpr int few_waves() { return DHP == 256 ? 2 : 4; }
 template <int DHP>
 constexpr int few_lds() { return few_waves<DHP>() * 2 * 2 * 32 * DHP * 2; }
 
-template <int DHP, bool BF16>
-__global__ __launch_bounds__(64 * few_waves<DHP>()) void attend_few(AttendArgs a, Cut cut, int blocks) {
+template <int DHP, bool BF16, bool TURN>
+__global__ __launch_bounds__(64 * few_waves<DHP>(), DHP == 256 ? 1 : 2) void attend_few(AttendArgs a, Cut cut, int blocks) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int NW = few_waves<DHP>();
   __shared__ float stat[NW][32][2];
@@ -657,7 +756,7 @@ __global__ __launch_bounds__(64 * few_waves<DHP>()) void attend_few(AttendArgs a
   int k0, k1;
   bool alone;
   if (!cut_keys(a, it, part, sp.lo, sp.hi, k0, k1, alone)) return;
-  Wave<DHP, BF16, 1> w;
+  Wave<DHP, BF16, 1, TURN> w;
   w.init(a, col, lane >> 5);
   const float slope = a.slopes && col.row >= 0 ? a.slopes[col.head] * kLog2e : 0.f;
   unsigned char* my = smem + wave * 4 * TILE;
@@ -665,33 +764,42 @@ __global__ __launch_bounds__(64 * few_waves<DHP>()) void attend_few(AttendArgs a
     for (int i = lane; i < 4 * TILE / 16; i += 64) ((uint4*)my)[i] = uint4{0, 0, 0, 0};
     __syncthreads();
   }
-  const uint16_t* kb = (const uint16_t*)a.k.p + kvh * a.k.head;
-  const uint16_t* vb = (const uint16_t*)a.v.p + kvh * a.v.head;
+  const char* kb = (const char*)a.k.p + 2 * kvh * a.k.head;
+  const char* vb = (const char*)a.v.p + 2 * kvh * a.v.head;
   const int32_t* table = a.b.pages + (it.s < a.b.S ? it.s : 0) * a.b.pages_stride;
   const int end = min(sp.hi, it.len);
   constexpr int N = 32 / G::KPI, STEP = 32 * NW;
   // lane l holds the page of half l & 1 of this wave's tile l / 2
-  const auto ids_from = [&](int key) { return page_ids(a, table, key + (lane >> 1) * STEP + (lane & 1) * 16, end); };
+  const auto pages_from = [&](int key) { return pages_of(a, table, key + (lane >> 1) * STEP + (lane & 1) * 16, end); };
   const int first = k0 + wave * 32;
-  if (first < k1) {
-    int ids = ids_from(first);
-    uint64_t good = good_keys<32>(ids, 0, first, end), next_good = 0;
-    stage<DHP, N>(a, kb, vb, first, 0, ids, 0, good, my, my + TILE);
+  Copies<DHP, N> copies;
+  copies.init(a, 0);
+  const auto run = [&](auto careful) __attribute__((always_inline)) {
+    Pages pg = pages_from(first);
+    uint64_t good = good_keys<32>(pg.has, 0, first, end), next_good = 0;
+    copies.issue(a, kb, vb, first, 0, pg, 0, good, my, 0, TILE);
     for (int key = first, t = 0; key < k1; key += STEP, ++t) {
-      unsigned char *now = my + (t & 1) * 2 * TILE, *next = my + ((t + 1) & 1) * 2 * TILE;
+      const uint32_t now = (t & 1) * 2 * TILE, next = ((t + 1) & 1) * 2 * TILE;
       bool all = false;
       if (key + STEP < k1) {
         const int g = (t + 1) * 2 & 63;
-        if (g == 0) ids = ids_from(key + STEP);
-        next_good = good_keys<32>(ids, g, key + STEP, end);
-        asm volatile("" ::: "memory");
-        all = stage<DHP, N>(a, kb, vb, key + STEP, 0, ids, g, next_good, next, next + TILE);
+        if (g == 0) pg = pages_from(key + STEP);
+        next_good = good_keys<32>(pg.has, g, key + STEP, end);
+        all = copies.issue(a, kb, vb, key + STEP, 0, pg, g, next_good, my, next, next + TILE);
       }
       if (all) vm_wait<2 * N>();
       else vm_wait<0>();
       asm volatile("" ::: "memory");
-      w.step(a, col, now, now + TILE, key, good, key < sp.all_lo || key + 32 > sp.all_hi || good != 0xffffffffull, slope);
+      w.template step<decltype(careful)::value>(a, col, my + now, my + now + TILE, key, good,
+                                                key < sp.all_lo || key + 32 > sp.all_hi || good != 0xffffffffull, slope);
       good = next_good;
+    }
+  };
+  if (first < k1) {
+    run(std::false_type{});
+    if (w.any_nan()) {
+      w.reset();
+      run(std::true_type{});
     }
   }
   // join the waves
@@ -838,23 +946,31 @@ hipError_t allow_lds(F kernel, int bytes, std::atomic<uint64_t>& done) {
   return e;
 }
 
-template <int DHP, bool BF16>
-hipError_t launch_dh(const AttendArgs& a, const Plan& p, hipStream_t s) {
+template <int DHP, bool BF16, bool TURN>
+hipError_t launch_kernel(const AttendArgs& a, const Plan& p, hipStream_t s) {
   static std::atomic<uint64_t> few_done{0}, wide_done{0};
   if (p.few) {
-    hipError_t e = allow_lds(attend_few<DHP, BF16>, few_lds<DHP>(), few_done);
+    hipError_t e = allow_lds(attend_few<DHP, BF16, TURN>, few_lds<DHP>(), few_done);
     if (e != hipSuccess) return e;
-    hvd_launch((attend_few<DHP, BF16>), dim3(p.blocks), dim3(64 * few_waves<DHP>()), few_lds<DHP>(), s, a, p.cut, p.blocks);
+    hvd_launch((attend_few<DHP, BF16, TURN>), dim3(p.blocks), dim3(64 * few_waves<DHP>()), few_lds<DHP>(), s, a, p.cut, p.blocks);
   } else {
-    hipError_t e = allow_lds(attend_wide<DHP, BF16>, wide_lds<DHP>(), wide_done);
+    hipError_t e = allow_lds(attend_wide<DHP, BF16, TURN>, wide_lds<DHP>(), wide_done);
     if (e != hipSuccess) return e;
-    hvd_launch((attend_wide<DHP, BF16>), dim3(p.blocks), dim3(256), wide_lds<DHP>(), s, a, p.cut, p.blocks);
-  }
-  if (p.cut.target) {
-    const int64_t waves = (int64_t)a.b.T * a.Hq;
-    hvd_launch((attend_join<DHP, BF16>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, a, p.cut, p.blocks);
+    hvd_launch((attend_wide<DHP, BF16, TURN>), dim3(p.blocks), dim3(256), wide_lds<DHP>(), s, a, p.cut, p.blocks);
   }
   return hipGetLastError();
+}
+
+template <int DHP, bool BF16>
+hipError_t launch_dh(const AttendArgs& a, const Plan& p, hipStream_t s) {
+  const bool turn = a.cap > 0.f || a.slopes || !(a.scale > 0.f);
+  hipError_t e = turn ? launch_kernel<DHP, BF16, true>(a, p, s) : launch_kernel<DHP, BF16, false>(a, p, s);
+  if (e == hipSuccess && p.cut.target) {
+    const int64_t waves = (int64_t)a.b.T * a.Hq;
+    hvd_launch((attend_join<DHP, BF16>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, a, p.cut, p.blocks);
+    e = hipGetLastError();
+  }
+  return e;
 }
 
 }  // namespace

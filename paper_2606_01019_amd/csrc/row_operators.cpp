@@ -67,7 +67,7 @@ hvd_status check_kv(const hvd_paged_kv* c, const hvd_row_batch* b, CacheView& k,
   for (int64_t s : {c->k_page_stride, c->k_head_stride, c->k_token_stride, c->v_page_stride, c->v_head_stride, c->v_token_stride})
     if (s < 0 || s % 8) return set_err(HVD_ERR_ARG, "the cache's strides must be multiples of 8");
   if (c->k_token_stride > kMaxTokStride || c->v_token_stride > kMaxTokStride)
-    return set_err(HVD_ERR_ARG, "the cache's token strides must be at most 2^28");
+    return set_err(HVD_ERR_ARG, "the cache's token strides must be at most 2^26");
   if (!apart(c->k_page_stride, c->k_head_stride, c->k_token_stride, *c) || !apart(c->v_page_stride, c->v_head_stride, c->v_token_stride, *c))
     return set_err(HVD_ERR_ARG, "places of the cache overlap");
   k = CacheView{c->k, c->k_page_stride, c->k_head_stride, c->k_token_stride};

@@ -16,7 +16,7 @@ constexpr int kMaxStepRows = 1 << 20;  // rows of one call
 constexpr int kMaxRowHeads = 256;      // heads of one tensor
 constexpr int kMaxRowDim = 256;        // head dimension
 constexpr int kMaxKeys = 1 << 29;      // keys that a sequence's pages may hold
-constexpr int64_t kMaxTokStride = 1 << 28;
+constexpr int64_t kMaxTokStride = 1 << 26;
 constexpr int kMaxVocab = 1 << 24;
 constexpr int kMaxAdjustRows = 1 << 16;  // rows of one call of adjust_logits
 constexpr int kMaxHistory = (1 << 20) - 1 - kMaxAdjustRows;  // a count has 20 bits

@@ -60,7 +60,7 @@ BAD_KV = [dict(k=None), dict(v=None), dict(k=A + 8), dict(v=A + 2), dict(n_pages
           dict(page_size=8), dict(page_size=48), dict(page_size=2048), dict(head_dim=0), dict(head_dim=60),
           dict(head_dim=264), dict(dtype=2), dict(dtype=3), dict(dtype=-1), dict(k_page_stride=2047),
           dict(k_page_stride=1024), dict(k_token_stride=56), dict(v_head_stride=32), dict(v_token_stride=64),
-          dict(k_token_stride=(1 << 28) + 8), dict(k_head_stride=-8), dict(v_page_stride=0), dict(k_page_stride=1 << 60)]
+          dict(k_token_stride=(1 << 26) + 8), dict(k_head_stride=-8), dict(v_page_stride=0), dict(k_page_stride=1 << 60)]
 
 
 @pytest.mark.parametrize("kw", BAD_BATCH + BAD_KEYS)
