@@ -74,16 +74,16 @@ __device__ __forceinline__ float other_half_sum(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// How the work is cut: columns per tile; `target` items wanted, or 0: a tile's
-// keys are not split.
+// How the work is cut: columns per tile; workgroups that the card holds at once, or
+// 0: no tile's keys are split; the fewest keys of a split.
 struct Cut {
-  int cols, target, min_chunk;
+  int cols, slots, min_chunk;
 };
 
 // One item: columns [col0, col0 + cols) of sequence s over the keys of split
 // `split` of its tile.
 struct Item {
-  int s, row0, n, len, tile, split, splits, chunk, first_item;
+  int s, row0, n, len, tile, split, splits, chunk;
 };
 
 // How many keys a tile of sequence s may see at most, and its tiles.
@@ -101,33 +101,46 @@ __device__ __forceinline__ void seq_load(const AttendArgs& a, const Cut& c, int 
   if (range < 0) range = len;
 }
 
-// The keys of one split: the same in every workgroup.
+// The keys of one split, the same in every workgroup: so many that there are 3
+// items for 2 slots.  Nothing is split where the tiles fill the card by themselves
+// and none is much longer than a slot's share.
 __device__ __forceinline__ int chunk_of(const AttendArgs& a, const Cut& c) {
-  if (c.target == 0) return 1 << 30;
+  constexpr int kWhole = 1 << 30;
+  if (c.slots == 0) return kWhole;
   const int lane = threadIdx.x & 63;
   float total = 0.f;
+  int count = 0, longest = 0;
   for (int s = 0; s <= a.b.S; s += 64) {
     int row0, n, len, tiles, range;
     seq_load(a, c, s + lane, row0, n, len, tiles, range);
     total += (float)tiles * (float)range;
+    count += tiles;
+    longest = max(longest, tiles > 0 ? range : 0);
   }
   total = wave_sum(total) * (float)a.H;
-  int k = (int)fminf(total / (float)c.target, 1.0e9f);
+  for (int o = 32; o > 0; o >>= 1) {
+    count += __shfl_xor(count, o);
+    longest = max(longest, __shfl_xor(longest, o));
+  }
+  if (count * a.H * 8 >= c.slots * 7 && (float)longest * (float)c.slots <= 1.2f * total) return kWhole;
+  int k = (int)fminf(total / (1.5f * (float)c.slots), 1.0e9f);
   k = (k + 127) & ~63;
   return __builtin_amdgcn_readfirstlane(max(k, c.min_chunk));
 }
 
+// A tile of up to `range` keys in even splits of at most `chunk`.
 __device__ __forceinline__ int splits_of(int range, int chunk) { return max(1, (int)(((int64_t)range + 63 + chunk - 1) / chunk)); }
+__device__ __forceinline__ int even_chunk(int range, int splits) { return (int)((((int64_t)range + 63 + splits - 1) / splits + 63) & ~63ll); }
 
 // Item number `idx`; false past the last one.
 __device__ __forceinline__ bool find_item(const AttendArgs& a, const Cut& c, int idx, Item& it) {
   const int lane = threadIdx.x & 63;
-  it.chunk = chunk_of(a, c);
+  const int chunk = chunk_of(a, c);
   int base = 0;
   for (int s = 0; s <= a.b.S; s += 64) {
     int row0, n, len, tiles, range;
     seq_load(a, c, s + lane, row0, n, len, tiles, range);
-    const int splits = splits_of(range, it.chunk), mine = tiles * splits;
+    const int splits = splits_of(range, chunk), mine = tiles * splits;
     const int upto = wave_scan(mine);
     const uint64_t past = __builtin_amdgcn_ballot_w64(base + upto > idx);
     if (past) {
@@ -142,7 +155,7 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const Cut& c, int
       const int t = at / it.splits;
       it.tile = __builtin_amdgcn_readlane(tiles, l) - 1 - t;
       it.split = at - t * it.splits;
-      it.first_item = idx - it.split;
+      it.chunk = even_chunk(__builtin_amdgcn_readlane(range, l), it.splits);
       return true;
     }
     base += __builtin_amdgcn_readlane(upto, 63);
@@ -590,32 +603,35 @@ __device__ __forceinline__ void store_out(const AttendArgs& a, int row, int head
   *(uint2*)p = uint2{(uint32_t)H::bits(x) | (uint32_t)H::bits(y) << 16, (uint32_t)H::bits(z) | (uint32_t)H::bits(w) << 16};
 }
 
-// Partial results of an item (a.part): [blocks][cols][DHP] sums, [blocks][cols][2]
-// maxima (base 2) and weights' sums, [blocks] how many splits of the tile are live.
+// Partial results of the items (a.part): [blocks][cols][DHP] sums, [blocks][cols][2]
+// maxima (base 2) and weights' sums; and for each row and head the place of its
+// first split and how many there are (1: its result is written already).
 struct Part {
   float *o, *ml;
-  int* live;
+  int2* where;
 };
 __device__ __forceinline__ Part part_of(const AttendArgs& a, int blocks, int cols, int dhp) {
   Part p;
   p.o = a.part;
   p.ml = a.part + (size_t)blocks * cols * dhp;
-  p.live = (int*)(p.ml + (size_t)blocks * cols * 2);
+  p.where = (int2*)(p.ml + (size_t)blocks * cols * 2);
   return p;
 }
 
-// This block's item cut down to the keys [k0, k1) it is to look at; false: none.
-__device__ __forceinline__ bool cut_keys(const AttendArgs& a, const Item& it, const Part& part, int lo, int hi, int& k0, int& k1,
-                                         bool& alone) {
+// Cuts an item down to the keys [k0, k1) it is to look at; false: none.  live: the
+// splits of its tile that have keys.
+__device__ __forceinline__ bool cut_keys(const Item& it, int lo, int hi, int& k0, int& k1, int& live) {
   const int base = lo == kNoKey ? 0 : lo & ~63;
   hi = max(hi, base);
-  const int live = (int)(((int64_t)hi - base + it.chunk - 1) / it.chunk);
-  if (it.split > 0 && it.split >= live) return false;
-  alone = live <= 1;
-  if (it.splits > 1 && it.split == 0 && threadIdx.x == 0) part.live[blockIdx.x] = live;
+  live = max(1, (int)(((int64_t)hi - base + it.chunk - 1) / it.chunk));
+  if (it.split >= live) return false;
   k0 = base + it.split * it.chunk;
   k1 = (int)min((int64_t)hi, (int64_t)k0 + it.chunk);
   return true;
+}
+// The first split says where the results of a column (of its lane) are.
+__device__ __forceinline__ void tell_where(const AttendArgs& a, const Part& part, const Item& it, const Column& col, int at, int live) {
+  if (a.part && it.split == 0 && col.row >= 0) part.where[(int64_t)col.row * a.Hq + col.head] = int2{at, live};
 }
 
 // Many columns: four waves of 32 share the tiles of 64 keys (32 where a key is 256
@@ -648,9 +664,10 @@ __global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArg
   const int lo = min(min(red[0][0], red[1][0]), min(red[2][0], red[3][0]));
   const int hi = max(max(red[0][1], red[1][1]), max(red[2][1], red[3][1]));
   const Part part = part_of(a, blocks, kWideCols, DHP);
-  int k0, k1;
-  bool alone;
-  if (!cut_keys(a, it, part, lo, hi, k0, k1, alone)) return;
+  int k0, k1, live;
+  if (!cut_keys(it, lo, hi, k0, k1, live)) return;
+  const int at = blockIdx.x * kWideCols + wave * 32 + (lane & 31);
+  if (lane < 32) tell_where(a, part, it, col, at, live);
   Wave<DHP, BF16, NB, TURN> w;
   w.init(a, col, lane >> 5);
   const float slope = a.slopes && col.row >= 0 ? a.slopes[col.head] * kLog2e : 0.f;
@@ -711,7 +728,7 @@ __global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArg
   if (col.row < 0) return;
   const float l = other_half_sum(w.l), mb = w.m == -INFINITY ? -INFINITY : w.m * w.c;
   const int h = lane >> 5;
-  if (alone) {
+  if (live == 1) {
     const float f = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
     for (int d = 0; d < DHP / 32; ++d)
@@ -720,13 +737,12 @@ __global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArg
         store_out<BF16>(a, col.row, col.head, 32 * d + 2 * i + 4 * h, w.o[d][i] * f, w.o[d][i + 1] * f, w.o[d][i + 2] * f,
                         w.o[d][i + 3] * f);
   } else {
-    const size_t at = (size_t)blockIdx.x * kWideCols + wave * 32 + (lane & 31);
 #pragma unroll
     for (int d = 0; d < DHP / 32; ++d)
 #pragma unroll
       for (int i = 0; i < 16; i += 4)
-        *(float4*)(part.o + at * DHP + 32 * d + 2 * i + 4 * h) = float4{w.o[d][i], w.o[d][i + 1], w.o[d][i + 2], w.o[d][i + 3]};
-    if (h == 0) *(float2*)(part.ml + at * 2) = float2{mb, l};
+        *(float4*)(part.o + (size_t)at * DHP + 32 * d + 2 * i + 4 * h) = float4{w.o[d][i], w.o[d][i + 1], w.o[d][i + 2], w.o[d][i + 3]};
+    if (h == 0) *(float2*)(part.ml + (size_t)at * 2) = float2{mb, l};
   }
 }
 
@@ -753,9 +769,9 @@ __global__ __launch_bounds__(64 * few_waves<DHP>(), DHP == 256 ? 1 : 2) void att
   const Column col = column_of(a, it, it.tile * kFewCols + (lane & 31), kvh * (a.Hq / a.H));
   const Span sp = span_of(a, col);
   const Part part = part_of(a, blocks, kFewCols, DHP);
-  int k0, k1;
-  bool alone;
-  if (!cut_keys(a, it, part, sp.lo, sp.hi, k0, k1, alone)) return;
+  int k0, k1, live;
+  if (!cut_keys(it, sp.lo, sp.hi, k0, k1, live)) return;
+  if (tid < 32) tell_where(a, part, it, col, blockIdx.x * kFewCols + lane, live);
   Wave<DHP, BF16, 1, TURN> w;
   w.init(a, col, lane >> 5);
   const float slope = a.slopes && col.row >= 0 ? a.slopes[col.head] * kLog2e : 0.f;
@@ -842,7 +858,7 @@ __global__ __launch_bounds__(64 * few_waves<DHP>(), DHP == 256 ? 1 : 2) void att
         q += f * t.w;
       }
     }
-    if (alone) {
+    if (live == 1) {
       const float f = sum == 0.f ? 0.f : 1.f / sum;
       const int mm = it.tile * kFewCols + r, i = mm / G_;
       store_out<BF16>(a, it.row0 + i, kvh * G_ + (mm - i * G_), piece * 4, x * f, y * f, z * f, q * f);
@@ -854,56 +870,70 @@ __global__ __launch_bounds__(64 * few_waves<DHP>(), DHP == 256 ? 1 : 2) void att
   }
 }
 
-// Joins the splits of each row and head: a wave each, its lanes over the dimensions.
-template <int DHP, bool BF16>
-__global__ __launch_bounds__(256) void attend_join(AttendArgs a, Cut cut, int blocks) {
+// Joins the splits of each row and head: NW waves each, which take them by turns,
+// their lanes over the dimensions.
+template <int DHP, bool BF16, int NW>
+__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void attend_join(AttendArgs a, int cols, int blocks) {
+  constexpr int VL = DHP / 64;  // dimensions per lane
+  typedef float vec __attribute__((ext_vector_type(VL)));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t at = (int64_t)blockIdx.x * 4 + wave;
-  const int row = (int)(at / a.Hq), head = (int)(at - (int64_t)row * a.Hq);
-  if (row >= a.b.T) return;
-  const int sq = seq_of_row(a.b, row);
-  if (sq >= a.b.S) return;  // written by its only item
-  const int chunk = chunk_of(a, cut);
-  int base = 0, row0 = 0, tiles = 0, splits = 1;
-  for (int s = 0; s <= sq; s += 64) {
-    int r0, n, len, ts, range;
-    seq_load(a, cut, s + lane, r0, n, len, ts, range);
-    const int sp = splits_of(range, chunk), upto = wave_scan(ts * sp);
-    if (sq < s + 64) {
-      const int l = sq - s;
-      row0 = __builtin_amdgcn_readlane(r0, l);
-      tiles = __builtin_amdgcn_readlane(ts, l);
-      splits = __builtin_amdgcn_readlane(sp, l);
-      base += __builtin_amdgcn_readlane(upto, l) - tiles * splits;
-    } else {
-      base += __builtin_amdgcn_readlane(upto, 63);
-    }
-  }
-  if (splits <= 1) return;
-  const int G = a.Hq / a.H, kvh = head / G;
-  const int m = (row - row0) * G + head - kvh * G;
-  const int tile = m / cut.cols;
-  const int first = base + (tiles - 1 - tile) * splits;
-  const Part part = part_of(a, blocks, cut.cols, DHP);
-  const int live = part.live[(int64_t)first * a.H + kvh];
+  const int64_t rh = NW == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
+  const int first = NW == 1 ? 0 : wave;
+  if (rh >= (int64_t)a.b.T * a.Hq) return;
+  const Part part = part_of(a, blocks, cols, DHP);
+  const int2 where = part.where[rh];
+  const int live = where.y;
   if (live <= 1) return;
-  const auto place = [&](int sp) { return ((size_t)(first + sp) * a.H + kvh) * cut.cols + (m - tile * cut.cols); };
-  float top = -INFINITY;
-  for (int i = lane; i < live; i += 64) top = fmaxf(top, part.ml[place(i) * 2]);
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-  constexpr int VL = DHP >= 256 ? 4 : DHP / 64;  // dimensions per lane
-  float sum = 0.f, x[VL] = {};
-#pragma unroll 4
-  for (int i = 0; i < live; ++i) {
-    const size_t p = place(i);
-    const float mi = part.ml[p * 2], li = part.ml[p * 2 + 1];
-    const float f = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mi - top);
-    if (mi > -INFINITY || !(li == 0.f)) {
-      sum += f * li;
+  const int64_t step = (int64_t)a.H * cols;  // places from one split to the next
+  float top = -INFINITY, sum = 0.f;
+  float x[VL] = {};
+  for (int s0 = first; s0 < live; s0 += 64 * NW) {
+    const int mine = s0 + lane * NW, n = min(64, (live - s0 + NW - 1) / NW);
+    float2 ml = float2{-INFINITY, 0.f};
+    if (mine < live) ml = *(const float2*)(part.ml + (where.x + mine * step) * 2);
+    float t = ml.x;
+    for (int o = 32; o > 0; o >>= 1) t = fmaxf(t, __shfl_xor(t, o));
+    t = fmaxf(t, top);
+    const float old = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - t);
+    // (nothing seen: no weight; but a NaN is handed on)
+    const float f = ml.x > -INFINITY ? __builtin_amdgcn_exp2f(ml.x - t) : ml.y == 0.f ? 0.f : 1.f;
+    sum = sum * old + wave_sum(f * ml.y);
+    top = t;
 #pragma unroll
-      for (int j = 0; j < VL; ++j) x[j] += f * part.o[p * DHP + lane * VL + j];
+    for (int j = 0; j < VL; ++j) x[j] *= old;
+    const float* o = part.o + (where.x + s0 * step) * DHP + lane * VL;
+#pragma unroll 8
+    for (int i = 0; i < n; ++i) {
+      const vec v = *(const vec*)(o + i * NW * step * DHP);
+      const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i));
+#pragma unroll
+      for (int j = 0; j < VL; ++j) x[j] += fi == 0.f ? 0.f : fi * v[j];
     }
   }
+  if constexpr (NW > 1) {
+    __shared__ float so[NW][DHP], st[NW][2];
+#pragma unroll
+    for (int j = 0; j < VL; ++j) so[wave][lane * VL + j] = x[j];
+    if (lane == 0) {
+      st[wave][0] = top;
+      st[wave][1] = sum;
+    }
+    __syncthreads();
+    if (wave != 0) return;
+    const int waves = min(NW, live);
+    for (int w = 0; w < waves; ++w) top = fmaxf(top, st[w][0]);
+    sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < VL; ++j) x[j] = 0.f;
+    for (int w = 0; w < waves; ++w) {
+      const float f = st[w][0] > -INFINITY ? __builtin_amdgcn_exp2f(st[w][0] - top) : st[w][1] == 0.f ? 0.f : 1.f;
+      if (f == 0.f) continue;
+      sum += f * st[w][1];
+#pragma unroll
+      for (int j = 0; j < VL; ++j) x[j] += f * so[w][lane * VL + j];
+    }
+  }
+  const int row = (int)(rh / a.Hq), head = (int)(rh - (int64_t)row * a.Hq);
   const float f = sum == 0.f ? 0.f : 1.f / sum;
   uint16_t* out = (uint16_t*)a.out + (int64_t)row * a.out_row + head * a.out_head;
 #pragma unroll
@@ -928,10 +958,11 @@ Plan plan_of(const AttendArgs& a) {
   p.cut.cols = p.few ? kFewCols : kWideCols;
   const int64_t most = cols / p.cut.cols + std::min(a.b.S + 1, a.b.T);  // tiles there can be
   const int64_t likely = std::max<int64_t>(seqs, (cols + p.cut.cols - 1) / p.cut.cols);
-  const int target = p.few ? 512 : 768;
+  // workgroups at once: by the registers of a kernel's waves and the LDS of its tiles
+  const int dim = padded_dim(a.D), slots = 256 * (dim == 64 ? 3 : dim == 128 ? 2 : 1);
   p.cut.min_chunk = p.few ? 128 : 256;
-  p.cut.target = likely * a.H < target ? target : 0;
-  const int64_t items = p.cut.target ? 2 * most + target / a.H + 9 : most;
+  p.cut.slots = likely * a.H < 3 * slots ? slots : 0;
+  const int64_t items = p.cut.slots ? 2 * most + (3 * slots / 2) / a.H + 9 : most;
   p.blocks = (int)(items * a.H);
   return p;
 }
@@ -965,9 +996,10 @@ template <int DHP, bool BF16>
 hipError_t launch_dh(const AttendArgs& a, const Plan& p, hipStream_t s) {
   const bool turn = a.cap > 0.f || a.slopes || !(a.scale > 0.f);
   hipError_t e = turn ? launch_kernel<DHP, BF16, true>(a, p, s) : launch_kernel<DHP, BF16, false>(a, p, s);
-  if (e == hipSuccess && p.cut.target) {
-    const int64_t waves = (int64_t)a.b.T * a.Hq;
-    hvd_launch((attend_join<DHP, BF16>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, a, p.cut, p.blocks);
+  if (e == hipSuccess && p.cut.slots) {
+    const int64_t n = (int64_t)a.b.T * a.Hq;
+    if (n >= 1024) hvd_launch((attend_join<DHP, BF16, 1>), dim3((unsigned)((n + 3) / 4)), dim3(256), 0, s, a, p.cut.cols, p.blocks);
+    else hvd_launch((attend_join<DHP, BF16, 8>), dim3((unsigned)n), dim3(512), 0, s, a, p.cut.cols, p.blocks);
     e = hipGetLastError();
   }
   return e;
@@ -977,8 +1009,8 @@ hipError_t launch_dh(const AttendArgs& a, const Plan& p, hipStream_t s) {
 
 size_t attend_workspace(const AttendArgs& a) {
   const Plan p = plan_of(a);
-  if (!p.cut.target) return 0;
-  return (size_t)p.blocks * (p.cut.cols * (padded_dim(a.D) + 2) + 1) * sizeof(float);
+  if (!p.cut.slots) return 0;
+  return (size_t)p.blocks * p.cut.cols * (padded_dim(a.D) + 2) * sizeof(float) + (size_t)a.b.T * a.Hq * sizeof(int2);
 }
 
 hipError_t launch_attend(const AttendArgs& a, hipStream_t s) {
