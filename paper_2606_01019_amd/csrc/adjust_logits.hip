@@ -18,10 +18,17 @@
 // counts live in LDS, a word per token: bits 0-19 the count n, 20-30 the entry
 // of the bias list + 1 (the later entry wins), 31 "in the history's prompt".
 // A sequence's history is counted once for its rows of the run (integer
-// atomics: no order matters), a row's path is added and taken away.
+// atomics: no order matters); from row to row the words follow the path.
+//
+// Bound by memory for many rows: a row's logits of the part are on their way to
+// registers before the words are ready, and only touched tokens cost more than
+// a copy.  845 rows of 128256 32-bit logits, everything given: 240 us, 3.9 TB/s
+// (a large copy: 4.7); one row, 16 us, bound by the call itself (kernels: 8).
 #include "common.h"
 #include "kernels.h"
 #include "rows.h"
+
+#include <algorithm>
 
 namespace hvd {
 namespace {
@@ -35,20 +42,6 @@ constexpr uint32_t kCount = (1u << 20) - 1;
 typedef uint16_t u16x8_a2 __attribute__((ext_vector_type(8), aligned(2)));
 typedef float f32x4_e __attribute__((ext_vector_type(4), aligned(4)));
 
-__device__ __forceinline__ void load8(const void* p, int64_t i, int type, float (&v)[8]) {
-  if (type == ET_F32) {
-    const f32x4_e a = *(const f32x4_e*)((const float*)p + i), b = *(const f32x4_e*)((const float*)p + i + 4);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      v[j] = a[j];
-      v[4 + j] = b[j];
-    }
-  } else {
-    const u16x8_a2 a = *(const u16x8_a2*)((const uint16_t*)p + i);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = type == ET_BF16 ? bf2f(a[j]) : h2f(a[j]);
-  }
-}
 __device__ __forceinline__ float load1(const void* p, int64_t i, int type) {
   if (type == ET_F32) return ((const float*)p)[i];
   const uint16_t b = ((const uint16_t*)p)[i];
@@ -74,8 +67,8 @@ __device__ __forceinline__ void store1(void* p, int64_t i, int type, float v) {
   else ((uint16_t*)p)[i] = half_bits(v, type);
 }
 
-// Larger for a larger value, then for a lower token; 0 for a value that is
-// never chosen (-inf, NaN).  Both zeros count as equal.
+// Larger for a larger value, then for a lower token; 0 for a value that is never
+// chosen (-inf, NaN).  Both zeros count as equal.
 __device__ __forceinline__ uint64_t rank_of(float v, int token) {
   if (!(v > -INFINITY)) return 0;
   const uint32_t u = __float_as_uint(v + 0.f);
@@ -88,6 +81,28 @@ __device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
     v = w > v ? w : v;
   }
   return v;
+}
+template <int CTRL>
+__device__ __forceinline__ float dpp_f(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float wave_max_f(float v) {
+  v = fmaxf(v, dpp_f<0xB1>(v));
+  v = fmaxf(v, dpp_f<0x4E>(v));
+  v = fmaxf(v, dpp_f<0x141>(v));
+  v = fmaxf(v, dpp_f<0x140>(v));
+  return rows_max(v);
+}
+
+__device__ __forceinline__ int wave_min_i(int v) {
+  v = min(v, __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, false));
+  v = min(v, __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xf, 0xf, false));
+  v = min(v, __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, false));
+  v = min(v, __builtin_amdgcn_update_dpp(0, v, 0x140, 0xf, 0xf, false));
+  const auto a = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+  v = min((int)a[0], (int)a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+  return min((int)b[0], (int)b[1]);
 }
 
 struct Penalty {
@@ -108,49 +123,125 @@ __device__ __forceinline__ float adjusted(float x, uint32_t w, const Penalty& p)
   return x;
 }
 
-__global__ __launch_bounds__(kThreads) void adjust_rows(AdjustArgs a, int seg, int segs, int run) {
+// Eight logits of one row.
+template <int TYPE>
+struct Octet {
+  f32x4_e a, b;
+  __device__ __forceinline__ void load(const void* p, int64_t at) {
+    a = *(const f32x4_e*)((const float*)p + at);
+    b = *(const f32x4_e*)((const float*)p + at + 4);
+  }
+  __device__ __forceinline__ void values(float (&x)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[j] = a[j];
+      x[4 + j] = b[j];
+    }
+  }
+};
+template <int TYPE>
+struct HalfOctet {
+  u16x8_a2 a;
+  __device__ __forceinline__ void load(const void* p, int64_t at) { a = *(const u16x8_a2*)((const uint16_t*)p + at); }
+  __device__ __forceinline__ void values(float (&x)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = TYPE == ET_BF16 ? bf2f(a[j]) : h2f(a[j]);
+  }
+};
+template <>
+struct Octet<ET_F16> : HalfOctet<ET_F16> {};
+template <>
+struct Octet<ET_BF16> : HalfOctet<ET_BF16> {};
+
+// The words of a sequence's history: 16 tokens per thread at once.
+__device__ __forceinline__ void count_history(const AdjustArgs& a, int s, int v0, int nv, uint32_t* word) {
+  typedef int32_t i32x4_e __attribute__((ext_vector_type(4), aligned(4)));
+  const int n = min(max(a.history_lengths[s], 0), a.max_history);
+  const int prompt = a.prompt_lengths ? a.prompt_lengths[s] : 0;
+  const int32_t* h = a.history + s * a.history_stride;
+  constexpr int U = 4;
+  for (int i0 = threadIdx.x * 4; i0 < n; i0 += kThreads * 4 * U) {
+    i32x4_e t[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * kThreads * 4;
+      t[u] = i32x4_e{-1, -1, -1, -1};
+      if (i + 4 <= n) {
+        t[u] = *(const i32x4_e*)(h + i);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+          if (i + j < n) t[u][j] = h[i + j];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int d = t[u][j] - v0;
+        if (t[u][j] >= 0 && (unsigned)d < (unsigned)nv) {
+          if (i0 + u * kThreads * 4 + j < prompt) atomicOr(&word[d], kPrompt);
+          else atomicAdd(&word[d], 1u);
+        }
+      }
+  }
+}
+
+// CH octets of logits per thread: a part has 2048 CH tokens, octet i of thread t
+// starts at token (i * 256 + t) * 8 of it; the vocabulary's last tokens, where
+// they are no octet, go one to a thread.
+template <int CH, int TYPE>
+__global__ __launch_bounds__(kThreads, 4) void adjust_rows(AdjustArgs a, int segs, int run) {
   extern __shared__ __attribute__((aligned(16))) uint32_t word[];
-  __shared__ uint64_t red[2][kThreads / 64];  // by turns: a row is read while the next one is written
+  __shared__ float2 red[2][kThreads / 64];  // by turns: a row is read while the next one is written
+  constexpr int SEG = CH * kThreads * 8;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int part = blockIdx.x % segs;
-  const int v0 = part * seg, nv = min(seg, a.V - v0);
+  const int v0 = part * SEG, nv = min(SEG, a.V - v0), nv8 = nv & ~7;
   const int r0 = blockIdx.x / segs * run, r1 = min(r0 + run, a.b.T);
   const bool counts = a.repetition || a.frequency || a.presence;
-  const bool words = counts || a.n_bias > 0;
-  auto bump = [&](int token, uint32_t by) __attribute__((always_inline)) {
+  const bool words = counts || a.n_bias > 0, path = counts && a.tokens;
+  const auto clear = [&]() __attribute__((always_inline)) {
+    for (int i = tid * 4; i < SEG; i += kThreads * 4) *(uint4*)&word[i] = uint4{0, 0, 0, 0};
+  };
+  const auto bump = [&](int token, uint32_t by) __attribute__((always_inline)) {
     const int d = token - v0;
     if ((unsigned)d < (unsigned)nv) atomicAdd(&word[d], by);
   };
-  int held = -1;  // the sequence whose words are in LDS
-  int b = 0, e = 0;
+  if (words) clear();
+  bool live = false;
+  int b = 0, e = 0;        // rows of the sequence whose words are in LDS
+  uint64_t on_path = 0;    // its rows that are counted in them (tree)
+  int my_token = -1;       // of row b + tid (tree)
   Penalty p{};
   for (int row = r0; row < r1; ++row) {
-    const int s = seq_of_row(a.b, row);
-    const bool live = s < a.b.S;
-    uint64_t mask = 0;
-    if (live) {
-      seq_rows(a.b, s, b, e);
-      if (counts && a.b.tree) mask = a.b.tree[row];
-      if (s != held) {
+    // (octets past the part's end are not used: any other in their place)
+    Octet<TYPE> raw[CH];
+    const auto load = [&]() __attribute__((always_inline)) {
+      if (nv8 > 0) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) raw[i].load(a.logits, row * a.logits_stride + v0 + min((i * kThreads + tid) * 8, nv8 - 8));
+      }
+    };
+    // on their way while the words are made, where registers allow it
+    constexpr bool kEarly = CH * (TYPE == ET_F32 ? 2 : 1) <= 4;
+    if (kEarly) load();
+    if (row == r0 || (live && row >= e)) {
+      const int s = seq_of_row(a.b, row);
+      live = s < a.b.S;
+      if (live) {
+        seq_rows(a.b, s, b, e);
         if (words) {
-          __syncthreads();
-          for (int i = tid; i < nv; i += kThreads) word[i] = 0;
+          if (row != r0) clear();  // (every wave has read them: the barrier at a row's end)
           __syncthreads();
         }
-        if (counts && a.history) {
-          const int n = min(max(a.history_lengths[s], 0), a.max_history);
-          const int prompt = a.prompt_lengths ? a.prompt_lengths[s] : 0;
-          const int32_t* h = a.history + s * a.history_stride;
-          for (int i = tid; i < n; i += kThreads) {
-            const int d = h[i] - v0;
-            if ((unsigned)d < (unsigned)nv) {
-              if (i < prompt) atomicOr(&word[d], kPrompt);
-              else atomicAdd(&word[d], 1u);
-            }
-          }
+        if (counts && a.history) count_history(a, s, v0, nv, word);
+        if (path) {
+          on_path = 0;
+          if (a.b.tree) my_token = tid < 64 && b + tid < e ? a.tokens[b + tid] : -1;
+          else
+            for (int i = b + tid; i < row; i += kThreads) bump(a.tokens[i], 1u);
         }
-        if (counts && a.tokens && !a.b.tree)
-          for (int i = b + tid; i < row; i += kThreads) bump(a.tokens[i], 1u);
         for (int i = tid; i < a.n_bias; i += kThreads) {
           const int d = a.bias_ids[s * a.bias_ids_stride + i] - v0;
           if ((unsigned)d < (unsigned)nv) {
@@ -162,7 +253,6 @@ __global__ __launch_bounds__(kThreads) void adjust_rows(AdjustArgs a, int seg, i
             }
           }
         }
-        held = s;
         p.rep = a.repetition != nullptr;
         p.freq = a.frequency != nullptr;
         p.pres = a.presence != nullptr;
@@ -171,62 +261,88 @@ __global__ __launch_bounds__(kThreads) void adjust_rows(AdjustArgs a, int seg, i
         p.presence = p.pres ? a.presence[s] : 0.f;
         p.bias = a.bias + s * a.bias_stride;
       }
-      if (counts && a.tokens) {
-        if (!a.b.tree) {
-          if (tid == 0) bump(a.tokens[row], 1u);
-        } else if (tid < 64 && (mask >> tid & 1) && b + tid < e) {
-          bump(a.tokens[b + tid], 1u);
+    }
+    if (!kEarly) load();
+    if (live) {
+      if (path) {
+        if (a.b.tree) {  // from the last row's path to this one's
+          const uint64_t mask = (uint64_t)a.b.tree[row], change = mask ^ on_path;
+          if (tid < 64 && (change >> lane & 1)) bump(my_token, mask >> lane & 1 ? 1u : ~0u);
+          on_path = mask;
+        } else if (tid == 0) {
+          bump(a.tokens[row], 1u);
         }
       }
       if (words) __syncthreads();
     }
-    const int64_t in = row * a.logits_stride + v0, to = row * a.out_stride + v0;
+    const int64_t to = row * a.out_stride + v0;
     const int32_t* ok = live && a.allowed ? a.allowed + row * a.allowed_stride : nullptr;
-    uint64_t best = 0;
-    for (int c = tid * 8; c < nv; c += kThreads * 8) {
-      const int v = v0 + c;
-      const uint32_t bits = ok ? (uint32_t)ok[v >> 5] >> (v & 31) : 0xffu;
-      if (c + 8 <= nv) {
-        float x[8];
-        load8(a.logits, in + c, a.type, x);
-        if (live && words) {
-          const uint4 wa = *(const uint4*)&word[c], wb = *(const uint4*)&word[c + 4];
-          const uint32_t w[8] = {wa.x, wa.y, wa.z, wa.w, wb.x, wb.y, wb.z, wb.w};
+    float top = -INFINITY;  // the thread's largest and its first place: 8 i + j, 8 CH for the single token
+    int place = 0;
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (w[j]) x[j] = adjusted(x[j], w[j], p);
-        }
+    for (int i = 0; i < CH; ++i) {
+      __builtin_amdgcn_sched_barrier(0);  // one octet at a time: registers
+      const int c = (i * kThreads + tid) * 8;
+      if (c >= nv8) break;
+      float x[8];
+      raw[i].values(x);
+      if (live && words) {
+        const uint4 wa = *(const uint4*)&word[c], wb = *(const uint4*)&word[c + 4];
+        const uint32_t w[8] = {wa.x, wa.y, wa.z, wa.w, wb.x, wb.y, wb.z, wb.w};
+        uint32_t touched = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (!(bits >> j & 1)) x[j] = -INFINITY;
-        if (a.out) store8(a.out, to + c, a.type, x);
+        for (int j = 0; j < 8; ++j) touched |= w[j] ? 1u << j : 0;
+        while (touched) {  // few are: one at a time
+          const int j = __builtin_ctz(touched);
+          touched &= touched - 1;
+          float v = x[0];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const uint64_t k = rank_of(x[j], v + j);
-          best = k > best ? k : best;
+          for (int q = 1; q < 8; ++q) v = j == q ? x[q] : v;
+          v = adjusted(v, word[c + j], p);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) x[q] = j == q ? v : x[q];
         }
-      } else {
-        for (int j = 0; c + j < nv; ++j) {
-          float x = load1(a.logits, in + c + j, a.type);
-          if (live && words && word[c + j]) x = adjusted(x, word[c + j], p);
-          if (!(bits >> j & 1)) x = -INFINITY;
-          if (a.out) store1(a.out, to + c + j, a.type, x);
-          const uint64_t k = rank_of(x, v + j);
-          best = k > best ? k : best;
-        }
+      }
+      if (ok) {
+        const uint32_t bits = (uint32_t)ok[(v0 + c) >> 5] >> (c & 31);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = bits >> j & 1 ? x[j] : -INFINITY;
+      }
+      if (a.out) store8(a.out, to + c, TYPE, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const bool more = x[j] > top;
+        top = more ? x[j] : top;
+        place = more ? 8 * i + j : place;
+      }
+    }
+    if (nv8 + tid < nv) {
+      const int c = nv8 + tid;
+      float x = load1(a.logits, row * a.logits_stride + v0 + c, TYPE);
+      if (live && words && word[c]) x = adjusted(x, word[c], p);
+      if (ok && !((uint32_t)ok[(v0 + c) >> 5] >> (c & 31) & 1)) x = -INFINITY;
+      if (a.out) store1(a.out, to + c, TYPE, x);
+      if (x > top) {
+        top = x;
+        place = 8 * CH;
       }
     }
     if (a.best) {
-      best = wave_max_u64(best);
-      if (lane == 0) red[row & 1][wave] = best;
+      const int token = v0 + (place == 8 * CH ? nv8 + tid : ((place >> 3) * kThreads + tid) * 8 + (place & 7));
+      const float most = wave_max_f(top);
+      const int lowest = wave_min_i(top == most ? token : 0x7fffffff);
+      if (lane == 0) red[row & 1][wave] = float2{most, __int_as_float(lowest)};
     }
     __syncthreads();
     if (a.best && tid == 0) {
-      for (int w = 1; w < kThreads / 64; ++w) best = red[row & 1][w] > best ? red[row & 1][w] : best;
-      a.part[(int64_t)row * segs + part] = live ? best : 0;
+      uint64_t k = 0;
+#pragma unroll
+      for (int w = 0; w < kThreads / 64; ++w) {
+        const uint64_t r = rank_of(red[row & 1][w].x, __float_as_int(red[row & 1][w].y));
+        k = r > k ? r : k;
+      }
+      a.part[(int64_t)row * segs + part] = live ? k : 0;
     }
-    // a tree's next row starts without this one's path
-    if (live && counts && a.tokens && a.b.tree && tid < 64 && (mask >> tid & 1) && b + tid < e) bump(a.tokens[b + tid], ~0u);
   }
 }
 
@@ -244,13 +360,29 @@ __global__ __launch_bounds__(kThreads) void best_of_parts(const uint64_t* part, 
 
 // The vocabulary's parts and the rows of a workgroup.
 struct Plan {
-  int seg, segs, run;
+  bool small;  // parts of 2048 tokens
+  int segs, run;
 };
 Plan plan_of(const AdjustArgs& a) {
-  const int seg = a.b.T <= 8 ? 2048 : 8192;
+  const bool small = a.b.T <= 8;
+  const int seg = small ? 2048 : 8192;
   const int segs = (a.V + seg - 1) / seg;
-  const int run = std::min(16, std::max(1, (int)((int64_t)a.b.T * segs / 2048)));
-  return Plan{seg, segs, run};
+  const int run = std::min(16, std::max(1, (int)((int64_t)a.b.T * segs / 4096)));
+  return Plan{small, segs, run};
+}
+
+template <int CH, int TYPE>
+void launch_type(const AdjustArgs& a, const Plan& p, hipStream_t s) {
+  const bool words = a.repetition || a.frequency || a.presence || a.n_bias > 0;
+  const int groups = (a.b.T + p.run - 1) / p.run;
+  hvd_launch((adjust_rows<CH, TYPE>), dim3((unsigned)(groups * p.segs)), dim3(kThreads), words ? CH * kThreads * 8 * 4 : 0, s, a,
+             p.segs, p.run);
+}
+template <int CH>
+void launch_ch(const AdjustArgs& a, const Plan& p, hipStream_t s) {
+  if (a.type == ET_F32) launch_type<CH, ET_F32>(a, p, s);
+  else if (a.type == ET_F16) launch_type<CH, ET_F16>(a, p, s);
+  else launch_type<CH, ET_BF16>(a, p, s);
 }
 
 }  // namespace
@@ -259,9 +391,8 @@ size_t adjust_workspace(const AdjustArgs& a) { return (size_t)a.b.T * plan_of(a)
 
 hipError_t launch_adjust_logits(const AdjustArgs& a, hipStream_t s) {
   const Plan p = plan_of(a);
-  const int groups = (a.b.T + p.run - 1) / p.run;
-  const bool words = a.repetition || a.frequency || a.presence || a.n_bias > 0;
-  hvd_launch(adjust_rows, dim3((unsigned)(groups * p.segs)), dim3(kThreads), words ? p.seg * 4 : 0, s, a, p.seg, p.segs, p.run);
+  if (p.small) launch_ch<1>(a, p, s);
+  else launch_ch<4>(a, p, s);
   if (a.best)
     hvd_launch(best_of_parts, dim3((a.b.T + 3) / 4), dim3(kThreads), 0, s, (const uint64_t*)a.part, p.segs, a.b.T, a.best);
   return hipGetLastError();
