@@ -39,6 +39,7 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLazy = 8.f;     // the running maximum may lag by this (base 2)
+constexpr float kCancels = 64.f;
 constexpr int kNoKey = 0x7fffffff;
 
 template <bool BF16>
@@ -305,23 +306,33 @@ template <int DHP, int N>
 struct Copies {
   using G = Geo<DHP>;
   static constexpr int PER = N * G::KPI < 16 ? N : 16 / G::KPI;  // copies per group
-  uint32_t k_off[PER], v_off[PER];  // of this lane, from the first key's place
-  int piece[PER];
+  static constexpr bool KEEP = DHP < 256;  // a wide head's sums leave no registers for every copy's place
+  int place;  // of this lane: its piece of the first key, in bytes
+  uint32_t k_off[KEEP ? PER : 1], v_off[KEEP ? PER : 1];  // from the first key's place
 
   // k0: the first key's place in the tile (of a group, or of this part of one)
   __device__ __forceinline__ void init(const AttendArgs& a, int k0) {
     const int lane = threadIdx.x & 63, kk = lane / G::CH;
+    place = ((lane % G::CH) ^ G::swz(k0 + kk)) * 16;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int k = i * G::KPI + kk;
-      piece[i] = (lane % G::CH) ^ G::swz(k0 + k);
-      k_off[i] = 2u * (uint32_t)(k * (int)a.k.tok + piece[i] * 8);
-      v_off[i] = 2u * (uint32_t)(k * (int)a.v.tok + piece[i] * 8);
+    for (int i = 0; i < (KEEP ? PER : 1); ++i) {
+      k_off[i] = 2u * (uint32_t)((i * G::KPI + kk) * (int)a.k.tok) + (KEEP ? piece(i) : 0);
+      v_off[i] = 2u * (uint32_t)((i * G::KPI + kk) * (int)a.v.tok) + (KEEP ? piece(i) : 0);
     }
+  }
+  // The lane's piece in copy i of a group (a key's swizzle is linear in its bits).
+  __device__ __forceinline__ uint32_t piece(int i) const {
+    return (uint32_t)((KEEP ? place : afresh(place)) ^ (G::swz(i * G::KPI) * 16));
+  }
+  // Copy i of keys or values: from `from`, a group's first key.
+  __device__ __forceinline__ void copy(int i, const char* from, int64_t tok, const uint32_t* off, uint32_t to) const {
+    if constexpr (KEEP) copy_to_lds(from, off[i], to);
+    else copy_to_lds(from + 2u * i * G::KPI * (uint32_t)tok, off[0] + piece(i), to);
   }
 
   // The tile begins with key0; group g0 of `pg` is its first, `good` its keys that
-  // have a page.  Returns false if fewer than 2 N copies were asked for.
+  // have a page.  Returns false if fewer than N copies (of each) were asked for.
+  template <bool K = true, bool V = true>
   __device__ __forceinline__ bool issue(const AttendArgs& a, const char* kb, const char* vb, int key0, int k0, const Pages& pg, int g0,
                                         uint64_t good, unsigned char* smem, uint32_t lk, uint32_t lv) const {
     constexpr uint64_t kMine = N * G::KPI >= 64 ? ~0ull : (1ull << (N * G::KPI & 63)) - 1;
@@ -339,8 +350,8 @@ struct Copies {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
           const uint32_t at = (first + i * G::KPI) * G::ROW;
-          copy_to_lds(kp, k_off[i], base + lk + at);
-          copy_to_lds(vp, v_off[i], base + lv + at);
+          if constexpr (K) copy(i, kp, a.k.tok, k_off, base + lk + at);
+          if constexpr (V) copy(i, vp, a.v.tok, v_off, base + lv + at);
         }
       } else {
         // pieces past the head dimension stay zero, keys without a page become it
@@ -348,14 +359,14 @@ struct Copies {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
           const uint32_t at = (first + i * G::KPI) * G::ROW;
-          const bool in = piece[i] * 8 < a.D, ok = good >> (first + i * G::KPI + lane / G::CH) & 1;
+          const bool in = (int)piece(i) < 2 * a.D, ok = good >> (first + i * G::KPI + lane / G::CH) & 1;
           if (in && ok) {
-            copy_to_lds(kp, k_off[i], base + lk + at);
-            copy_to_lds(vp, v_off[i], base + lv + at);
+            if constexpr (K) copy(i, kp, a.k.tok, k_off, base + lk + at);
+            if constexpr (V) copy(i, vp, a.v.tok, v_off, base + lv + at);
           }
           if (in && !ok) {
-            *(uint4*)(smem + lk + at + lane * 16) = uint4{0, 0, 0, 0};
-            *(uint4*)(smem + lv + at + lane * 16) = uint4{0, 0, 0, 0};
+            if constexpr (K) *(uint4*)(smem + lk + at + lane * 16) = uint4{0, 0, 0, 0};
+            if constexpr (V) *(uint4*)(smem + lv + at + lane * 16) = uint4{0, 0, 0, 0};
           }
         }
       }
@@ -403,6 +414,127 @@ struct Wave {
     }
   }
 
+  // Scores become base-2 exponents (with a factor c of 1) by a cap and a bias.
+  __device__ __forceinline__ void turn(const AttendArgs& a, const Column& col, int key0, float slope, f32x16 (&s)[NB]) {
+    const int h = (threadIdx.x & 63) >> 5;
+    if (a.cap > 0.f) {
+      // tanh y = 1 - 2 / (exp 2y + 1).  Near 0 that cancels: off by 2^-22, which up to
+      // this cap is 2^-16 of a weight; past it the series takes over there
+      const float cl = a.cap * kLog2e, inv = fminf(fmaxf(a.scale / a.cap, -1e38f), 1e38f);
+      const float two = inv * (2.f * kLog2e);
+      if (a.cap <= kCancels) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            s[b][i] = __builtin_fmaf(-2.f * cl, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[b][i] * two) + 1.f), cl);
+      } else {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float y = s[b][i] * inv, y2 = y * y;
+            const float far = 1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[b][i] * two) + 1.f);
+            const float near = y * (1.f + y2 * (-1.f / 3.f + y2 * (2.f / 15.f - y2 * (17.f / 315.f))));
+            s[b][i] = cl * (fabsf(y) < 0.25f ? near : far);
+          }
+      }
+    } else {
+      const float f = a.scale * kLog2e;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[b][i] *= f;
+    }
+    if (a.slopes) {
+      const float apart = (float)(col.pos - key0 - 4 * h);
+      if (a.b.tree && key0 + 32 * NB > col.ctx) {  // this step's keys stand at the positions of their depth
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int k = 32 * b + 8 * (i >> 2) + (i & 3), j = key0 + 4 * h + k - col.ctx;
+            const int d = col.pos - col.ctx - __builtin_popcountll(col.path & below(j));
+            s[b][i] -= slope * fabsf(j >= 0 ? (float)d : apart - (float)k);
+          }
+      } else {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[b][i] -= slope * fabsf(apart - (float)(32 * b + 8 * (i >> 2) + (i & 3)));
+      }
+    }
+  }
+
+  // -inf for keys that the column does not see.
+  __device__ __forceinline__ void hide(const AttendArgs& a, const Column& col, int key0, uint64_t good, f32x16 (&s)[NB]) {
+    const int h = (threadIdx.x & 63) >> 5;
+    // bit k: key k of the tile is seen
+    uint64_t see = below(col.hi - key0) & ~below(col.lo - key0);
+    if (a.b.tree) {
+      const int from = key0 - col.ctx;
+      see |= from >= 64 || from <= -64 ? 0 : from >= 0 ? col.see >> from : col.see << -from;
+    }
+    see = (see & good) >> (4 * h);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        s[b][i] = ((uint32_t)(see >> (32 * b)) & 1u << (8 * (i >> 2) + (i & 3))) ? s[b][i] : -INFINITY;
+  }
+
+  // Has the maximum and the sums up to date with a tile's scores; what they lack to a
+  // weight's exponent.
+  template <bool APART>
+  __device__ __forceinline__ float follow(const f32x16 (&s)[NB]) {
+    float top = s[0][0];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+    top = other_half_max(top);
+    // The maximum lags until a weight would pass 2^kLazy: most tiles rescale nothing
+    if (__builtin_amdgcn_ballot_w64(top * c > m * c + kLazy)) {
+      if constexpr (APART) keep_apart();
+      const float mn = fmaxf(m, top);
+      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * c);
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < DHP / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] *= f;
+      if constexpr (APART) keep_apart();
+      m = mn;
+    }
+    return (m == -INFINITY ? 0.f : m * c) - H::kShift;
+  }
+  // The weights, and their sum.
+  __device__ __forceinline__ void weigh(f32x16 (&s)[NB], float mc, s16x8 (&p)[2 * NB]) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], c, -mc));
+        l += s[b][i];
+      }
+#pragma unroll
+    for (int t = 0; t < 2 * NB; ++t)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) p[t][j] = (short)H::bits(s[t >> 1][8 * (t & 1) + j]);
+  }
+
+  // The keys' operand of a tile.  (Piece 2t + h of key 32b + r: the key's swizzle does
+  // not depend on b, nor its low bit on t.)
+  __device__ __forceinline__ void read_keys(const unsigned char* lk, s16x8 (&kf)[DHP / 16][NB]) {
+    const int lane = threadIdx.x & 63, h = lane >> 5, r = lane & 31;
+    const unsigned char* kr = lk + r * G::ROW;
+    const int kx = afresh((h ^ G::swz(r)) * 16);
+#pragma unroll
+    for (int t = 0; t < DHP / 16; ++t)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) kf[t][b] = *(const s16x8*)(kr + (kx ^ (32 * t)) + 32 * b * G::ROW);
+  }
+
   // One tile: keys key0 .. key0 + 32 NB - 1.  masked: some column does not see some
   // key of it.  CAREFUL: with what is not finite in V taken care of.
   // The operands of a product are read from LDS before it begins (and half of V
@@ -411,17 +543,11 @@ struct Wave {
   template <bool CAREFUL>
   __device__ __forceinline__ void step(const AttendArgs& a, const Column& col, const unsigned char* lk, const unsigned char* lv,
                                        int key0, uint64_t good, bool masked, float slope) {
-    const int lane = threadIdx.x & 63, h = lane >> 5, r = lane & 31;
+    const int h = (threadIdx.x & 63) >> 5;
     f32x16 s[NB];
     {
-      // (piece 2t + h of key 32b + r: the key's swizzle does not depend on b, nor its low bit on t)
-      const unsigned char* kr = lk + r * G::ROW;
-      const int kx = afresh((h ^ G::swz(r)) * 16);
       s16x8 kf[DHP / 16][NB];
-#pragma unroll
-      for (int t = 0; t < DHP / 16; ++t)
-#pragma unroll
-        for (int b = 0; b < NB; ++b) kf[t][b] = *(const s16x8*)(kr + (kx ^ (32 * t)) + 32 * b * G::ROW);
+      read_keys(lk, kf);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int b = 0; b < NB; ++b)
@@ -440,85 +566,11 @@ struct Wave {
         for (int d = 0; d < DHP / 32; ++d) vf[t][d] = read_v8(lv, t, h, d);
       __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (TURN) {
-      const float f = a.scale * kLog2e, cl = a.cap * kLog2e, inv = a.cap > 0.f ? a.scale / a.cap : 0.f;
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float x = s[b][i] * f;
-          if (a.cap > 0.f) {
-            // tanh y = 1 - 2 / (exp 2y + 1); near 0, where that cancels, its series
-            const float y = s[b][i] * inv, y2 = y * y;
-            const float far = 1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * (2.f * kLog2e)) + 1.f);
-            const float near = y * (1.f + y2 * (-1.f / 3.f + y2 * (2.f / 15.f - y2 * (17.f / 315.f))));
-            x = cl * (fabsf(y) < 0.25f ? near : far);
-          }
-          s[b][i] = x;
-        }
-      if (a.slopes) {
-        const float apart = (float)(col.pos - key0 - 4 * h);
-        if (a.b.tree && key0 + 32 * NB > col.ctx) {  // this step's keys stand at the positions of their depth
-#pragma unroll
-          for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int k = 32 * b + 8 * (i >> 2) + (i & 3), j = key0 + 4 * h + k - col.ctx;
-              const int d = col.pos - col.ctx - __builtin_popcountll(col.path & below(j));
-              s[b][i] -= slope * fabsf(j >= 0 ? (float)d : apart - (float)k);
-            }
-        } else {
-#pragma unroll
-          for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[b][i] -= slope * fabsf(apart - (float)(32 * b + 8 * (i >> 2) + (i & 3)));
-        }
-      }
-    }
-    if (masked) {
-      // bit k: key k of the tile is seen
-      uint64_t see = below(col.hi - key0) & ~below(col.lo - key0);
-      if (a.b.tree) {
-        const int from = key0 - col.ctx;
-        see |= from >= 64 || from <= -64 ? 0 : from >= 0 ? col.see >> from : col.see << -from;
-      }
-      see = (see & good) >> (4 * h);
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          s[b][i] = ((uint32_t)(see >> (32 * b)) & 1u << (8 * (i >> 2) + (i & 3))) ? s[b][i] : -INFINITY;
-    }
-    float top = s[0][0];
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-    top = other_half_max(top);
-    // The maximum lags until a weight would pass 2^kLazy: most tiles rescale nothing
-    if (__builtin_amdgcn_ballot_w64(top * c > m * c + kLazy)) {
-      const float mn = fmaxf(m, top);
-      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * c);
-      l *= f;
-#pragma unroll
-      for (int d = 0; d < DHP / 32; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] *= f;
-      m = mn;
-    }
-    const float mc = (m == -INFINITY ? 0.f : m * c) - H::kShift;
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], c, -mc));
-        l += s[b][i];
-      }
+    if constexpr (TURN) turn(a, col, key0, slope, s);
+    if (masked) hide(a, col, key0, good, s);
+    const float mc = follow<false>(s);
     s16x8 p[2 * NB];
-#pragma unroll
-    for (int t = 0; t < 2 * NB; ++t)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) p[t][j] = (short)H::bits(s[t >> 1][8 * (t & 1) + j]);
+    weigh(s, mc, p);
     if constexpr (CAREFUL) {
       add_not_finite(lv, p, h);
     } else {
@@ -532,6 +584,66 @@ struct Wave {
       for (int t = 0; t < 2 * NB; ++t)
 #pragma unroll
         for (int d = 0; d < DHP / 32; ++d) o[d] = H::mfma(vf[t][d], p[t], o[d]);
+    }
+  }
+
+  // The same with the products of one tile between the softmax of another, for a
+  // wave that has its vector unit to itself.  `s` are the tile's scores, turned;
+  // they become those of the next tile, whose keys lie at lk.
+  __device__ __forceinline__ void first_scores(const AttendArgs& a, const Column& col, const unsigned char* lk, int key0, float slope,
+                                               f32x16 (&s)[NB]) {
+    s16x8 kf[DHP / 16][NB];
+    read_keys(lk, kf);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+#pragma unroll
+    for (int t = 0; t < DHP / 16; ++t)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) s[b] = H::mfma(kf[t][b], q[t], s[b]);
+    if constexpr (TURN) turn(a, col, key0, slope, s);
+  }
+  __device__ __forceinline__ void piped_step(const AttendArgs& a, const Column& col, const unsigned char* lk, const unsigned char* lv,
+                                             int key0, uint64_t good, bool masked, float slope, f32x16 (&s)[NB]) {
+    static_assert(NB == 1);
+    const int h = (threadIdx.x & 63) >> 5;
+    s16x8 kf[DHP / 16][NB], vf[2 * NB][DHP / 32], p[2 * NB];
+    read_keys(lk, kf);
+    __builtin_amdgcn_sched_barrier(0);
+    if (masked) hide(a, col, key0, good, s);
+    const float mc = follow<true>(s);
+    __builtin_amdgcn_sched_barrier(0);
+    read_values(lv, vf);
+    __builtin_amdgcn_sched_barrier(0);
+    f32x16 n[NB];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) n[0][i] = 0.f;
+#pragma unroll
+    for (int t = 0; t < DHP / 16; ++t) n[0] = H::mfma(kf[t][0], q[t], n[0]);
+    asm volatile("" : "+v"(n[0]));  // (not among the accumulation registers: vector operations follow)
+    weigh(s, mc, p);
+#pragma unroll
+    for (int t = 0; t < DHP / 16; ++t) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a matrix product,
+      __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);  // vector operations,
+      __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);  // an exponential
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int t = 0; t < 2 * NB; ++t)
+#pragma unroll
+      for (int d = 0; d < DHP / 32; ++d) o[d] = H::mfma(vf[t][d], p[t], o[d]);
+    s[0] = n[0];
+    if constexpr (TURN) turn(a, col, key0 + 32 * NB, slope, s);
+  }
+
+  // Has the sums of a wide head in accumulation registers here, and so from step to
+  // step: the compiler would else move all of them for the rare rescaling.
+  __device__ __forceinline__ void keep_apart() {
+    if constexpr (DHP == 256) {
+#pragma unroll
+      for (int d = 0; d < DHP / 32; ++d) asm volatile("" : "+a"(o[d]));
     }
   }
 
@@ -556,6 +668,21 @@ struct Wave {
     const int x = afresh(((dim >> 3) ^ G::swz(key)) * 16);  // (key + 8: another piece, two away)
     return join4(__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (x ^ (64 * d)))),
                  __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (x ^ (64 * d) ^ 32) + 8 * G::ROW)));
+  }
+
+  // The values' operand of a whole tile, which begins at a multiple of a key's bytes.
+  __device__ __forceinline__ void read_values(const unsigned char* lv, s16x8 (&vf)[2 * NB][DHP / 32]) {
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    const int key = 4 * h + (lane >> 2 & 3), dim = (lane & 16) + (lane & 3) * 4;
+    const uint32_t p = (uint32_t)(uintptr_t)(lds_void*)lv + key * G::ROW + (dim & 7) * 2 + (((dim >> 3) ^ G::swz(key)) * 16);
+#pragma unroll
+    for (int d = 0; d < DHP / 32; ++d) {
+      const uint32_t one = p ^ (64 * d), two = p ^ (64 * d) ^ 32;
+#pragma unroll
+      for (int t = 0; t < 2 * NB; ++t)
+        vf[t][d] = join4(__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(one + 16 * t * G::ROW)),
+                         __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(two + (16 * t + 8) * G::ROW)));
+    }
   }
 
   // A value that a column does not see must not reach it, and 0 times an infinity
@@ -640,11 +767,12 @@ constexpr int kWideCols = 128;
 template <int DHP>
 constexpr int wide_blocks() { return DHP == 256 ? 1 : 2; }
 template <int DHP>
-constexpr int wide_lds() { return 2 * 2 * 32 * wide_blocks<DHP>() * DHP * 2; }
+constexpr int wide_lds() { return 2 * 2 * 64 * DHP * 2; }
 
 template <int DHP, bool BF16, bool TURN>
 __global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArgs a, Cut cut, int blocks) {
-  extern __shared__ __align__(16) unsigned char smem[];
+  extern __shared__ __align__(1024) unsigned char tiles[];  // (addresses in them are made by XOR)
+  unsigned char* const smem = tiles;
   __shared__ int red[4][2];
   using G = Geo<DHP>;
   constexpr int NB = wide_blocks<DHP>(), KT = 32 * NB, TILE = KT * G::ROW;
@@ -673,7 +801,7 @@ __global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArg
   const float slope = a.slopes && col.row >= 0 ? a.slopes[col.head] * kLog2e : 0.f;
   if (k0 < k1) {
     if (a.D < DHP) {
-      for (int i = tid; i < 4 * TILE / 16; i += 256) ((uint4*)smem)[i] = uint4{0, 0, 0, 0};
+      for (int i = tid; i < wide_lds<DHP>() / 16; i += 256) ((uint4*)smem)[i] = uint4{0, 0, 0, 0};
       __syncthreads();
     }
     const char* kb = (const char*)a.k.p + 2 * kvh * a.k.head;
@@ -719,7 +847,50 @@ __global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArg
       }
       skip(k1);
     };
-    run(std::false_type{});
+    if constexpr (DHP == 256) {
+      // Two steps a round, the scores of each made a step ahead: the keys that are
+      // copied for a round begin 32 after its values.
+      constexpr int KW = 2 * KT, WIDE = 2 * TILE;
+      const int my = 2 * mine;
+      Copies<DHP, 2 * N> two;
+      two.init(a, my);
+      Pages pv = pages_of(a, table, k0 + lane * 16, end), pk = pages_of(a, table, k0 + KT + lane * 16, end);
+      uint64_t good = good_keys<KW>(pv.has, 0, k0, end);
+      copies.template issue<true, false>(a, kb, vb, k0, mine, pv, 0, good & kAll, smem, 2 * WIDE, 0);
+      two.template issue<false, true>(a, kb, vb, k0, my, pv, 0, good, smem, 0, WIDE);
+      two.template issue<true, false>(a, kb, vb, k0 + KT, my, pk, 0, good_keys<KW>(pk.has, 0, k0 + KT, end), smem, 0, 0);
+      vm_wait<0>();
+      block_barrier();
+      f32x16 s[NB];
+      w.first_scores(a, col, smem + 2 * WIDE, k0, slope, s);
+      for (int key = k0, t = 0; key < k1; key += KW, ++t) {
+        const uint32_t now = (t & 1) * 2 * WIDE, next = ((t + 1) & 1) * 2 * WIDE;
+        vm_wait<0>();
+        block_barrier();
+        uint64_t coming = 0;
+        if (key + KW < k1) {
+          const int g = (t + 1) * (KW / 16) & 63;
+          if (g == 0) {
+            pv = pages_of(a, table, key + KW + lane * 16, end);
+            pk = pages_of(a, table, key + KW + KT + lane * 16, end);
+          }
+          coming = good_keys<KW>(pv.has, g, key + KW, end);
+          two.template issue<false, true>(a, kb, vb, key + KW, my, pv, g, coming, smem, 0, next + WIDE);
+          two.template issue<true, false>(a, kb, vb, key + KW + KT, my, pk, g, good_keys<KW>(pk.has, g, key + KW + KT, end), smem,
+                                          next, 0);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int at = key + u * KT;
+          const uint64_t there = good >> (32 * u) & 0xffffffffull;
+          w.piped_step(a, col, smem + now + u * TILE, smem + now + WIDE + u * TILE, at, there,
+                       at < sp.all_lo || at + KT > sp.all_hi || there != 0xffffffffull, slope, s);
+        }
+        good = coming;
+      }
+    } else {
+      run(std::false_type{});
+    }
     if (__syncthreads_or(w.any_nan())) {  // (all of them: the tiles are shared)
       w.reset();
       run(std::true_type{});
@@ -902,12 +1073,17 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void attend_join(AttendArg
 #pragma unroll
     for (int j = 0; j < VL; ++j) x[j] *= old;
     const float* o = part.o + (where.x + s0 * step) * DHP + lane * VL;
-#pragma unroll 8
-    for (int i = 0; i < n; ++i) {
-      const vec v = *(const vec*)(o + i * NW * step * DHP);
-      const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i));
+    constexpr int U = 4;  // on their way at once (the last one again past the end, without weight)
+    for (int i = 0; i < n; i += U) {
+      vec v[U];
 #pragma unroll
-      for (int j = 0; j < VL; ++j) x[j] += fi == 0.f ? 0.f : fi * v[j];
+      for (int u = 0; u < U; ++u) v[u] = *(const vec*)(o + min(i + u, n - 1) * NW * step * DHP);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float fi = i + u < n ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i + u)) : 0.f;
+#pragma unroll
+        for (int j = 0; j < VL; ++j) x[j] += fi == 0.f ? 0.f : fi * v[u][j];
+      }
     }
   }
   if constexpr (NW > 1) {
