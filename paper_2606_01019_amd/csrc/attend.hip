@@ -75,88 +75,146 @@ __device__ __forceinline__ float other_half_sum(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+template <int CTRL>
+__device__ __forceinline__ int dpp(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, false);
+}
+// f over all lanes of a wave (one that does not mind a value twice)
+template <class F>
+__device__ __forceinline__ int wave_all(int v, F f) {
+  v = f(v, dpp<0xB1>(v));
+  v = f(v, dpp<0x4E>(v));
+  v = f(v, dpp<0x141>(v));
+  v = f(v, dpp<0x140>(v));
+  const auto x = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+  v = f((int)x[0], (int)x[1]);
+  const auto y = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+  return __builtin_amdgcn_readfirstlane(f((int)y[0], (int)y[1]));
+}
+
 // How the work is cut: columns per tile; workgroups that the card holds at once, or
-// 0: no tile's keys are split; the fewest keys of a split.
+// 0: no tile's keys are split; the fewest keys of a split; the items there is
+// room for.
 struct Cut {
-  int cols, slots, min_chunk;
+  int cols, slots, min_chunk, items;
+  float item, split;  // what they cost, in keys
 };
 
 // One item: columns [col0, col0 + cols) of sequence s over the keys of split
 // `split` of its tile.
 struct Item {
-  int s, row0, n, len, tile, split, splits, chunk;
+  int s, row0, n, ctx, len, tile, split, splits, chunk;
 };
 
-// How many keys a tile of sequence s may see at most, and its tiles.
-__device__ __forceinline__ void seq_load(const AttendArgs& a, const Cut& c, int s, int& row0, int& n, int& len, int& tiles,
-                                         int& range) {
-  row0 = n = len = tiles = range = 0;
-  if (s > a.b.S) return;
-  int e;
-  seq_rows(a.b, s, row0, e);
-  n = e - row0;
-  if (s < a.b.S) len = min(max(a.b.lengths[s], 0), a.b.P << a.page_shift);
-  tiles = (int)(((int64_t)n * (a.Hq / a.H) + c.cols - 1) / c.cols);
-  range = len;
-  if (a.window > 0 && !a.prefix && !a.b.tree) range = min(len, a.window + min(n, a.b.T));
-  if (range < 0) range = len;
-}
-
-// The keys of one split, the same in every workgroup: so many that there are 3
-// items for 2 slots.  Nothing is split where the tiles fill the card by themselves
-// and none is much longer than a slot's share.
-__device__ __forceinline__ int chunk_of(const AttendArgs& a, const Cut& c) {
-  constexpr int kWhole = 1 << 30;
-  if (c.slots == 0) return kWhole;
-  const int lane = threadIdx.x & 63;
-  float total = 0.f;
-  int count = 0, longest = 0;
-  for (int s = 0; s <= a.b.S; s += 64) {
-    int row0, n, len, tiles, range;
-    seq_load(a, c, s + lane, row0, n, len, tiles, range);
-    total += (float)tiles * (float)range;
-    count += tiles;
-    longest = max(longest, tiles > 0 ? range : 0);
-  }
-  total = wave_sum(total) * (float)a.H;
-  for (int o = 32; o > 0; o >>= 1) {
-    count += __shfl_xor(count, o);
-    longest = max(longest, __shfl_xor(longest, o));
-  }
-  if (count * a.H * 8 >= c.slots * 7 && (float)longest * (float)c.slots <= 1.2f * total) return kWhole;
-  int k = (int)fminf(total / (1.5f * (float)c.slots), 1.0e9f);
-  k = (k + 127) & ~63;
-  return __builtin_amdgcn_readfirstlane(max(k, c.min_chunk));
+// A sequence's rows, context, keys and tiles; how many keys one of its tiles spans at
+// most, and in the mean (about).
+struct Load {
+  int row0, n, ctx, len, tiles, range;
+  float mean;
+};
+__device__ __forceinline__ Load seq_load(const AttendArgs& a, const Cut& c, int s) {
+  Load d{};
+  if (s > a.b.S) return d;
+  int e, len = 0;
+  seq_rows(a.b, s, d.row0, e);
+  if (s < a.b.S) len = a.b.lengths[s];
+  d.n = e - d.row0;
+  d.ctx = len - d.n;
+  d.len = min(max(len, 0), a.b.P << a.page_shift);
+  const int G = a.Hq / a.H;
+  d.tiles = (int)(((int64_t)d.n * G + c.cols - 1) / c.cols);
+  const bool chain = !a.b.tree && !a.prefix;
+  const int rows = chain ? min(d.n, (c.cols + G - 1) / G + 1) : d.n;  // behind the first one's last key
+  d.range = d.len;
+  if (a.window > 0 && a.window < kNoKey - rows) d.range = min(d.len, a.window + rows);
+  d.mean = (float)d.range;
+  // (a chain's first tiles end before its last keys)
+  if (chain && d.range == d.len && d.tiles > 1) d.mean = fmaxf((float)d.len - 0.5f * (float)d.n, 0.5f * (float)d.len);
+  return d;
 }
 
 // A tile of up to `range` keys in even splits of at most `chunk`.
 __device__ __forceinline__ int splits_of(int range, int chunk) { return max(1, (int)(((int64_t)range + 63 + chunk - 1) / chunk)); }
 __device__ __forceinline__ int even_chunk(int range, int splits) { return (int)((((int64_t)range + 63 + splits - 1) / splits + 63) & ~63ll); }
 
+// The most keys of one split, the same in every workgroup.  Up to 63 sequences: the
+// best of 16 lengths, a lane each and the first so long that nothing is split, by
+// when the last workgroup would be done -- its items in rounds of equal length or
+// one after the other, whichever is sooner.
+constexpr int kWhole = 1 << 30;
+constexpr float kStore = 60.f;  // keys' time that the last stores of a split take
+__device__ __forceinline__ int chunk_of(const AttendArgs& a, const Cut& c, const Load& first) {
+  if (c.slots == 0) return kWhole;
+  const int lane = threadIdx.x & 63;
+  const float slots = (float)c.slots / (float)a.H;
+  float worst = 0.f, total = 0.f;
+  int count = 0, longest = 0;
+  for (int s = 0; s <= a.b.S; s += 64) {
+    const Load d = s == 0 ? first : seq_load(a, c, s + lane);
+    worst += (float)d.tiles * (float)d.range;
+    total += (float)d.tiles * d.mean;
+    count += d.tiles;
+    longest = max(longest, d.tiles > 0 ? d.range : 0);
+  }
+  worst = wave_sum(worst);
+  // 3 items for 2 slots: there is room for them, whatever the lengths
+  const int usual = __builtin_amdgcn_readfirstlane(max(((int)fminf(worst / (1.5f * slots), 1.0e9f) + 127) & ~63, c.min_chunk));
+  if (a.b.S >= 64) {  // whole where the tiles fill the card and none is much longer than a slot's share
+    for (int o = 32; o > 0; o >>= 1) {
+      count += __shfl_xor(count, o);
+      longest = max(longest, __shfl_xor(longest, o));
+    }
+    return (float)count * 8.f >= slots * 7.f && (float)longest * slots <= 1.2f * worst ? kWhole : usual;
+  }
+  const float share = wave_sum(total) / slots;
+  const int pick = lane & 15;
+  const int mine = pick == 0 ? kWhole : max(((int)fminf(share * (0.3f + 0.13f * (float)pick), 1.0e9f) + 127) & ~63, c.min_chunk);
+  const float inv = 1.f / (float)mine;
+  float items = 0.f, most = 0.f;
+  for (int s = 0; s <= a.b.S; ++s) {
+    const int tiles = __builtin_amdgcn_readlane(first.tiles, s);
+    if (tiles == 0) continue;
+    const float range = (float)(__builtin_amdgcn_readlane(first.range, s) + 63);
+    const float mean = 63.f + __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(first.mean), s));
+    const float splits = fmaxf(1.f, ceilf(range * inv - 0.001f)), each = range * __builtin_amdgcn_rcpf(splits);
+    items += (float)tiles * (mean < range ? fminf(splits, mean * __builtin_amdgcn_rcpf(each) + 0.5f) : splits);
+    most = fmaxf(most, each);
+  }
+  const float turns = items / slots, path = most + c.item + (pick ? kStore : 0.f);
+  float end = share + turns * c.item + (turns > 1.f ? most : 0.f);
+  end = fmaxf(fminf(end, ceilf(turns - 0.001f) * path), path) + (pick ? turns * c.split : 0.f);
+  if (pick == 0) end *= a.first ? 0.7f : 0.95f;  // (documents' tiles are shorter than that)
+  const int best = wave_all((int)((__float_as_uint(end) & ~15u) | pick), [](int x, int y) { return x < y ? x : y; }) & 15;
+  const int chunk = __builtin_amdgcn_readlane(mine, best);
+  const float all = wave_sum((float)first.tiles * (float)splits_of(first.range, chunk));
+  return all <= (float)c.items ? chunk : usual;
+}
+
 // Item number `idx`; false past the last one.
 __device__ __forceinline__ bool find_item(const AttendArgs& a, const Cut& c, int idx, Item& it) {
   const int lane = threadIdx.x & 63;
-  const int chunk = chunk_of(a, c);
+  const Load first = seq_load(a, c, lane);
+  const int chunk = chunk_of(a, c, first);
   int base = 0;
   for (int s = 0; s <= a.b.S; s += 64) {
-    int row0, n, len, tiles, range;
-    seq_load(a, c, s + lane, row0, n, len, tiles, range);
-    const int splits = splits_of(range, chunk), mine = tiles * splits;
+    const Load d = s == 0 ? first : seq_load(a, c, s + lane);
+    const int splits = splits_of(d.range, chunk), mine = d.tiles * splits;
     const int upto = wave_scan(mine);
     const uint64_t past = __builtin_amdgcn_ballot_w64(base + upto > idx);
     if (past) {
       const int l = __builtin_ctzll(past);
       it.s = s + l;
-      it.row0 = __builtin_amdgcn_readlane(row0, l);
-      it.n = __builtin_amdgcn_readlane(n, l);
-      it.len = __builtin_amdgcn_readlane(len, l);
+      it.row0 = __builtin_amdgcn_readlane(d.row0, l);
+      it.n = __builtin_amdgcn_readlane(d.n, l);
+      it.ctx = __builtin_amdgcn_readlane(d.ctx, l);
+      it.len = __builtin_amdgcn_readlane(d.len, l);
       it.splits = __builtin_amdgcn_readlane(splits, l);
       const int at = idx - base - __builtin_amdgcn_readlane(upto - mine, l);
       // the last tiles of a sequence see the most keys: they go first
       const int t = at / it.splits;
-      it.tile = __builtin_amdgcn_readlane(tiles, l) - 1 - t;
+      it.tile = __builtin_amdgcn_readlane(d.tiles, l) - 1 - t;
       it.split = at - t * it.splits;
-      it.chunk = even_chunk(__builtin_amdgcn_readlane(range, l), it.splits);
+      it.chunk = even_chunk(__builtin_amdgcn_readlane(d.range, l), it.splits);
       return true;
     }
     base += __builtin_amdgcn_readlane(upto, 63);
@@ -179,7 +237,7 @@ __device__ __forceinline__ Column column_of(const AttendArgs& a, const Item& it,
   const bool on = i < it.n, in_seq = it.s < a.b.S;
   c.row = on ? it.row0 + i : -1;
   c.head = head0 + (m - i * G);
-  c.ctx = (in_seq ? a.b.lengths[it.s] : 0) - it.n;
+  c.ctx = it.ctx;
   c.path = c.see = 0;
   c.pos = c.ctx + i;
   const int first = on && a.first ? max(a.first[c.row], 0) : 0;
@@ -203,23 +261,6 @@ __device__ __forceinline__ Column column_of(const AttendArgs& a, const Item& it,
   if (!on || !in_seq || c.hi <= c.lo) c.hi = c.lo = 0;
   if (!on || !in_seq) c.see = 0;
   return c;
-}
-
-template <int CTRL>
-__device__ __forceinline__ int dpp(int v) {
-  return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, false);
-}
-// f over all lanes of a wave (one that does not mind a value twice)
-template <class F>
-__device__ __forceinline__ int wave_all(int v, F f) {
-  v = f(v, dpp<0xB1>(v));
-  v = f(v, dpp<0x4E>(v));
-  v = f(v, dpp<0x141>(v));
-  v = f(v, dpp<0x140>(v));
-  const auto x = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
-  v = f((int)x[0], (int)x[1]);
-  const auto y = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
-  return __builtin_amdgcn_readfirstlane(f((int)y[0], (int)y[1]));
 }
 
 // The keys that some column of a wave sees lie in [lo, hi); all columns (that
@@ -301,12 +342,11 @@ __device__ __forceinline__ void copy_to_lds(const char* base, uint32_t off, uint
 }
 
 // Copies of N * KPI keys of a tile to LDS, K and V: whole groups of 16, or a part
-// of one.
-template <int DHP, int N>
+// of one.  KEEP: each copy's place is kept in registers, where there are some left.
+template <int DHP, int N, bool KEEP>
 struct Copies {
   using G = Geo<DHP>;
   static constexpr int PER = N * G::KPI < 16 ? N : 16 / G::KPI;  // copies per group
-  static constexpr bool KEEP = DHP < 256;  // a wide head's sums leave no registers for every copy's place
   int place;  // of this lane: its piece of the first key, in bytes
   uint32_t k_off[KEEP ? PER : 1], v_off[KEEP ? PER : 1];  // from the first key's place
 
@@ -559,9 +599,10 @@ struct Wave {
         for (int b = 0; b < NB; ++b) s[b] = H::mfma(kf[t][b], q[t], s[b]);
     }
     s16x8 vf[2 * NB][DHP / 32];
+    constexpr int AHEAD = TURN && NB == 2 && DHP == 128 ? 0 : NB;  // (no registers are left for these)
     if constexpr (!CAREFUL) {
 #pragma unroll
-      for (int t = 0; t < NB; ++t)
+      for (int t = 0; t < AHEAD; ++t)
 #pragma unroll
         for (int d = 0; d < DHP / 32; ++d) vf[t][d] = read_v8(lv, t, h, d);
       __builtin_amdgcn_sched_barrier(0);
@@ -576,7 +617,7 @@ struct Wave {
     } else {
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int t = NB; t < 2 * NB; ++t)
+      for (int t = AHEAD; t < 2 * NB; ++t)
 #pragma unroll
         for (int d = 0; d < DHP / 32; ++d) vf[t][d] = read_v8(lv, t, h, d);
       __builtin_amdgcn_sched_barrier(0);
@@ -781,8 +822,7 @@ __global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArg
   const int idx = blockIdx.x / a.H, kvh = blockIdx.x - idx * a.H;
   Item it;
   if (!find_item(a, cut, idx, it)) return;
-  const int m = it.tile * kWideCols + wave * 32 + (lane & 31);
-  const Column col = column_of(a, it, m, kvh * (a.Hq / a.H));
+  const Column col = column_of(a, it, it.tile * kWideCols + wave * 32 + (lane & 31), kvh * (a.Hq / a.H));
   const Span sp = span_of(a, col);
   if (lane == 0) {
     red[wave][0] = sp.lo;
@@ -794,8 +834,7 @@ __global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArg
   const Part part = part_of(a, blocks, kWideCols, DHP);
   int k0, k1, live;
   if (!cut_keys(it, lo, hi, k0, k1, live)) return;
-  const int at = blockIdx.x * kWideCols + wave * 32 + (lane & 31);
-  if (lane < 32) tell_where(a, part, it, col, at, live);
+  if (lane < 32) tell_where(a, part, it, col, blockIdx.x * kWideCols + wave * 32 + lane, live);
   Wave<DHP, BF16, NB, TURN> w;
   w.init(a, col, lane >> 5);
   const float slope = a.slopes && col.row >= 0 ? a.slopes[col.head] * kLog2e : 0.f;
@@ -810,7 +849,7 @@ __global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArg
     const int end = min(hi, it.len);
     constexpr int N = KT / G::KPI / 4;
     const int mine = wave * N * G::KPI;
-    Copies<DHP, N> copies;
+    Copies<DHP, N, DHP <= 128> copies;
     copies.init(a, mine);
     const auto run = [&](auto careful) __attribute__((always_inline)) {
       Pages pg = pages_of(a, table, k0 + lane * 16, end);
@@ -852,7 +891,7 @@ __global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArg
       // copied for a round begin 32 after its values.
       constexpr int KW = 2 * KT, WIDE = 2 * TILE;
       const int my = 2 * mine;
-      Copies<DHP, 2 * N> two;
+      Copies<DHP, 2 * N, false> two;
       two.init(a, my);
       Pages pv = pages_of(a, table, k0 + lane * 16, end), pk = pages_of(a, table, k0 + KT + lane * 16, end);
       uint64_t good = good_keys<KW>(pv.has, 0, k0, end);
@@ -908,6 +947,7 @@ __global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArg
         store_out<BF16>(a, col.row, col.head, 32 * d + 2 * i + 4 * h, w.o[d][i] * f, w.o[d][i + 1] * f, w.o[d][i + 2] * f,
                         w.o[d][i + 3] * f);
   } else {
+    const int at = blockIdx.x * kWideCols + wave * 32 + (lane & 31);
 #pragma unroll
     for (int d = 0; d < DHP / 32; ++d)
 #pragma unroll
@@ -959,7 +999,7 @@ __global__ __launch_bounds__(64 * few_waves<DHP>(), DHP == 256 ? 1 : 2) void att
   // lane l holds the page of half l & 1 of this wave's tile l / 2
   const auto pages_from = [&](int key) { return pages_of(a, table, key + (lane >> 1) * STEP + (lane & 1) * 16, end); };
   const int first = k0 + wave * 32;
-  Copies<DHP, N> copies;
+  Copies<DHP, N, DHP <= 128> copies;
   copies.init(a, 0);
   const auto run = [&](auto careful) __attribute__((always_inline)) {
     Pages pg = pages_from(first);
@@ -1054,8 +1094,9 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void attend_join(AttendArg
   const Part part = part_of(a, blocks, cols, DHP);
   const int2 where = part.where[rh];
   const int live = where.y;
-  if (live <= 1) return;
   const int64_t step = (int64_t)a.H * cols;  // places from one split to the next
+  // (nor if it is no place: a row that no sequence has, where starts does not begin at 0)
+  if (live <= 1 || where.x < 0 || where.x + (live - 1) * step >= (int64_t)blocks * cols) return;
   float top = -INFINITY, sum = 0.f;
   float x[VL] = {};
   for (int s0 = first; s0 < live; s0 += 64 * NW) {
@@ -1134,11 +1175,17 @@ Plan plan_of(const AttendArgs& a) {
   p.cut.cols = p.few ? kFewCols : kWideCols;
   const int64_t most = cols / p.cut.cols + std::min(a.b.S + 1, a.b.T);  // tiles there can be
   const int64_t likely = std::max<int64_t>(seqs, (cols + p.cut.cols - 1) / p.cut.cols);
-  // workgroups at once: by the registers of a kernel's waves and the LDS of its tiles
-  const int dim = padded_dim(a.D), slots = 256 * (dim == 64 ? 3 : dim == 128 ? 2 : 1);
-  p.cut.min_chunk = p.few ? 128 : 256;
+  // workgroups at once, by a kernel's registers and the LDS of its tiles
+  const int dim = padded_dim(a.D), at_once = p.few ? (dim == 64 ? 2 : 1) : dim == 64 ? 3 : dim == 128 ? 2 : 1, slots = 256 * at_once;
+  p.cut.min_chunk = 128;
   p.cut.slots = likely * a.H < 3 * slots ? slots : 0;
-  const int64_t items = p.cut.slots ? 2 * most + (3 * slots / 2) / a.H + 9 : most;
+  const int64_t items = p.cut.slots ? most + most / 2 + 2 * slots / a.H + 9 : most;
+  p.cut.items = (int)items;
+  // An item takes about 3 us before its first key; a split's sums are written and read
+  // again, which takes as long as this many keys do (35 ns a key of a wide tile's at
+  // its matrix products' rate, a narrow one's keys at the memory's).
+  p.cut.item = 80.f;
+  p.cut.split = p.few ? 64.f : dim == 256 ? 250.f : 400.f;
   p.blocks = (int)(items * a.H);
   return p;
 }
