@@ -180,6 +180,66 @@ def test_attend_long_contexts_are_split(hvd, rows, G):
     check(hvd, Case([(rows, 3000), (1, 11), (2, 700)], 2, 64, 64, seed=rows + G), 2 * G, cap=30.0)
 
 
+@pytest.mark.parametrize("seqs", [1, 2, 62, 63, 64, 65, 130])
+@pytest.mark.parametrize("rows", [1, 40])
+def test_attend_splits_of_few_and_many_sequences(hvd, seqs, rows):
+    """The lengths of splits are chosen apart for up to 63 sequences and for more."""
+    check(hvd, Case([(rows if s % 20 == 0 else 1, (s * 97) % 700 + 200 * (s == 0)) for s in range(seqs)], 1, 64, seed=seqs, pad=2), 3)
+
+
+@pytest.mark.parametrize("G", [1, 3, 5, 32])
+@pytest.mark.parametrize("window", [1, 63, 200, 450])
+@pytest.mark.parametrize("prefix", [False, True])
+def test_attend_windows_over_prompts(hvd, G, window, prefix):
+    """What a tile of a windowed prompt can span, where its rows end between columns."""
+    c = Case([(150, 500), (1, 300), (66, 0)], 1, 64, seed=G + window, pad=1)
+    check(hvd, c, G, window=window, prefix=torch.tensor([600, 0, 20], dtype=torch.int32) if prefix else None)
+
+
+@pytest.mark.parametrize("dtype,D", [(F16, 256), (BF16, 256), (F16, 128), (BF16, 64)])
+@pytest.mark.parametrize("cap", [0.0, 20.0, 100.0])
+def test_attend_tiles_of_many_keys(hvd, dtype, D, cap):
+    """Tiles that are not split (as many as the card has places for), over more keys
+    than one look at the page table gives.  The tolerance is attend_ref's."""
+    n, ctx, G = 2085, 1203, 8
+    c = Case([(n, ctx)], 2, D, dtype=dtype, seed=D)
+    q = c.rnd(n, 2 * G, D).to(dtype).cuda()
+    got = hvd.attend(q, c.k_cache, c.v_cache, c.batch(hvd), cap=cap).double()
+    L, u, scale = n + ctx, torch.finfo(dtype).eps / 2, D ** -0.5
+    ids = torch.from_numpy(c.pages[0]).long().cuda()
+    seen = torch.arange(L, device="cuda")[None, :] <= ctx + torch.arange(n, device="cuda")[:, None]
+    for h in range(2 * G):
+        K, V = (t[ids, h // G].reshape(-1, D)[:L].double() for t in (c.k_cache, c.v_cache))
+        Q = q[:, h].double()
+        x = torch.mm(Q, K.t().contiguous()) * scale
+        big = torch.mm(Q.abs(), K.abs().t().contiguous()).masked_fill(~seen, 0).amax(1) * scale
+        d = (D + 8) * 2.0 ** -23 * big
+        if cap:
+            x = cap * torch.tanh(x / cap)
+            d = d + 8 * 2.0 ** -23 * big.clamp(min=cap)
+        d = d + 8 * 2.0 ** -23 * x.masked_fill(~seen, 0).abs().amax(1)
+        p = torch.softmax(x.masked_fill(~seen, -math.inf), 1)
+        o, A = torch.mm(p, V), torch.mm(p, V.abs())
+        keys = seen.sum(1)[:, None].double()
+        tol = 1.02 * (u * o.abs() + (u + 2 * d[:, None] + keys * 2.0 ** -23) * A + keys * 2.0 ** -32 * V.abs().amax(0))
+        over = (got[:, h] - o).abs() - tol
+        assert float(over.max()) <= 0, (h, float(over.max()))
+
+
+def test_attend_starts_that_leave_rows_out(hvd):
+    """Rows before the first start, and starts that go back, are no sequence's or some
+    sequence's: no place that does not exist is read for them, and the other
+    rows have their results."""
+    c = Case([(4, 900), (30, 50)], 2, 64, seed=41)
+    q = c.rnd(c.T, 4, 64).to(F16).cuda()
+    want = hvd.attend(q, c.k_cache, c.v_cache, c.batch(hvd))
+    c.starts[0], c.lengths[0] = 2, c.lengths[0]
+    got = hvd.attend(q, c.k_cache, c.v_cache, c.batch(hvd))
+    assert torch.equal(got[4:], want[4:])
+    c.starts[:] = [0, 30, 3]
+    assert hvd.attend(q, c.k_cache, c.v_cache, c.batch(hvd)).shape == q.shape
+
+
 def test_attend_a_long_prompt(hvd):
     check(hvd, Case([(300, 0), (129, 77)], 1, 128, seed=5), 3)
 
@@ -206,10 +266,11 @@ def test_attend_rows_that_see_nothing_are_zero(hvd):
 @pytest.mark.parametrize("rows", [2, 60])
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
-def test_attend_hidden_places_do_not_reach_a_row(hvd, rows, dtype, what):
+@pytest.mark.parametrize("D", [64, 128, 200, 256])
+def test_attend_hidden_places_do_not_reach_a_row(hvd, rows, dtype, what, D):
     """What lies behind a sequence, before a row's document or after the row may be
     anything; what a row sees reaches it and no other."""
-    c = Case([(rows, 90), (rows, 30)], 2, 64, dtype=dtype, seed=rows)
+    c = Case([(rows, 90), (rows, 30)], 2, D, dtype=dtype, seed=rows)
     for cache in (c.k_cache, c.v_cache):
         for s, (n, ctx) in enumerate(c.sizes):
             for j in range(n + ctx, c.pages.shape[1] * 16):
@@ -244,8 +305,9 @@ def test_attend_infinite_scores(hvd):
 
 
 @pytest.mark.parametrize("rows", [3, 50])
-def test_attend_without_pages(hvd, rows):
-    c = Case([(rows, 100), (rows, 60)], 1, 64, seed=22)
+@pytest.mark.parametrize("D", [64, 96, 128, 200, 256])
+def test_attend_without_pages(hvd, rows, D):
+    c = Case([(rows, 100), (rows, 60)], 1, D, seed=22)
     c.pages[0, 2] = -1
     c.pages[0, 5] = c.n_pages
     c.pages[1, 0] = 1 << 30
