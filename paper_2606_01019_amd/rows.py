@@ -78,9 +78,10 @@ def _array(t, what, dtype, shape, device):
     """The address of a contiguous tensor of that type and shape (None: any size)."""
     if t.dtype != dtype or t.device != device or t.dim() != len(shape) or not t.is_contiguous():
         _refuse(f"{what} must be a contiguous {dtype} tensor of {len(shape)} dimension(s) on the arguments' device")
-    for n, m in zip(t.shape, shape):
-        if m is not None and n != m:
-            _refuse(f"{what} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if t.shape != shape:  # (None: any)
+        for n, m in zip(t.shape, shape):
+            if m is not None and n != m:
+                _refuse(f"{what} has shape {tuple(t.shape)}, not {tuple(shape)}")
     if t.requires_grad:
         _no_grad(t, what)
     return t.data_ptr()
