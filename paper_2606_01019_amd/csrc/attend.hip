@@ -376,7 +376,7 @@ struct Copies {
   __device__ __forceinline__ bool issue(const AttendArgs& a, const char* kb, const char* vb, int key0, int k0, const Pages& pg, int g0,
                                         uint64_t good, unsigned char* smem, uint32_t lk, uint32_t lv) const {
     constexpr uint64_t kMine = N * G::KPI >= 64 ? ~0ull : (1ull << (N * G::KPI & 63)) - 1;
-    const bool whole = (good >> k0 & kMine) == kMine && a.D == DHP;
+    const bool full = (good >> k0 & kMine) == kMine, whole = full && a.D == DHP;
     const uint32_t base = (uint32_t)(uintptr_t)(lds_void*)smem;
 #pragma unroll
     for (int f = 0; f < N; f += PER) {
@@ -411,8 +411,8 @@ struct Copies {
         }
       }
     }
-    if (!whole) __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the zeros are there before the barrier
-    return whole;
+    if (!full) __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the zeros are there before the barrier
+    return full;  // (a narrower head's copies have lanes with a piece each all the same)
   }
 };
 
