@@ -299,18 +299,23 @@ struct Geo {
 };
 
 // Where 64 groups of 16 keys lie in the cache, one per lane (group l starts at key
-// `key` of lane l): byte offsets of their pages, and which of them have one --
-// none past `end`, and none that the cache does not have.
+// `key` of lane l): the addresses of their first keys and values of one head, and
+// which of them have a page -- none past `end`, and none that the cache does not
+// have.
 struct Pages {
   uint32_t k_lo, k_hi, v_lo, v_hi;
   uint64_t has;
 };
-__device__ __forceinline__ Pages pages_of(const AttendArgs& a, const int32_t* table, int key, int end) {
-  const int pi = key >> a.page_shift;
+__device__ __forceinline__ Pages pages_of(const AttendArgs& a, const int32_t* table, int kvh, int key, int end) {
+  const int pi = key >> a.page_shift, tok = key & ((1 << a.page_shift) - 1);
   const int p = key < end && pi < a.b.P ? table[pi] : -1;
   const bool in = (unsigned)p < (unsigned)a.n_pages;
-  const int64_t k = 2 * (in ? p : 0) * a.k.page, v = 2 * (in ? p : 0) * a.v.page;
+  const uint64_t k = (uint64_t)((const uint16_t*)a.k.p + kvh * a.k.head + (in ? p * a.k.page + tok * a.k.tok : 0));
+  const uint64_t v = (uint64_t)((const uint16_t*)a.v.p + kvh * a.v.head + (in ? p * a.v.page + tok * a.v.tok : 0));
   return Pages{(uint32_t)k, (uint32_t)(k >> 32), (uint32_t)v, (uint32_t)(v >> 32), __builtin_amdgcn_ballot_w64(in)};
+}
+__device__ __forceinline__ const char* address_of(uint32_t lo, uint32_t hi, int lane) {
+  return (const char*)((uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, lane) << 32 | (uint32_t)__builtin_amdgcn_readlane(lo, lane));
 }
 
 // Which of a tile's NK keys have a page: group g0 is the tile's first.
@@ -374,7 +379,7 @@ struct Copies {
   // The tile begins with key0; group g0 of `pg` is its first, `good` its keys that
   // have a page.  Returns false if fewer than N copies (of each) were asked for.
   template <bool K = true, bool V = true>
-  __device__ __forceinline__ bool issue(const AttendArgs& a, const char* kb, const char* vb, int key0, int k0, const Pages& pg, int g0,
+  __device__ __forceinline__ bool issue(const AttendArgs& a, int k0, const Pages& pg, int g0,
                                         uint64_t good, unsigned char* smem, uint32_t lk, uint32_t lv) const {
     constexpr uint64_t kMine = N * G::KPI >= 64 ? ~0ull : (1ull << (N * G::KPI & 63)) - 1;
     const bool full = (good >> k0 & kMine) == kMine, whole = full && a.D == DHP;
@@ -382,11 +387,9 @@ struct Copies {
 #pragma unroll
     for (int f = 0; f < N; f += PER) {
       const int first = k0 + f * G::KPI, g = g0 + (first >> 4);  // wave-uniform
-      const uint32_t tok = 2u * ((key0 + first) & ((1 << a.page_shift) - 1));
-      const char* kp = kb + (uint64_t)tok * (uint32_t)a.k.tok +
-                       ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(pg.k_hi, g) << 32 | (uint32_t)__builtin_amdgcn_readlane(pg.k_lo, g));
-      const char* vp = vb + (uint64_t)tok * (uint32_t)a.v.tok +
-                       ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(pg.v_hi, g) << 32 | (uint32_t)__builtin_amdgcn_readlane(pg.v_lo, g));
+      const uint32_t in_group = PER * G::KPI < 16 ? first & 15 : 0;
+      const char* kp = address_of(pg.k_lo, pg.k_hi, g) + 2u * in_group * (uint32_t)a.k.tok;
+      const char* vp = address_of(pg.v_lo, pg.v_hi, g) + 2u * in_group * (uint32_t)a.v.tok;
       if (whole) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
@@ -476,8 +479,8 @@ struct Wave {
           for (int i = 0; i < 16; ++i) {
             const float y = s[b][i] * inv, y2 = y * y;
             const float far = 1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[b][i] * two) + 1.f);
-            const float near = y * (1.f + y2 * (-1.f / 3.f + y2 * (2.f / 15.f - y2 * (17.f / 315.f))));
-            s[b][i] = cl * (fabsf(y) < 0.25f ? near : far);
+            const float near = 1.f + y2 * (-1.f / 3.f + y2 * (2.f / 15.f - y2 * (17.f / 315.f)));  // of y
+            s[b][i] = fabsf(y) < 0.25f ? s[b][i] * (a.scale * kLog2e) * near : cl * far;
           }
       }
     } else {
@@ -849,8 +852,6 @@ __global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArg
       for (int i = tid; i < wide_lds<DHP>() / 16; i += 256) ((uint4*)smem)[i] = uint4{0, 0, 0, 0};
       __syncthreads();
     }
-    const char* kb = (const char*)a.k.p + 2 * kvh * a.k.head;
-    const char* vb = (const char*)a.v.p + 2 * kvh * a.v.head;
     const int32_t* table = a.b.pages + (it.s < a.b.S ? it.s : 0) * a.b.pages_stride;
     const int end = min(hi, it.len);
     constexpr int N = KT / G::KPI / 4;
@@ -858,9 +859,9 @@ __global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArg
     Copies<DHP, N, DHP <= 128> copies;
     copies.init(a, mine);
     const auto run = [&](auto careful) __attribute__((always_inline)) {
-      Pages pg = pages_of(a, table, k0 + lane * 16, end);
+      Pages pg = pages_of(a, table, kvh, k0 + lane * 16, end);
       uint64_t good = good_keys<KT>(pg.has, 0, k0, end), next_good = 0;
-      copies.issue(a, kb, vb, k0, mine, pg, 0, good, smem, 0, TILE);
+      copies.issue(a, mine, pg, 0, good, smem, 0, TILE);
       int key = k0, t = 0;
       // waits for this tile and begins to copy the next one
       const auto next = [&]() __attribute__((always_inline)) {
@@ -868,10 +869,10 @@ __global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArg
         block_barrier();
         if (key + KT < k1) {
           const int g = (t + 1) * (KT / 16) & 63;
-          if (g == 0) pg = pages_of(a, table, key + KT + lane * 16, end);
+          if (g == 0) pg = pages_of(a, table, kvh, key + KT + lane * 16, end);
           next_good = good_keys<KT>(pg.has, g, key + KT, end);
           const uint32_t to = ((t + 1) & 1) * 2 * TILE;
-          copies.issue(a, kb, vb, key + KT, mine, pg, g, next_good, smem, to, to + TILE);
+          copies.issue(a, mine, pg, g, next_good, smem, to, to + TILE);
         }
       };
       const auto skip = [&](int until) __attribute__((always_inline)) {
@@ -899,11 +900,11 @@ __global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArg
       const int my = 2 * mine;
       Copies<DHP, 2 * N, false> two;
       two.init(a, my);
-      Pages pv = pages_of(a, table, k0 + lane * 16, end), pk = pages_of(a, table, k0 + KT + lane * 16, end);
+      Pages pv = pages_of(a, table, kvh, k0 + lane * 16, end), pk = pages_of(a, table, kvh, k0 + KT + lane * 16, end);
       uint64_t good = good_keys<KW>(pv.has, 0, k0, end);
-      copies.template issue<true, false>(a, kb, vb, k0, mine, pv, 0, good & kAll, smem, 2 * WIDE, 0);
-      two.template issue<false, true>(a, kb, vb, k0, my, pv, 0, good, smem, 0, WIDE);
-      two.template issue<true, false>(a, kb, vb, k0 + KT, my, pk, 0, good_keys<KW>(pk.has, 0, k0 + KT, end), smem, 0, 0);
+      copies.template issue<true, false>(a, mine, pv, 0, good & kAll, smem, 2 * WIDE, 0);
+      two.template issue<false, true>(a, my, pv, 0, good, smem, 0, WIDE);
+      two.template issue<true, false>(a, my, pk, 0, good_keys<KW>(pk.has, 0, k0 + KT, end), smem, 0, 0);
       vm_wait<0>();
       block_barrier();
       f32x16 s[NB];
@@ -916,12 +917,12 @@ __global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArg
         if (key + KW < k1) {
           const int g = (t + 1) * (KW / 16) & 63;
           if (g == 0) {
-            pv = pages_of(a, table, key + KW + lane * 16, end);
-            pk = pages_of(a, table, key + KW + KT + lane * 16, end);
+            pv = pages_of(a, table, kvh, key + KW + lane * 16, end);
+            pk = pages_of(a, table, kvh, key + KW + KT + lane * 16, end);
           }
           coming = good_keys<KW>(pv.has, g, key + KW, end);
-          two.template issue<false, true>(a, kb, vb, key + KW, my, pv, g, coming, smem, 0, next + WIDE);
-          two.template issue<true, false>(a, kb, vb, key + KW + KT, my, pk, g, good_keys<KW>(pk.has, g, key + KW + KT, end), smem,
+          two.template issue<false, true>(a, my, pv, g, coming, smem, 0, next + WIDE);
+          two.template issue<true, false>(a, my, pk, g, good_keys<KW>(pk.has, g, key + KW + KT, end), smem,
                                           next, 0);
         }
 #pragma unroll
@@ -999,20 +1000,18 @@ __global__ __launch_bounds__(64 * few_waves<DHP>(), DHP == 256 ? 1 : 2) void att
     for (int i = lane; i < 4 * TILE / 16; i += 64) ((uint4*)my)[i] = uint4{0, 0, 0, 0};
     __syncthreads();
   }
-  const char* kb = (const char*)a.k.p + 2 * kvh * a.k.head;
-  const char* vb = (const char*)a.v.p + 2 * kvh * a.v.head;
   const int32_t* table = a.b.pages + (it.s < a.b.S ? it.s : 0) * a.b.pages_stride;
   const int end = min(sp.hi, it.len);
   constexpr int N = 32 / G::KPI, STEP = 32 * NW;
   // lane l holds the page of half l & 1 of this wave's tile l / 2
-  const auto pages_from = [&](int key) { return pages_of(a, table, key + (lane >> 1) * STEP + (lane & 1) * 16, end); };
+  const auto pages_from = [&](int key) { return pages_of(a, table, kvh, key + (lane >> 1) * STEP + (lane & 1) * 16, end); };
   const int first = k0 + wave * 32;
   Copies<DHP, N, DHP <= 128> copies;
   copies.init(a, 0);
   const auto run = [&](auto careful) __attribute__((always_inline)) {
     Pages pg = pages_from(first);
     uint64_t good = good_keys<32>(pg.has, 0, first, end), next_good = 0;
-    copies.issue(a, kb, vb, first, 0, pg, 0, good, my, 0, TILE);
+    copies.issue(a, 0, pg, 0, good, my, 0, TILE);
     for (int key = first, t = 0; key < k1; key += STEP, ++t) {
       const uint32_t now = (t & 1) * 2 * TILE, next = ((t + 1) & 1) * 2 * TILE;
       bool all = false;
@@ -1020,7 +1019,7 @@ __global__ __launch_bounds__(64 * few_waves<DHP>(), DHP == 256 ? 1 : 2) void att
         const int g = (t + 1) * 2 & 63;
         if (g == 0) pg = pages_from(key + STEP);
         next_good = good_keys<32>(pg.has, g, key + STEP, end);
-        all = copies.issue(a, kb, vb, key + STEP, 0, pg, g, next_good, my, next, next + TILE);
+        all = copies.issue(a, 0, pg, g, next_good, my, next, next + TILE);
       }
       if (all) vm_wait<2 * N>();
       else vm_wait<0>();

@@ -226,6 +226,22 @@ def test_attend_tiles_of_many_keys(hvd, dtype, D, cap):
         assert float(over.max()) <= 0, (h, float(over.max()))
 
 
+@pytest.mark.parametrize("rows,D", [(1, 64), (40, 128), (40, 256)])
+@pytest.mark.parametrize("cap", [1e-30, 0.01, 64.0, 65.0])
+def test_attend_small_and_usual_caps(hvd, rows, D, cap):
+    check(hvd, Case([(rows, 100)], 1, D, seed=rows), 2, cap=cap)
+
+
+@pytest.mark.parametrize("rows,D", [(1, 64), (40, 128), (40, 256)])
+@pytest.mark.parametrize("cap", [1e6, 1e30, 3.4e38])
+def test_attend_a_cap_far_above_the_scores_changes_nothing(hvd, rows, D, cap):
+    """x (1 - (x / cap)^2 / 3 + ..) is x to 2^-24 where |x| < 2^-11 cap: the tolerance is
+    that of no cap."""
+    c = Case([(rows, 100)], 1, D, seed=rows + 1)
+    q = c.rnd(c.T, 2, D).to(F16).cuda()
+    check_attend(c, hvd.attend(q, c.k_cache, c.v_cache, c.batch(hvd), cap=cap), q)
+
+
 def test_attend_starts_that_leave_rows_out(hvd):
     """Rows before the first start, and starts that go back, are no sequence's or some
     sequence's: no place that does not exist is read for them, and the other
