@@ -217,12 +217,19 @@ __global__ __launch_bounds__(kThreads, 4) void adjust_rows(AdjustArgs a, int seg
   for (int row = r0; row < r1; ++row) {
     // (octets past the part's end are not used: any other in their place)
     Octet<TYPE> raw[CH];
+    uint32_t bits[CH];  // of the mask
     const auto load = [&]() __attribute__((always_inline)) {
       if (nv8 > 0) {
 #pragma unroll
-        for (int i = 0; i < CH; ++i) raw[i].load(a.logits, row * a.logits_stride + v0 + min((i * kThreads + tid) * 8, nv8 - 8));
+        for (int i = 0; i < CH; ++i) {
+          const int c = min((i * kThreads + tid) * 8, nv8 - 8);
+          raw[i].load(a.logits, row * a.logits_stride + v0 + c);
+          bits[i] = a.allowed ? (uint32_t)a.allowed[row * a.allowed_stride + ((v0 + c) >> 5)] >> (c & 31) : ~0u;
+        }
       }
     };
+    const uint64_t mask = path && a.b.tree ? (uint64_t)a.b.tree[row] : 0;
+    const int own = path && !a.b.tree ? a.tokens[row] : -1;
     // on their way while the words are made, where registers allow it
     constexpr bool kEarly = CH * (TYPE == ET_F32 ? 2 : 1) <= 4;
     if (kEarly) load();
@@ -266,11 +273,11 @@ __global__ __launch_bounds__(kThreads, 4) void adjust_rows(AdjustArgs a, int seg
     if (live) {
       if (path) {
         if (a.b.tree) {  // from the last row's path to this one's
-          const uint64_t mask = (uint64_t)a.b.tree[row], change = mask ^ on_path;
+          const uint64_t change = mask ^ on_path;
           if (tid < 64 && (change >> lane & 1)) bump(my_token, mask >> lane & 1 ? 1u : ~0u);
           on_path = mask;
         } else if (tid == 0) {
-          bump(a.tokens[row], 1u);
+          bump(own, 1u);
         }
       }
       if (words) __syncthreads();
@@ -304,9 +311,8 @@ __global__ __launch_bounds__(kThreads, 4) void adjust_rows(AdjustArgs a, int seg
         }
       }
       if (ok) {
-        const uint32_t bits = (uint32_t)ok[(v0 + c) >> 5] >> (c & 31);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = bits >> j & 1 ? x[j] : -INFINITY;
+        for (int j = 0; j < 8; ++j) x[j] = bits[i] >> j & 1 ? x[j] : -INFINITY;
       }
       if (a.out) store8(a.out, to + c, TYPE, x);
 #pragma unroll
