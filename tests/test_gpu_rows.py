@@ -571,6 +571,57 @@ def test_a_captured_step_follows_its_tensors(hvd):
             assert torch.equal(x, y)
 
 
+@pytest.mark.parametrize("D,rows", [(256, 70), (128, 70), (64, 1), (72, 2), (256, 1)])
+def test_a_captured_attention_alone(hvd, D, rows):
+    c = Case([(rows, 300), (1, 40)], 1, D, seed=D)
+    q = c.rnd(c.T, 4, D).to(F16).cuda()
+    b = c.batch(hvd)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        got = hvd.attend(q, c.k_cache, c.v_cache, b)
+    for _ in range(3):
+        q.copy_(c.rnd(c.T, 4, D).to(F16))
+        graph.replay()
+        torch.cuda.synchronize()
+        check_attend(c, got, q)
+        assert torch.equal(got, hvd.attend(q, c.k_cache, c.v_cache, b))
+
+
+def test_two_graphs_at_once(hvd):
+    """Each graph has a workspace of its own."""
+    c = Case([(1, 2000), (5, 300)], 2, 128, seed=37)
+    b = c.batch(hvd)
+    qs = [c.rnd(c.T, 8, 128).to(F16).cuda() for _ in range(2)]
+    graphs, got = [], []
+    for q in qs:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            got.append(hvd.attend(q, c.k_cache, c.v_cache, b))
+    want = [hvd.attend(q, c.k_cache, c.v_cache, b) for q in qs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(10):
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
+
+
+def test_inference_mode(hvd):
+    c = Case([(1, 20), (5, 30)], 2, 64, seed=38)
+    b = c.batch(hvd)
+    with torch.inference_mode():
+        k, q = c.rnd(c.T, 2, 64).cuda(), c.rnd(c.T, 4, 64).to(F16).cuda()
+        hvd.append_kv(c.k_cache, c.v_cache, k, k, b)
+        out = hvd.attend(q, c.k_cache, c.v_cache, b, out=torch.empty_like(q))
+        check_attend(c, out, q)
+        l = torch.zeros(c.T, 100, device="cuda")
+        assert hvd.adjust_logits(l, b, out=l)[1].tolist() == [0] * c.T
+
+
 def test_streams_other_than_the_tensors(hvd):
     c = Case([(1, 900), (5, 30)], 2, 64, seed=33)
     q = c.rnd(c.T, 8, 64).to(F16).cuda()
