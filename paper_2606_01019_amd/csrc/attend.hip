@@ -604,11 +604,9 @@ struct Wave {
     }
     s16x8 vf[2 * NB][DHP / 32];
     constexpr int AHEAD = TURN && NB == 2 && DHP == 128 ? 0 : NB;  // (no registers are left: 161 us, 158 without)
+    const uint32_t values = values_at(lv);
     if constexpr (!CAREFUL) {
-#pragma unroll
-      for (int t = 0; t < AHEAD; ++t)
-#pragma unroll
-        for (int d = 0; d < DHP / 32; ++d) vf[t][d] = read_v8(lv, t, h, d);
+      read_values<0, AHEAD>(values, vf);
       __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (TURN) turn(a, col, key0, slope, s);
@@ -620,10 +618,7 @@ struct Wave {
       add_not_finite(lv, p, h);
     } else {
       __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int t = AHEAD; t < 2 * NB; ++t)
-#pragma unroll
-        for (int d = 0; d < DHP / 32; ++d) vf[t][d] = read_v8(lv, t, h, d);
+read_values<AHEAD, 2 * NB>((uint32_t)afresh((int)values), vf);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int t = 0; t < 2 * NB; ++t)
@@ -659,7 +654,7 @@ struct Wave {
     if (masked) hide(a, col, key0, good, s);
     const float mc = follow<true>(s);
     __builtin_amdgcn_sched_barrier(0);
-    read_values(lv, vf);
+    read_values<0, 2 * NB>(values_at(lv), vf);
     __builtin_amdgcn_sched_barrier(0);
     f32x16 n[NB];
 #pragma unroll
@@ -715,16 +710,20 @@ struct Wave {
                  __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (x ^ (64 * d) ^ 32) + 8 * G::ROW)));
   }
 
-  // The values' operand of a whole tile, which begins at a multiple of a key's bytes.
-  __device__ __forceinline__ void read_values(const unsigned char* lv, s16x8 (&vf)[2 * NB][DHP / 32]) {
+  // The same for 16-key operands T0 .. T1 - 1 and all dimensions: a tile begins at a
+  // multiple of 1024, so an XOR of a lane's place gives each dimension's.
+  __device__ __forceinline__ uint32_t values_at(const unsigned char* lv) {
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int key = 4 * h + (lane >> 2 & 3), dim = (lane & 16) + (lane & 3) * 4;
-    const uint32_t p = (uint32_t)(uintptr_t)(lds_void*)lv + key * G::ROW + (dim & 7) * 2 + (((dim >> 3) ^ G::swz(key)) * 16);
+    return (uint32_t)(uintptr_t)(lds_void*)lv + (key * G::ROW + (dim & 7) * 2 + (((dim >> 3) ^ G::swz(key)) * 16));
+  }
+  template <int T0, int T1>
+  __device__ __forceinline__ void read_values(uint32_t p, s16x8 (&vf)[2 * NB][DHP / 32]) {
 #pragma unroll
     for (int d = 0; d < DHP / 32; ++d) {
       const uint32_t one = p ^ (64 * d), two = p ^ (64 * d) ^ 32;
 #pragma unroll
-      for (int t = 0; t < 2 * NB; ++t)
+      for (int t = T0; t < T1; ++t)
         vf[t][d] = join4(__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(one + 16 * t * G::ROW)),
                          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(two + (16 * t + 8) * G::ROW)));
     }
@@ -977,7 +976,8 @@ constexpr int few_lds() { return few_waves<DHP>() * 2 * 2 * 32 * DHP * 2; }
 
 template <int DHP, bool BF16, bool TURN>
 __global__ __launch_bounds__(64 * few_waves<DHP>(), DHP == 256 ? 1 : 2) void attend_few(AttendArgs a, Cut cut, int blocks) {
-  extern __shared__ __align__(16) unsigned char smem[];
+  extern __shared__ __align__(1024) unsigned char tiles[];  // (addresses in them are made by XOR)
+  unsigned char* const smem = tiles;
   constexpr int NW = few_waves<DHP>();
   __shared__ float stat[NW][32][2];
   using G = Geo<DHP>;
