@@ -140,8 +140,8 @@ __device__ __forceinline__ int even_chunk(int range, int splits) { return (int)(
 // The most keys of one split, the same in every workgroup.  Up to 63 sequences: the
 // best of 16 lengths, a lane each and the first so long that nothing is split, by
 // when the last workgroup would be done -- its items in rounds of equal length or
-// one after the other, whichever is sooner.  (8 trees over 8192 keys 162 us, with 3
-// items for 2 slots throughout 178; one tree over 16384 keys 36 and 49.)
+// one after the other, whichever is sooner.  (8 trees over 8192 keys 162 us when
+// it came, with 3 items for 2 slots throughout 178; one tree over 16384 keys 36 and 49.)
 constexpr int kWhole = 1 << 30;
 constexpr float kStore = 60.f;  // keys' time that the last stores of a split take
 __device__ __forceinline__ int chunk_of(const AttendArgs& a, const Cut& c, const Load& first) {
@@ -812,10 +812,10 @@ __device__ __forceinline__ void tell_where(const AttendArgs& a, const Part& part
 
 // Many columns: four waves of 32 share the tiles of 64 keys, one being copied while
 // one is worked on.  Bound by the matrix cores and what is issued beside them, two
-// workgroups a CU: 2048 rows of 32 heads of 128 over 16384 keys 560 us, 0.92
+// workgroups a CU: 2048 rows of 32 heads of 128 over 16384 keys 533 us, 0.97
 // PFLOP/s (a large product: 1.2).  Where a key is 256 wide a wave has its vector unit
 // to itself, and a tile is two steps of 32 keys whose softmax goes on beside the next
-// one's products: 1500 rows of 16 heads over 3500 keys 152 us (296 one after
+// one's products: 1500 rows of 16 heads over 3500 keys 147 us (296 one after
 // the other).
 constexpr int kWideCols = 128;
 template <int DHP>
