@@ -1194,7 +1194,11 @@ Plan plan_of(const AttendArgs& a) {
   const int dim = padded_dim(a.D), at_once = p.few ? (dim == 64 ? 2 : 1) : dim == 64 ? 3 : dim == 128 ? 2 : 1, slots = 256 * at_once;
   p.cut.min_chunk = 128;
   p.cut.slots = likely * a.H < 3 * slots ? slots : 0;
-  const int64_t items = p.cut.slots ? most + most / 2 + 2 * slots / a.H + 9 : most;
+  int64_t items = most;
+  if (p.cut.slots) {  // (nor more than splits of the longest sequence that the table holds)
+    const int64_t splits = (((int64_t)a.b.P << a.page_shift) + 63 + p.cut.min_chunk - 1) / p.cut.min_chunk;
+    items = std::min(most + most / 2 + 2 * slots / a.H + 9, most * splits);
+  }
   p.cut.items = (int)items;
   // An item takes about 3 us before its first key; a split's sums are written and read
   // again, which takes as long as this many keys do (35 ns a key of a wide tile's at

@@ -277,7 +277,7 @@ def attend(q, k_cache, v_cache, batch, *, scale=None, cap=0.0, window=0, slopes=
     sp = _array(slopes, "slopes", torch.float32, (Hq,), dev) if slopes is not None else 0
     fp = _array(first, "first", torch.int32, (rows,), dev) if first is not None else 0
     pp = _array(prefix, "prefix", torch.int32, (batch.n_seqs,), dev) if prefix is not None else 0
-    key = (rows, Hq, H, D)
+    key = (rows, Hq, H, D, k_cache.shape[2])
     n = batch._sizes.get(key)
     if n is None:
         n = lib.hvd_attend_workspace(batch._p, kv, Hq, rows)

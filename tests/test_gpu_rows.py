@@ -588,6 +588,17 @@ def test_a_captured_attention_alone(hvd, D, rows):
         assert torch.equal(got, hvd.attend(q, c.k_cache, c.v_cache, b))
 
 
+def test_one_batch_for_caches_of_two_page_sizes(hvd):
+    """What a call needs depends on how many keys the table can hold."""
+    small = Case([(1, 100), (2, 60)], 1, 64, 16, seed=39, max_pages=7)
+    large = Case([(1, 100), (2, 60)], 1, 64, 1024, seed=39, max_pages=7, spare=30)
+    large.pages, large.lengths = small.pages, np.array([101, 62], np.int32)
+    b = small.batch(hvd)
+    q = small.rnd(small.T, 2, 64).to(F16).cuda()
+    for c in (small, large, small):
+        check_attend(c, hvd.attend(q, c.k_cache, c.v_cache, b), q)
+
+
 def test_two_graphs_at_once(hvd):
     """Each graph has a workspace of its own."""
     c = Case([(1, 2000), (5, 300)], 2, 128, seed=37)
