@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <array>
 #include <cmath>
 #include <string>
 #include <utility>
@@ -39,17 +40,23 @@ hvd_status check_batch(const hvd_row_batch* b, int rows, int most, bool keys, Ro
   return HVD_OK;
 }
 
-// Pages, heads and tokens of one half of the cache must not overlap.
-bool apart(int64_t page, int64_t head, int64_t tok, const hvd_paged_kv& c) {
-  std::pair<int64_t, int64_t> d[] = {{page, c.n_pages}, {head, c.n_heads}, {tok, c.page_size}};
-  std::sort(d, d + 3);
-  int64_t extent = c.head_dim;
+// Dimensions of a tensor beside its contiguous one: (stride, size).
+using Dims = std::array<std::pair<int64_t, int64_t>, 3>;
+
+// Whether runs of `width` elements at these strides are apart from one another.
+bool apart(Dims d, int64_t width) {
+  std::sort(d.begin(), d.end());
+  int64_t extent = width;
   for (const auto& [stride, n] : d) {
     if (n <= 1) continue;
     if (stride < extent || stride > ((int64_t)1 << 46) / n) return false;
     extent += stride * (n - 1);
   }
   return true;
+}
+// The same for pages, heads and tokens of one half of the cache.
+bool apart(int64_t page, int64_t head, int64_t tok, const hvd_paged_kv& c) {
+  return apart({{{page, c.n_pages}, {head, c.n_heads}, {tok, c.page_size}}}, c.head_dim);
 }
 
 hvd_status check_kv(const hvd_paged_kv* c, const hvd_row_batch* b, CacheView& k, CacheView& v, int& shift) {
@@ -162,7 +169,7 @@ extern "C" hvd_status hvd_attend(const hvd_row_batch* batch, const hvd_paged_kv*
   if (!aligned(g->q, 16) || !aligned(g->out, 16)) return set_err(HVD_ERR_ARG, "q and out must be 16-byte aligned");
   for (int64_t s : {g->q_row_stride, g->q_head_stride, g->out_row_stride, g->out_head_stride})
     if (s < 0 || s % 8) return set_err(HVD_ERR_ARG, "strides of q and out must be multiples of 8");
-  if ((rows > 1 && g->out_row_stride < kv->head_dim) || (g->q_heads > 1 && g->out_head_stride < kv->head_dim))
+  if (!apart({{{g->out_row_stride, rows}, {g->out_head_stride, g->q_heads}, {0, 1}}}, kv->head_dim))
     return set_err(HVD_ERR_ARG, "rows or heads of out overlap");
   if (!aligned(g->slopes, 4) || !aligned(g->first, 4) || !aligned(g->prefix, 4))
     return set_err(HVD_ERR_ARG, "a buffer is not aligned to its elements");

@@ -155,3 +155,12 @@ def test_tensors_on_the_host_are_refused():
                  lambda: hvd.adjust_logits(z, None)):
         with pytest.raises(hvd.HvdError):
             call()
+
+
+@pytest.mark.parametrize("kw", [
+    dict(out_row_stride=64, out_head_stride=64),  # head 1 of a row is head 0 of the next one
+    dict(out_row_stride=128, out_head_stride=64), dict(out_row_stride=64, out_head_stride=128),
+    dict(out_row_stride=184, out_head_stride=64), dict(out_row_stride=1 << 60), dict(out_row_stride=0)])
+def test_attend_places_of_out_that_meet(lib, kw):
+    assert lib.hvd_attend(ref(batch()), ref(kv()), ref(attend(q=2 * A, **kw)), 4, A, 1 << 40, None) == HVD_ERR_ARG
+    assert b"out overlap" in lib.hvd_last_error()
