@@ -536,7 +536,7 @@ hvd_status hvd_append_kv(const hvd_row_batch* batch, const hvd_paged_kv* kv, con
 typedef struct {
   const void* q;           /* [rows][q_heads][head_dim], strides multiples of 8, 16-byte aligned */
   int64_t q_row_stride, q_head_stride;
-  void* out;               /* the same, rows and heads at places of their own; may be q itself */
+  void* out;               /* the same, rows and heads at places of their own; q itself (with its strides) or apart from it */
   int64_t out_row_stride, out_head_stride;
   const float* slopes;     /* nullable [q_heads] */
   const int32_t* first;    /* nullable [rows]: keys before it belong to another document */

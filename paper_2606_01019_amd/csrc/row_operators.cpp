@@ -59,6 +59,45 @@ bool apart(int64_t page, int64_t head, int64_t tok, const hvd_paged_kv& c) {
   return apart({{{page, c.n_pages}, {head, c.n_heads}, {tok, c.page_size}}}, c.head_dim);
 }
 
+// A dimension of two tensors.
+struct Dim2 {
+  int64_t a, b, n;
+};
+// Whether runs of `width` elements at the places of d[0 .. left) have an element in
+// common, b's `delta` elements from a's; those of a are apart, the longest stride
+// first.  Strides that differ where the extents meet count as a place in common.
+bool meet(const Dim2* d, int left, __int128 delta, int64_t width) {
+  __int128 ea = width, eb = width;
+  for (int i = 0; i < left; ++i) {
+    ea += (__int128)d[i].a * (d[i].n - 1);
+    eb += (__int128)d[i].b * (d[i].n - 1);
+  }
+  if (delta >= ea || delta <= -eb) return false;
+  if (left == 0 || d->a != d->b) return true;
+  // what is left once the places in this dimension are i apart; few i come near
+  const __int128 last = (__int128)d->a * (d->n - 1), ia = ea - last, ib = eb - last;
+  for (__int128 i = -(d->n - 1), near = (delta - ia) / d->a - 1; (i = std::max(i, near)) <= d->n - 1; ++i) {
+    if (delta - i * d->a <= -ib) return false;
+    if (meet(d + 1, left - 1, delta - i * d->a, width)) return true;
+  }
+  return false;
+}
+// Whether two tensors of the same sizes have a place in common; a's are apart.
+bool meet(const void* pa, const Dims& a, const void* pb, const Dims& b, int64_t width, int64_t elem) {
+  Dim2 d[3];
+  int n = 0;
+  for (int i = 0; i < 3; ++i)
+    if (a[i].second > 1) d[n++] = Dim2{a[i].first, b[i].first, a[i].second};
+  std::sort(d, d + n, [](const Dim2& x, const Dim2& y) { return x.a > y.a; });
+  return meet(d, n, ((int64_t)(uintptr_t)pb - (int64_t)(uintptr_t)pa) / elem, width);
+}
+// The same places, element by element.
+bool in_place(const void* pa, const Dims& a, const void* pb, const Dims& b) {
+  bool same = pa == pb;
+  for (int i = 0; i < 3; ++i) same = same && (a[i].second <= 1 || a[i].first == b[i].first);
+  return same;
+}
+
 hvd_status check_kv(const hvd_paged_kv* c, const hvd_row_batch* b, CacheView& k, CacheView& v, int& shift) {
   if (!c) return set_err(HVD_ERR_ARG, "null cache");
   if (c->dtype != HVD_F16 && c->dtype != HVD_BF16) return set_err(HVD_ERR_ARG, "the cache's dtype must be HVD_F16 or HVD_BF16");
@@ -169,8 +208,12 @@ extern "C" hvd_status hvd_attend(const hvd_row_batch* batch, const hvd_paged_kv*
   if (!aligned(g->q, 16) || !aligned(g->out, 16)) return set_err(HVD_ERR_ARG, "q and out must be 16-byte aligned");
   for (int64_t s : {g->q_row_stride, g->q_head_stride, g->out_row_stride, g->out_head_stride})
     if (s < 0 || s % 8) return set_err(HVD_ERR_ARG, "strides of q and out must be multiples of 8");
-  if (!apart({{{g->out_row_stride, rows}, {g->out_head_stride, g->q_heads}, {0, 1}}}, kv->head_dim))
+  const Dims to = {{{g->out_row_stride, rows}, {g->out_head_stride, g->q_heads}, {0, 1}}};
+  if (!apart(to, kv->head_dim))
     return set_err(HVD_ERR_ARG, "rows or heads of out overlap");
+  const Dims from = {{{g->q_row_stride, rows}, {g->q_head_stride, g->q_heads}, {0, 1}}};
+  if (!in_place(g->out, to, g->q, from) && meet(g->out, to, g->q, from, kv->head_dim, 2))
+    return set_err(HVD_ERR_ARG, "out shares memory with q otherwise than in its place");
   if (!aligned(g->slopes, 4) || !aligned(g->first, 4) || !aligned(g->prefix, 4))
     return set_err(HVD_ERR_ARG, "a buffer is not aligned to its elements");
   a.q = g->q;

@@ -164,3 +164,27 @@ def test_tensors_on_the_host_are_refused():
 def test_attend_places_of_out_that_meet(lib, kw):
     assert lib.hvd_attend(ref(batch()), ref(kv()), ref(attend(q=2 * A, **kw)), 4, A, 1 << 40, None) == HVD_ERR_ARG
     assert b"out overlap" in lib.hvd_last_error()
+
+
+@pytest.mark.parametrize("kw", [
+    dict(out_row_stride=512), dict(out_row_stride=64, out_head_stride=256),  # at q itself with other strides
+    dict(out=A + 2 * 256), dict(out=A + 2 * 64), dict(out=A - 2 * 64), dict(out=A + 2 * (3 * 256 + 3 * 64)),
+    dict(out=A - 2 * (3 * 256 + 3 * 64)), dict(out=A + 2 * 24), dict(out=A - 2 * 56),
+    dict(q_row_stride=0), dict(q_row_stride=0, q_head_stride=0, out=A - 2 * (4 * 256 - 64)),
+    dict(out=A + 2 * 256, q_row_stride=512, out_row_stride=512, q_head_stride=72, out_head_stride=72)])
+def test_attend_out_that_shares_memory_with_q(lib, kw):
+    assert lib.hvd_attend(ref(batch()), ref(kv()), ref(attend(**kw)), 4, A, 1 << 40, None) == HVD_ERR_ARG
+    assert b"shares memory with q" in lib.hvd_last_error()
+
+
+@pytest.mark.parametrize("kw", [
+    dict(), dict(out=A + 2 * 4 * 256), dict(out=A - 2 * 4 * 256), dict(out=2 * A, out_row_stride=512),
+    # beside q in one buffer: rows of [q, out], heads of [q, out]
+    dict(out=A + 2 * 256, q_row_stride=512, out_row_stride=512), dict(out=A - 2 * 256, q_row_stride=512, out_row_stride=512),
+    dict(out=A + 2 * 64, q_row_stride=512, q_head_stride=128, out_row_stride=512, out_head_stride=128),
+    dict(out=A + 2 * 64, q_row_stride=128, q_head_stride=512, out_row_stride=128, out_head_stride=512),
+    dict(out=A + 2 * 256, q_row_stride=0)])
+def test_attend_out_that_has_its_own_memory(lib, kw):
+    """Goes as far as the workspace's check, the last one."""
+    assert lib.hvd_attend(ref(batch()), ref(kv()), ref(attend(**kw)), 4, None, 0, None) == HVD_ERR_ARG
+    assert b"work must be" in lib.hvd_last_error()
