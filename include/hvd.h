@@ -568,7 +568,7 @@ hvd_status hvd_attend(const hvd_row_batch* batch, const hvd_paged_kv* kv, const 
 typedef struct {
   const void* logits;      /* [rows][vocab], unit column stride, aligned to its elements; type `dtype` */
   int64_t logits_stride;
-  void* out;               /* nullable; may be logits itself (with its stride) */
+  void* out;               /* nullable; logits itself (with its stride) or apart from it */
   int64_t out_stride;
   int32_t* best;           /* nullable [rows]; out or best is wanted */
   const int32_t* tokens;   /* nullable [rows] */

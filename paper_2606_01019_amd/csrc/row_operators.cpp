@@ -266,8 +266,9 @@ extern "C" hvd_status hvd_adjust_logits(const hvd_row_batch* batch, const hvd_ad
   if (!aligned(g->logits, es) || !aligned(g->out, es)) return set_err(HVD_ERR_ARG, "logits or out is not aligned to its elements");
   if (rows > 1 && (g->logits_stride < g->vocab || (g->out && g->out_stride < g->vocab)))
     return set_err(HVD_ERR_ARG, "rows overlap");
-  if (g->out == g->logits && g->out_stride != g->logits_stride && rows > 1)
-    return set_err(HVD_ERR_ARG, "out in place of logits needs their stride");
+  const Dims to = {{{g->out_stride, rows}, {0, 1}, {0, 1}}}, from = {{{g->logits_stride, rows}, {0, 1}, {0, 1}}};
+  if (g->out && !in_place(g->out, to, g->logits, from) && meet(g->out, to, g->logits, from, g->vocab, (int64_t)es))
+    return set_err(HVD_ERR_ARG, "out shares memory with logits otherwise than in their place");
   a.logits = g->logits;
   a.logits_stride = g->logits_stride;
   a.out = g->out;

@@ -188,3 +188,21 @@ def test_attend_out_that_has_its_own_memory(lib, kw):
     """Goes as far as the workspace's check, the last one."""
     assert lib.hvd_attend(ref(batch()), ref(kv()), ref(attend(**kw)), 4, None, 0, None) == HVD_ERR_ARG
     assert b"work must be" in lib.hvd_last_error()
+
+
+@pytest.mark.parametrize("kw", [
+    dict(out_stride=101), dict(out=A + 400), dict(out=A - 400), dict(out=A + 4), dict(out=A - 4 * 99),
+    dict(out=A + 4 * 100, logits_stride=200, out_stride=300), dict(out=A + 4 * 99, logits_stride=200, out_stride=200),
+    dict(dtype=0, out=A + 2), dict(dtype=1, out=A - 2 * 399)])
+def test_adjust_out_that_shares_memory_with_logits(lib, kw):
+    assert lib.hvd_adjust_logits(ref(batch()), ref(adjust(**kw)), 4, A, 1 << 40, None) == HVD_ERR_ARG
+    assert b"shares memory with logits" in lib.hvd_last_error()
+
+
+@pytest.mark.parametrize("kw", [
+    dict(), dict(out=None), dict(out=A + 1600), dict(out=A - 1600), dict(out=A + 400, logits_stride=200, out_stride=200),
+    dict(out=A - 400, logits_stride=200, out_stride=200), dict(dtype=0, out=A + 800)])
+def test_adjust_out_that_has_its_own_memory(lib, kw):
+    """Goes as far as the workspace's check, the last one."""
+    assert lib.hvd_adjust_logits(ref(batch()), ref(adjust(**kw)), 4, None, 0, None) == HVD_ERR_ARG
+    assert b"work must be" in lib.hvd_last_error()
