@@ -505,7 +505,8 @@ typedef struct {
  * 64-bit, the rotation 32-bit, and each output is rounded once to the cache's
  * type.  The other columns, and values, are rounded alone.  q_out
  * [rows][q_heads][head_dim], contiguous, of the cache's type, receives the
- * queries (0 for rows of no sequence). */
+ * queries (0 for rows of no sequence).  k and v of the cache share no memory
+ * (for hvd_attend they may); q_out overlaps nothing else. */
 typedef struct {
   const void* k;           /* [rows][n_heads][head_dim] at any strides, head_dim contiguous; type `dtype` */
   int64_t k_row_stride, k_head_stride;

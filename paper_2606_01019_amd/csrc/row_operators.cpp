@@ -166,6 +166,9 @@ extern "C" hvd_status hvd_append_kv(const hvd_row_batch* batch, const hvd_paged_
   if (!aligned(g->q_out, 16)) return set_err(HVD_ERR_ARG, "q_out must be 16-byte aligned");
   for (int64_t s : {g->k_row_stride, g->k_head_stride, g->v_row_stride, g->v_head_stride, g->q_row_stride, g->q_head_stride})
     if (s < 0) return set_err(HVD_ERR_ARG, "strides must not be negative");
+  const auto places = [&](const CacheView& c) { return Dims{{{c.page, kv->n_pages}, {c.head, kv->n_heads}, {c.tok, kv->page_size}}}; };
+  if (kv->n_pages > 0 && meet(kv->k, places(a.k), kv->v, places(a.v), kv->head_dim, 2))
+    return set_err(HVD_ERR_ARG, "keys and values share memory");
   a.n_pages = kv->n_pages;
   a.H = kv->n_heads;
   a.Hq = g->q ? g->q_heads : 0;

@@ -683,3 +683,43 @@ def test_caches_count_as_written(hvd):
     was = c.k_cache._version, c.v_cache._version
     hvd.append_kv(c.k_cache, c.v_cache, k, k, c.batch(hvd))
     assert c.k_cache._version > was[0] and c.v_cache._version > was[1]
+
+
+@pytest.mark.parametrize("dim", range(4))
+def test_keys_and_values_in_one_buffer(hvd, dim):
+    """Keys beside values, page by page, head by head or token by token."""
+    c = Case([(3, 40), (60, 3)], 2, 64, seed=61)
+    shape = (c.n_pages, 2, 16, 64)
+    c.k_cache, c.v_cache = c.rnd(*shape[:dim], 2, *shape[dim:]).to(F16).cuda().unbind(dim)
+    check_append(hvd, c, heads=4)
+    check(hvd, c, 4)
+
+
+@pytest.mark.parametrize("dim", range(3))
+def test_queries_and_results_in_one_buffer(hvd, dim):
+    c = Case([(3, 40), (60, 3)], 2, 64, seed=62, pad=1)
+    shape = (c.T, 4, 64)
+    both = c.rnd(*shape[:dim], 2, *shape[dim:]).to(F16).cuda()
+    q, out = both.unbind(dim)
+    b, kept = c.batch(hvd), q.clone()
+    hvd.attend(q, c.k_cache, c.v_cache, b, out=out)
+    assert torch.equal(q, kept)
+    check_attend(c, out, kept)
+    moved = torch.empty(c.T + 1, 4, 64, dtype=F16, device="cuda")
+    moved[:-1] = kept
+    with pytest.raises(hvd.HvdError, match="shares memory"):
+        hvd.attend(moved[:-1], c.k_cache, c.v_cache, b, out=moved[1:])
+    assert torch.equal(moved[:-1], kept)
+
+
+def test_logits_and_results_in_one_buffer(hvd):
+    both = torch.randn(7, 2, 100, device="cuda")
+    l, out = both.unbind(1)
+    b, one = hvd.RowBatch(ints([0, 6])), torch.ones(1, device="cuda")
+    want, best = hvd.adjust_logits(l, b, tokens=ints([0, 5, 5, 99, 3, 3, 3]), frequency=one)
+    assert torch.equal(hvd.adjust_logits(l, b, tokens=ints([0, 5, 5, 99, 3, 3, 3]), frequency=one, out=out)[1], best)
+    assert torch.equal(out, want)
+    kept = both.clone()
+    with pytest.raises(hvd.HvdError, match="shares memory"):
+        hvd.adjust_logits(l[1:], hvd.RowBatch(ints([0, 6])), out=l[:-1])
+    assert torch.equal(both, kept)

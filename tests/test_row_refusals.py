@@ -206,3 +206,15 @@ def test_adjust_out_that_has_its_own_memory(lib, kw):
     """Goes as far as the workspace's check, the last one."""
     assert lib.hvd_adjust_logits(ref(batch()), ref(adjust(**kw)), 4, None, 0, None) == HVD_ERR_ARG
     assert b"work must be" in lib.hvd_last_error()
+
+
+SAME = dict(v_head_stride=1024, v_token_stride=64)  # the strides of k
+
+
+@pytest.mark.parametrize("kw", [
+    dict(), SAME, dict(SAME, v=A + 2 * 64), dict(SAME, v=A - 2 * 9 * 2048), dict(SAME, v=A + 2 * (9 * 2048 + 1024 + 15 * 64)),
+    dict(SAME, v=A + 2 * 32, k_token_stride=64, k_head_stride=2048, k_page_stride=4096, v_head_stride=2048, v_page_stride=4096),
+    dict(v=A + 2 * 1024, k_page_stride=4096, v_page_stride=4096)])
+def test_append_keys_and_values_that_share_memory(lib, kw):
+    assert lib.hvd_append_kv(ref(batch()), ref(kv(**kw)), ref(append()), 4, None) == HVD_ERR_ARG
+    assert b"share memory" in lib.hvd_last_error()
