@@ -39,6 +39,7 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLazy = 8.f;     // the running maximum may lag by this (base 2)
+constexpr float kFar = 4096.f;   // larger maxima are taken off the scores themselves (base 2)
 constexpr float kCancels = 64.f;
 constexpr int kNoKey = 0x7fffffff;
 
@@ -531,9 +532,11 @@ struct Wave {
   }
 
   // Has the maximum and the sums up to date with a tile's scores; what they lack to a
-  // weight's exponent.
-  template <bool APART>
-  __device__ __forceinline__ float follow(const f32x16 (&s)[NB]) {
+  // weight's exponent.  That is the maximum times c, rounded: by at most 2^-13 up to kFar, but
+  // by more than an exponent may hold for scores past 2^30.  EXACT: whatever the
+  // maximum's size, it is taken off the scores here, which leaves what is near it exact.
+  template <bool APART, bool EXACT>
+  __device__ __forceinline__ float follow(f32x16 (&s)[NB]) {
     float top = s[0][0];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -541,7 +544,7 @@ struct Wave {
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
     top = other_half_max(top);
     // The maximum lags until a weight would pass 2^kLazy: most tiles rescale nothing
-    if (__builtin_amdgcn_ballot_w64(top * c > m * c + kLazy)) {
+    if (__builtin_amdgcn_ballot_w64(EXACT ? (top - m) * c > kLazy : top * c > m * c + kLazy)) {
       if constexpr (APART) keep_apart();
       const float mn = fmaxf(m, top);
       const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * c);
@@ -552,6 +555,14 @@ struct Wave {
         for (int i = 0; i < 16; ++i) o[d][i] *= f;
       if constexpr (APART) keep_apart();
       m = mn;
+    }
+    if constexpr (EXACT) {
+      const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[b][i] -= base;
+      return -H::kShift;
     }
     return (m == -INFINITY ? 0.f : m * c) - H::kShift;
   }
@@ -583,7 +594,8 @@ struct Wave {
   }
 
   // One tile: keys key0 .. key0 + 32 NB - 1.  masked: some column does not see some
-  // key of it.  CAREFUL: with what is not finite in V taken care of.
+  // key of it.  CAREFUL: with what is not finite in V, and scores of any size, taken care
+  // of.
   // The operands of a product are read from LDS before it begins (and half of V
   // before the softmax), which the barriers for the scheduler say: left to
   // itself it reads each just before its use.
@@ -617,7 +629,7 @@ struct Wave {
     }
     if constexpr (TURN) turn(a, col, key0, slope, s);
     if (masked) hide(a, col, key0, good, s);
-    const float mc = follow<false>(s);
+    const float mc = follow<false, CAREFUL>(s);
     s16x8 p[2 * NB];
     weigh(s, mc, p);
     if constexpr (CAREFUL) {
@@ -660,7 +672,7 @@ struct Wave {
     read_keys(lk, kf);
     __builtin_amdgcn_sched_barrier(0);
     if (masked) hide(a, col, key0, good, s);
-    const float mc = follow<true>(s);
+    const float mc = follow<true, false>(s);
     __builtin_amdgcn_sched_barrier(0);
     read_values<0, 2 * NB>(values_at(lv), vf);
     __builtin_amdgcn_sched_barrier(0);
@@ -695,9 +707,10 @@ struct Wave {
     }
   }
 
-  // Whether some dimension of some column came out as a NaN.
-  __device__ __forceinline__ bool any_nan() const {
-    bool bad = false;
+  // Whether some dimension of some column came out as a NaN, or its scores were too
+  // large for what was taken off them: then the item is done once more with care.
+  __device__ __forceinline__ bool doubtful() const {
+    bool bad = m > -INFINITY && fabsf(m * c) > kFar;
 #pragma unroll
     for (int d = 0; d < DHP / 32; ++d)
 #pragma unroll
@@ -944,7 +957,7 @@ __global__ __launch_bounds__(256, DHP == 256 ? 1 : 2) void attend_wide(AttendArg
     } else {
       run(std::false_type{});
     }
-    if (__syncthreads_or(w.any_nan())) {  // (all of them: the tiles are shared)
+    if (__syncthreads_or(w.doubtful())) {  // (all of them: the tiles are shared)
       w.reset();
       run(std::true_type{});
     }
@@ -1039,7 +1052,7 @@ __global__ __launch_bounds__(64 * few_waves<DHP>(), DHP == 256 ? 1 : 2) void att
   };
   if (first < k1) {
     run(std::false_type{});
-    if (w.any_nan()) {
+    if (w.doubtful()) {
       w.reset();
       run(std::true_type{});
     }

@@ -723,3 +723,33 @@ def test_logits_and_results_in_one_buffer(hvd):
     with pytest.raises(hvd.HvdError, match="shares memory"):
         hvd.adjust_logits(l[1:], hvd.RowBatch(ints([0, 6])), out=l[:-1])
     assert torch.equal(both, kept)
+
+
+@pytest.mark.parametrize("rows,ctx,heads", [(1, 40, 2), (1, 3000, 2), (9, 40, 2), (70, 300, 6), (40, 2500, 4)])
+@pytest.mark.parametrize("D,dtype", [(64, F16), (128, BF16), (256, F16)])
+@pytest.mark.parametrize("scale", [1.0, 2.0 ** 9, 2.0 ** 17, 2.0 ** 22, 2.0 ** 40, 2.0 ** 110, -2.0 ** 22])
+@pytest.mark.parametrize("biased", [False, True])
+def test_attend_scores_of_any_size(hvd, rows, ctx, heads, D, dtype, scale, biased):
+    """Small whole numbers, so that every score is exact (up to 2^122): its place below the
+    row's largest is what counts, however large both are.  Tolerance: half a step of the type for
+    a weight and for the result; 2^-12 for two base-2 maxima of up to 2^12 that are rounded
+    before they are taken off (half a step of numbers in [2^11, 2^12) is 2^-13; larger ones
+    are taken off exactly); 2^-23 for each of the sums' operations; and three
+    roundings of an exponent of up to 2^7 (smaller weights are nothing)."""
+    c = Case([(rows, ctx)], 2, D, dtype=dtype, seed=rows + D)
+    c.k_cache.copy_(torch.randint(-8, 9, c.k_cache.shape, generator=c.g))
+    q = torch.randint(-8, 9, (rows, heads, D), generator=c.g).to(dtype).cuda()
+    got = hvd.attend(q, c.k_cache, c.v_cache, c.batch(hvd), scale=scale,
+                     slopes=torch.zeros(heads, device="cuda") if biased else None).double()
+    L, u = rows + ctx, torch.finfo(dtype).eps / 2
+    ids = torch.from_numpy(c.pages[0]).long().cuda()
+    seen = torch.arange(L, device="cuda")[None, :] <= ctx + torch.arange(rows, device="cuda")[:, None]
+    for h in range(heads):
+        K, V = (t[ids, h * 2 // heads].reshape(-1, D)[:L].double() for t in (c.k_cache, c.v_cache))
+        x = torch.mm(q[:, h].double(), K.t().contiguous()) * scale
+        p = torch.softmax(x.masked_fill(~seen, -math.inf), 1)
+        o, A = torch.mm(p, V), torch.mm(p, V.abs())
+        d = 2.0 ** -12 + 3 * 2.0 ** -24 * 2 ** 7 + L * 2.0 ** -23
+        tol = 1.02 * (u * o.abs() + (u + 2 * d) * A + L * 2.0 ** -32 * V.abs().amax(0))
+        over = (got[:, h] - o).abs() - tol
+        assert bool((over <= 0).all()), (h, float(over.max()))
