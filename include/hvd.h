@@ -531,7 +531,8 @@ hvd_status hvd_append_kv(const hvd_row_batch* batch, const hvd_paged_kv* kv, con
  *     x = scale * q.k,  x = cap * tanh(x / cap),  x = x - slopes[h] * |p - j|
  * out = sum exp(x) v / sum exp(x), 0 for a row that sees no key (or whose scores
  * are all -inf) and for rows of no sequence.  What a key or value holds that a
- * row does not see does not reach it, infinities and NaNs included.  q and out
+ * row does not see does not reach it, infinities and NaNs included.  Scores past
+ * 2^125 count as infinite (one of +inf makes a row NaN).  q and out
  * have the cache's type; scores, sums and outputs are 32-bit, weights are
  * rounded to the cache's type for the product with the values. */
 typedef struct {
@@ -542,7 +543,7 @@ typedef struct {
   const float* slopes;     /* nullable [q_heads] */
   const int32_t* first;    /* nullable [rows]: keys before it belong to another document */
   const int32_t* prefix;   /* nullable [n_seqs]: keys that all rows of the sequence see */
-  float scale;
+  float scale;             /* in [-2^127, 2^127] */
   float cap;               /* 0: none */
   int32_t q_heads;
   int32_t window;          /* 0: none */

@@ -203,7 +203,8 @@ extern "C" hvd_status hvd_attend(const hvd_row_batch* batch, const hvd_paged_kv*
   AttendArgs a{};
   if (!g) return set_err(HVD_ERR_ARG, "null arguments");
   if (hvd_status st = check_attend(batch, kv, g->q_heads, rows, a); st != HVD_OK) return st;
-  if (!std::isfinite(g->scale)) return set_err(HVD_ERR_ARG, "scale must be finite");
+  // (its factor to base-2 exponents has to be finite too)
+  if (!(std::fabs(g->scale) <= 0x1p127f)) return set_err(HVD_ERR_ARG, "scale must be in [-2^127, 2^127]");
   if (!(g->cap >= 0.f) || !std::isfinite(g->cap)) return set_err(HVD_ERR_ARG, "cap must be finite and >= 0");
   if (g->window < 0) return set_err(HVD_ERR_ARG, "window must be >= 0");
   if (rows == 0) return HVD_OK;

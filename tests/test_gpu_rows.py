@@ -753,3 +753,28 @@ def test_attend_scores_of_any_size(hvd, rows, ctx, heads, D, dtype, scale, biase
         tol = 1.02 * (u * o.abs() + (u + 2 * d) * A + L * 2.0 ** -32 * V.abs().amax(0))
         over = (got[:, h] - o).abs() - tol
         assert bool((over <= 0).all()), (h, float(over.max()))
+@pytest.mark.parametrize("rows,D", [(1, 64), (40, 128), (40, 256)])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("cap", [0.0, 30.0])
+def test_attend_the_largest_scale(hvd, rows, D, sign, cap):
+    """Queries of 2^-14 in one place and keys up to 2^-22 leave scores of up to 2^91 at
+    a scale of 2^127: one-hot weights, or a cap reached, by both forms."""
+    c = Case([(rows, 100)], 1, D, dtype=BF16, seed=rows)
+    c.k_cache.mul_(2.0 ** -24)
+    q = torch.zeros(c.T, 2, D, dtype=BF16, device="cuda")
+    q[..., 3] = 2.0 ** -14
+    got = hvd.attend(q, c.k_cache, c.v_cache, c.batch(hvd), scale=sign * 2.0 ** 127, cap=cap)
+    assert bool(torch.isfinite(got).all())
+    ids = torch.from_numpy(c.pages[0]).long().cuda()
+    K, V = (t[ids, 0].reshape(-1, D).double() for t in (c.k_cache, c.v_cache))
+    for r in range(rows):
+        n = 100 + r + 1
+        x = sign * K[:n, 3] * 2.0 ** 113
+        p = torch.softmax(cap * torch.tanh(x / cap) if cap else x, 0)
+        o, A = p @ V[:n], p @ V[:n].abs()
+        # a score is one product, exact; half a step for a weight and for the result, the cap's 8 roundings
+        tol = 1.02 * (2.0 ** -8 * (o.abs() + A) + (2 * 8 * 2.0 ** -23 * cap + n * 2.0 ** -22) * A)
+        assert bool(((got[r].double() - o).abs() <= tol).all())
+    for bad in (1.8e38, -2.4e38, math.inf, math.nan):
+        with pytest.raises(hvd.HvdError, match="scale"):
+            hvd.attend(q, c.k_cache, c.v_cache, c.batch(hvd), scale=bad)

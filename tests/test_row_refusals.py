@@ -218,3 +218,10 @@ SAME = dict(v_head_stride=1024, v_token_stride=64)  # the strides of k
 def test_append_keys_and_values_that_share_memory(lib, kw):
     assert lib.hvd_append_kv(ref(batch()), ref(kv(**kw)), ref(append()), 4, None) == HVD_ERR_ARG
     assert b"share memory" in lib.hvd_last_error()
+
+
+@pytest.mark.parametrize("scale", [1.8e38, -1.8e38, 3.4e38, 2.4e38, float("-inf")])
+def test_attend_a_scale_whose_exponents_have_no_factor(lib, scale):
+    """scale log2 e is infinite from 2.36e38 on."""
+    assert lib.hvd_attend(ref(batch()), ref(kv()), ref(attend(scale=scale)), 4, A, 1 << 40, None) == HVD_ERR_ARG
+    assert b"scale" in lib.hvd_last_error()
