@@ -270,6 +270,8 @@ def attend(q, k_cache, v_cache, batch, *, scale=None, cap=0.0, window=0, slopes=
     scale = D ** -0.5 if scale is None else scale if type(scale) is float else _number(scale, "scale")
     if not (abs(scale) <= 1.7014118346046923e38 and abs(cap) <= 3.4028234663852886e38):
         _refuse("scale must be in [-2^127, 2^127] and cap finite")
+    if cap != 0.0 and cap < 2.0 ** -149:  # (one that is 0 in 32 bits would be none)
+        _refuse("cap must be 0 or at least 2^-149")
     if type(window) is not int:
         window = _op._integer(window, "window")
     if not 0 <= window < 1 << 31:

@@ -778,3 +778,15 @@ def test_attend_the_largest_scale(hvd, rows, D, sign, cap):
     for bad in (1.8e38, -2.4e38, math.inf, math.nan):
         with pytest.raises(hvd.HvdError, match="scale"):
             hvd.attend(q, c.k_cache, c.v_cache, c.batch(hvd), scale=bad)
+
+
+def test_attend_a_cap_that_32_bits_do_not_hold(hvd):
+    """Rounded to 0 it would be none; the least that there is makes all weights equal."""
+    c = Case([(2, 20)], 1, 64, seed=63)
+    q = c.rnd(c.T, 2, 64).to(F16).cuda()
+    b = c.batch(hvd)
+    for cap in (1e-46, 1e-300, -1e-46):
+        with pytest.raises(hvd.HvdError, match="cap"):
+            hvd.attend(q, c.k_cache, c.v_cache, b, cap=cap)
+    for cap in (2.0 ** -149, 1e-40, 2.0 ** -126):
+        check_attend(c, hvd.attend(q, c.k_cache, c.v_cache, b, cap=cap), q, cap=cap)
