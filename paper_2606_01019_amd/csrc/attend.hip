@@ -258,7 +258,7 @@ __device__ __forceinline__ Column column_of(const AttendArgs& a, const Item& it,
     if (to < 64) c.see = to > 0 ? c.see & ((1ull << to) - 1) : 0;
   }
   c.lo = first;
-  if (a.window > 0) c.lo = max(c.lo, c.pos - a.window + 1);
+  if (a.window > 0) c.lo = (int)max((int64_t)c.lo, (int64_t)c.pos - a.window + 1);
   c.hi = c.pos + 1;
   if (a.b.tree) c.hi = c.ctx;
   else if (a.prefix && in_seq) c.hi = max(c.hi, a.prefix[it.s]);

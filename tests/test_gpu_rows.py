@@ -790,3 +790,18 @@ def test_attend_a_cap_that_32_bits_do_not_hold(hvd):
             hvd.attend(q, c.k_cache, c.v_cache, b, cap=cap)
     for cap in (2.0 ** -149, 1e-40, 2.0 ** -126):
         check_attend(c, hvd.attend(q, c.k_cache, c.v_cache, b, cap=cap), q, cap=cap)
+
+
+@pytest.mark.parametrize("rows", [3, 60])
+@pytest.mark.parametrize("window", [(1 << 31) - 1, (1 << 31) - 8])
+def test_attend_a_window_wider_than_any_distance(hvd, rows, window):
+    """Hides nothing, from rows before the first key either (a length less than the rows),
+    which see a prefix."""
+    c = Case([(rows, 40), (rows, 0)], 1, 64, seed=64)
+    q = c.rnd(c.T, 2, 64).to(F16).cuda()
+    check_attend(c, hvd.attend(q, c.k_cache, c.v_cache, c.batch(hvd), window=window), q)
+    c.lengths[:] = [2, 1]
+    prefix = ints([2, 1])
+    want = hvd.attend(q, c.k_cache, c.v_cache, c.batch(hvd), prefix=prefix)
+    assert want.any(-1).all()
+    assert torch.equal(hvd.attend(q, c.k_cache, c.v_cache, c.batch(hvd), prefix=prefix, window=window), want)
