@@ -345,10 +345,10 @@ __device__ __forceinline__ int afresh(int v) {
 // 16 bytes per lane from base + off (bytes; a wave-uniform base, 32 bits per lane)
 // to LDS at dst + 16 * lane.  In assembly because the compiler, which cannot tell
 // the tiles apart, would have a transposing read of one tile wait for the
-// copies to the other; the waits are the callers'.  (m0 takes a cycle to arrive;
-// nothing else here uses it.)
+// copies to the other; the waits are the callers'.  (m0 holds the place: an operand, so
+// that the compiler writes it and knows of it; it takes a cycle to arrive.)
 __device__ __forceinline__ void copy_to_lds(const char* base, uint32_t off, uint32_t dst) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(off), "s"(base) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(dst), "v"(off), "s"(base) : "memory");
 }
 
 // Copies of N * KPI keys of a tile to LDS, K and V: whole groups of 16, or a part
