@@ -53,7 +53,6 @@ struct Half<false> {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
   }
   __device__ static uint16_t bits(float v) { return f2h(v); }
-  __device__ static float value(uint16_t b) { return h2f(b); }
 };
 template <>
 struct Half<true> {
@@ -63,7 +62,6 @@ struct Half<true> {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   }
   __device__ static uint16_t bits(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
-  __device__ static float value(uint16_t b) { return bf2f(b); }
 };
 
 // A value of the lane 32 away.
@@ -667,7 +665,6 @@ struct Wave {
   __device__ __forceinline__ void piped_step(const AttendArgs& a, const Column& col, const unsigned char* lk, const unsigned char* lv,
                                              int key0, uint64_t good, bool masked, float slope, f32x16 (&s)[NB]) {
     static_assert(NB == 1);
-    const int h = (threadIdx.x & 63) >> 5;
     s16x8 kf[DHP / 16][NB], vf[2 * NB][DHP / 32], p[2 * NB];
     read_keys(lk, kf);
     __builtin_amdgcn_sched_barrier(0);
