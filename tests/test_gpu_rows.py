@@ -805,3 +805,150 @@ def test_attend_a_window_wider_than_any_distance(hvd, rows, window):
     want = hvd.attend(q, c.k_cache, c.v_cache, c.batch(hvd), prefix=prefix)
     assert want.any(-1).all()
     assert torch.equal(hvd.attend(q, c.k_cache, c.v_cache, c.batch(hvd), prefix=prefix, window=window), want)
+
+
+# ------------------------------------------------- many keys, by whole matrices
+
+def check_long(c, got, q, cap=0.0, first=None):
+    """attend_ref for chains over many keys, by matrices of 64 bits, with its tolerance
+    (cap as in test_attend_tiles_of_many_keys).  A weight of a value that is not finite
+    counts as one wherever it is not 0; a score that is a NaN makes its row one."""
+    g, u, scale = got.double(), torch.finfo(q.dtype).eps / 2, c.D ** -0.5
+    ids = torch.from_numpy(c.pages).long().cuda()
+    for s, (n, ctx) in enumerate(c.sizes):
+        if n == 0:
+            continue
+        L, a = n + ctx, int(c.starts[s])
+        j = torch.arange(L, device="cuda")
+        page = ids[s][j // c.page]
+        there = (page >= 0) & (page < c.n_pages)
+        at = torch.where(there, page, 0)
+        seen = (j[None, :] <= ctx + torch.arange(n, device="cuda")[:, None]) & there
+        if first is not None:
+            seen &= j[None, :] >= first[a:a + n, None]
+        for h in range(q.shape[1]):
+            K, V = (t[at, h * c.H // q.shape[1], j % c.page].double() for t in (c.k_cache, c.v_cache))
+            Q = q[a:a + n, h].double()
+            x = (torch.mm(Q, K.t().contiguous()) * scale).masked_fill(~seen, 0)
+            big = (torch.mm(Q.abs(), K.abs().t().contiguous()) * scale).masked_fill(~seen, 0).nan_to_num(0).amax(1)
+            nan_row = x.isnan().any(1, keepdim=True)
+            d = (c.D + 8) * 2.0 ** -23 * big
+            if cap:
+                x = cap * torch.tanh(x / cap)
+                d = d + 8 * 2.0 ** -23 * big.clamp(min=cap)
+            x = x.nan_to_num(0)
+            d = d + 8 * 2.0 ** -23 * x.abs().amax(1)
+            p = torch.softmax(x.masked_fill(~seen, -math.inf), 1)
+            plain = torch.where(V.isfinite(), V, 0.0)
+            o, A = torch.mm(p, plain), torch.mm(p, plain.abs())
+            up, down, bad = (torch.mm((p > 0).double(), w.double()) > 0 for w in (V == math.inf, V == -math.inf, V.isnan()))
+            bad = bad | (up & down) | nan_row
+            want = torch.where(up, math.inf, torch.where(down, -math.inf, o))
+            keys = seen.sum(1)[:, None].double()
+            tol = 1.02 * (u * o.abs() + (u + 2 * d[:, None] + keys * 2.0 ** -23) * A + keys * 2.0 ** -32 * plain.abs().amax(0))
+            mine = g[a:a + n, h]
+            assert torch.equal(mine.isnan(), bad), (s, h)
+            fine = ~(up | down | bad)
+            assert torch.equal(mine[(up | down) & ~bad], want[(up | down) & ~bad]), (s, h)
+            over = ((mine - o).abs() - tol)[fine]
+            assert over.numel() == 0 or float(over.max()) <= 0, (s, h, float(over.max()))
+
+
+@pytest.mark.parametrize("D,dtype,long", [(64, F16, 9000), (128, BF16, 9000), (72, F16, 4700), (256, BF16, 4500), (256, F16, 2200)])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+def test_attend_tokens_over_many_keys_in_one_piece(hvd, D, dtype, long, cap):
+    """A token each of so many sequences that no keys are split: a wave looks at the page
+    table again and again, pages without a place among those it finds there."""
+    sizes = [(1, (s * 7) % 50) for s in range(100)]
+    sizes[0], sizes[41], sizes[99] = (1, long), (1, long - 333), (1, long // 2 + 77)
+    c = Case(sizes, 16, D, dtype=dtype, seed=D)
+    for k in (0, 70, 129, 140, 141, 142, 200, 256, 270):
+        if k * 16 < long:
+            c.pages[0, k] = -1 if k % 2 else c.n_pages + k
+    q = c.rnd(c.T, 16, D).to(dtype).cuda()
+    check_long(c, hvd.attend(q, c.k_cache, c.v_cache, c.batch(hvd), cap=cap), q, cap)
+
+
+@pytest.mark.parametrize("seqs,rows,H,G", [(8, 40, 8, 8), (3, 9, 8, 4), (5, 64, 2, 4), (20, 3, 4, 4), (62, 1, 8, 1), (70, 2, 8, 2)])
+def test_attend_splits_of_many_lengths(hvd, seqs, rows, H, G):
+    c = Case([(rows, 4000 + 61 * (s % 17) if s % 3 else 900 + s) for s in range(seqs)], H, 64, seed=seqs)
+    q = c.rnd(c.T, H * G, 64).to(F16).cuda()
+    check_long(c, hvd.attend(q, c.k_cache, c.v_cache, c.batch(hvd)), q)
+
+
+@pytest.mark.parametrize("rows", [1, 5, 60])
+@pytest.mark.parametrize("D,dtype", [(64, F16), (128, BF16), (200, F16), (256, BF16)])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+def test_attend_what_is_not_finite_in_some_splits(hvd, rows, D, dtype, cap):
+    """Infinities and NaNs among 3000 keys, seen and hidden, of which most splits see none."""
+    c = Case([(rows, 3000), (rows, 2000)], 2, D, dtype=dtype, seed=rows + D)
+    inf, nan = math.inf, math.nan
+
+    def put(t, s, head, key, dim, v):
+        t[int(c.pages[s, key // 16]), head, key % 16, dim] = v
+
+    for key in range(64):  # before the first sequence's documents
+        put(c.k_cache, 0, 0, key, slice(None), nan)
+        put(c.v_cache, 0, 0, key, slice(None), inf if key % 2 else nan)
+    put(c.v_cache, 0, 0, 100, 3, inf)
+    put(c.v_cache, 0, 0, 2500, 3, -inf)  # both signs, apart: a NaN
+    put(c.v_cache, 0, 0, 1500, 4, nan)
+    put(c.v_cache, 0, 0, 2900, 5, inf)
+    put(c.v_cache, 0, 0, 200, 6, -inf)
+    put(c.v_cache, 0, 0, 2800, 6, -inf)
+    put(c.v_cache, 0, 0, 3000 + rows - 1, 7, inf)  # the last row's own
+    put(c.k_cache, 0, 1, 1000, 0, nan)  # a score: all rows of this head
+    put(c.k_cache, 1, 1, 2000 + rows - 1, 0, nan)  # the last row's of this one
+    first = torch.full((c.T,), 64, dtype=torch.int32, device="cuda")
+    q = c.rnd(c.T, 4, D).to(dtype).cuda()
+    got = hvd.attend(q, c.k_cache, c.v_cache, c.batch(hvd), cap=cap, first=first)
+    check_long(c, got, q, cap, first)
+    assert int(got.isfinite().sum()) == got.numel() - 2 * (4 * rows + 1) - 2 * rows * D - 2 * D
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [(1, 3), (2, 60)])
+def test_adjust_in_place_of_strided_logits_writes_nothing_else(hvd, dtype, rows):
+    rng = np.random.default_rng(9)
+    T, V = sum(rows) + 2, 9001
+    base = torch.from_numpy(rng.normal(size=T * (V + 2) + 3).astype(np.float32)).cuda().to(dtype)
+    l = torch.as_strided(base, (T, V), (V + 2, 1), 1)
+    kw = penalties(rng, 2, V)
+    starts = [0, rows[0], sum(rows)]
+    out, best = check_adjust(hvd, starts, l, **kw)
+    kept = base.clone()
+    again, gbest = hvd.adjust_logits(l, hvd.RowBatch(ints(starts)), out=l, **kw)
+    assert again.data_ptr() == l.data_ptr() and torch.equal(gbest, best) and same(l, out)
+    torch.as_strided(kept, (T, V), (V + 2, 1), 1).copy_(out)
+    assert torch.equal(base, kept)
+
+
+@pytest.mark.parametrize("starts", [[0, 30, 3], [2, 4, 34], [0, 1000, -5], [-7, 40, 34], [34, 34, 0], [1 << 30, -1 << 30, 9]])
+@pytest.mark.parametrize("lengths", [[904, 80], [3, -1], [(1 << 31) - 1, -1 << 31]])
+@pytest.mark.parametrize("tree", [False, True])
+def test_batches_that_are_none_reach_no_other_memory(hvd, starts, lengths, tree):
+    """Starts that go back or leave the rows, and lengths of anything: rows, keys and
+    pages that do not exist are neither read nor written."""
+    c = Case([(4, 900), (30, 50)], 2, 64, seed=65, tree=tree)
+    mine = sorted(set(c.pages[c.pages >= 0].tolist()))
+    q, k = c.rnd(c.T, 4, 64).to(F16).cuda(), c.rnd(c.T, 2, 64).cuda()
+    c.starts[:], c.lengths[:] = starts, lengths
+    b = c.batch(hvd)
+    room = torch.full((c.T + 6, 6, 64), 7.0, dtype=F16, device="cuda")
+    out = room[3:-3, 1:5]
+    hvd.attend(q, c.k_cache, c.v_cache, b, out=out)
+    edge = room.clone()
+    edge[3:-3, 1:5] = 7
+    assert bool((edge == 7).all())
+    kept = c.k_cache.clone(), c.v_cache.clone()
+    hvd.append_kv(c.k_cache, c.v_cache, k, k, b, q=q.float())
+    others = [i for i in range(c.n_pages) if i not in mine]
+    for new, old in zip((c.k_cache, c.v_cache), kept):
+        assert torch.equal(new[others], old[others])
+        # (no more places than rows)
+        assert int((new != old).any(-1).any(1).sum()) <= c.T
+    wide = torch.full((c.T + 6, 110), 7.0, device="cuda")
+    hvd.adjust_logits(torch.randn(c.T, 100, device="cuda"), b, tokens=torch.full((c.T,), 5, dtype=torch.int32, device="cuda"),
+                      frequency=torch.ones(2, device="cuda"), out=wide[3:-3, 5:105])
+    wide[3:-3, 5:105] = 7
+    assert bool((wide == 7).all())
