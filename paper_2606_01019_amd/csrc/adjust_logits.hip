@@ -23,7 +23,7 @@
 // Bound by memory for many rows: a row's logits of the part are on their way to
 // registers before the words are ready, and only touched tokens cost more than
 // a copy.  905 rows of 128256 32-bit logits, everything given: 233 us, 4.0 TB/s
-// (a large copy: 4.7); one row, 16 us, bound by the call itself (kernels: 8).
+// (a large copy: 4.7 to 4.8); one row, 16 to 17 us, bound by the call itself (kernels: 8).
 #include "common.h"
 #include "kernels.h"
 #include "rows.h"
@@ -364,7 +364,12 @@ __global__ __launch_bounds__(kThreads) void best_of_parts(const uint64_t* part, 
   if (lane == 0) best[row] = v ? (int32_t)(0xffffffffu - (uint32_t)v) : -1;
 }
 
-// The vocabulary's parts and the rows of a workgroup.
+// The vocabulary's parts and the rows of a workgroup.  Small parts while the rows do not
+// fill the card: up to 8 rows of 128256 logits 7.7 to 9.5 us of kernels, with large ones 9.9
+// to 12.2; every part reads the whole history, so that 33 rows with 4096 tokens take 18.3
+// in place of 15.7 (between them, 9 to 16 rows would still gain 2).  Runs of rows share
+// a count: one for every 4096 workgroups there would be takes 905 rows in 233 us, one for
+// every 2048 254 and every 8192 275.
 struct Plan {
   bool small;  // parts of 2048 tokens
   int segs, run;

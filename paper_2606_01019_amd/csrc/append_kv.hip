@@ -6,13 +6,14 @@
 // pages[(ctx + i) / page].  With the angle t = position * freqs[j] a pair (a, b)
 // becomes (a cos t - b sin t, b cos t + a sin t); pairs are (j, j + rot / 2) or
 // neighbours.  The angle is taken in 64 bits and reduced to a fraction of a turn
-// there, so that far positions lose nothing; its cosine and sine, and the
-// rotation, are 32-bit, and each output is rounded once to the cache's type.
+// there: off by the product's three roundings, 5e-7 radians at position 2^31 and less
+// before it.  Its cosine and sine, and the rotation, are 32-bit, and each output is
+// rounded once to the cache's type.
 //
 // Bound by memory for many rows and by latency for few.  A workgroup takes 4 rows
 // (parts of one row where there are fewer than 1024): its threads compute each row's
 // cosines and sines once for all heads, into LDS, and then go over the rows' octets
-// of columns.  16437 rows of 20 heads of 80: 30 us, 3.5 TB/s; 878 rows of 48 heads of
+// of columns.  16437 rows of 20 heads of 80: 27 to 30 us, 3.5 to 3.9 TB/s; 878 rows of 48 heads of
 // 128 from 32 bits 9.7 us.
 #include "common.h"
 #include "kernels.h"

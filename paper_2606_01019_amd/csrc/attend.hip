@@ -141,8 +141,10 @@ __device__ __forceinline__ int even_chunk(int range, int splits) { return (int)(
 // when the last workgroup would be done -- its items in rounds of equal length or
 // one after the other, whichever is sooner.  (8 trees over 8192 keys 162 us when
 // it came, with 3 items for 2 slots throughout 178; one tree over 16384 keys 36 and 49.)
+// The other 15 are 0.43 to 2.25 of a slot's share of the keys, in even steps: from more
+// than two rounds of items to less than half of one.
 constexpr int kWhole = 1 << 30;
-constexpr float kStore = 60.f;  // keys' time that the last stores of a split take
+constexpr float kStore = 60.f;  // keys' time that the last stores of a split take (with 0 all cases timed stayed within 1%)
 __device__ __forceinline__ int chunk_of(const AttendArgs& a, const Cut& c, const Load& first) {
   if (c.slots == 0) return kWhole;
   const int lane = threadIdx.x & 63;
@@ -186,7 +188,11 @@ __device__ __forceinline__ int chunk_of(const AttendArgs& a, const Cut& c, const
   const float turns = items / slots, path = most + c.item + (pick ? kStore : 0.f);
   float end = share + turns * c.item + (turns > 1.f ? most : 0.f);
   end = fmaxf(fminf(end, ceilf(turns - 0.001f) * path), path) + (pick ? turns * c.split : 0.f);
-  if (pick == 0) end *= a.first ? 0.7f : 0.95f;  // (documents' tiles are shorter than that)
+  // Whole tiles unless splits are clearly sooner: with 1 in place of both factors 4
+  // prompts 148 -> 188 us and packed prompts of documents 173 -> 206.  Documents' tiles are
+  // shorter than their range, by how much only their rows tell: with 0.95 they are split
+  // (207 us); other batches with a `first` came out the same with either.
+  if (pick == 0) end *= a.first ? 0.7f : 0.95f;
   const int best = wave_all((int)((__float_as_uint(end) & ~15u) | pick), [](int x, int y) { return x < y ? x : y; }) & 15;
   const int chunk = __builtin_amdgcn_readlane(mine, best);
   const float all = wave_sum((float)first.tiles * (float)splits_of(first.range, chunk));
@@ -705,7 +711,9 @@ struct Wave {
   }
 
   // Whether some dimension of some column came out as a NaN, or its scores were too
-  // large for what was taken off them: then the item is done once more with care.
+  // large for what was taken off them: then the item is done once more with care, which
+  // takes about three times as long (2048 rows over 4048 keys 124 -> 464 us in all); a branch
+  // per tile in its place cost ordinary scores up to 3%.
   __device__ __forceinline__ bool doubtful() const {
     bool bad = m > -INFINITY && fabsf(m * c) > kFar;
 #pragma unroll
@@ -825,8 +833,8 @@ __device__ __forceinline__ void tell_where(const AttendArgs& a, const Part& part
 
 // Many columns: four waves of 32 share the tiles of 64 keys, one being copied while
 // one is worked on.  Bound by the matrix cores and what is issued beside them, two
-// workgroups a CU: 2048 rows of 32 heads of 128 over 16384 keys 533 us, 0.97
-// PFLOP/s (a large product: 1.2).  Where a key is 256 wide a wave has its vector unit
+// workgroups a CU: 2048 rows of 32 heads of 128 over 16384 keys 517 to 549 us, from
+// card to card, 0.94 to 1.0 PFLOP/s (a large product: 1.2 to 1.36).  Where a key is 256 wide a wave has its vector unit
 // to itself, and a tile is two steps of 32 keys whose softmax goes on beside the next
 // one's products: 1500 rows of 16 heads over 3500 keys 147 us (296 one after
 // the other).
@@ -1196,6 +1204,8 @@ Plan plan_of(const AttendArgs& a) {
   Plan p{};
   const int64_t cols = (int64_t)a.b.T * (a.Hq / a.H);
   const int seqs = std::min(a.b.S, a.b.T);
+  // One form for the whole call, by the mean: what the sequences' rows are the host does
+  // not know.  (127 tokens and a prompt's 512 rows in one call 662 us, apart 412 + 164.)
   p.few = cols <= (int64_t)32 * std::max(1, seqs);
   p.cut.cols = p.few ? kFewCols : kWideCols;
   const int64_t most = cols / p.cut.cols + std::min(a.b.S + 1, a.b.T);  // tiles there can be
@@ -1203,6 +1213,8 @@ Plan plan_of(const AttendArgs& a) {
   // workgroups at once, by a kernel's registers and the LDS of its tiles
   const int dim = padded_dim(a.D), at_once = p.few ? (dim == 64 ? 2 : 1) : dim == 64 ? 3 : dim == 128 ? 2 : 1, slots = 256 * at_once;
   p.cut.min_chunk = 128;
+  // Three rounds of whole tiles or more are not split, nor looked at by the join.  (By counts
+  // alone: one sequence of 131072 keys among 94 of 1024 takes 182 us, among 127 1200.)
   p.cut.slots = likely * a.H < 3 * slots ? slots : 0;
   int64_t items = most;
   if (p.cut.slots) {  // (nor more than splits of the longest sequence that the table holds)
@@ -1212,7 +1224,9 @@ Plan plan_of(const AttendArgs& a) {
   p.cut.items = (int)items;
   // An item takes about 3 us before its first key; a split's sums are written and read
   // again, which takes as long as this many keys do (35 ns a key of a wide tile's at
-  // its matrix products' rate, a narrow one's keys at the memory's).
+  // its matrix products' rate, a narrow one's keys at the memory's).  Half or twice as much
+  // for an item, or twice for a split, changed no case timed by more than 1%; half for a
+  // split took 4 prompts from 148 to 200 us.
   p.cut.item = 80.f;
   p.cut.split = p.few ? 64.f : dim == 256 ? 250.f : 400.f;
   p.blocks = (int)(items * a.H);

@@ -200,7 +200,7 @@ def append_kv(k_cache, v_cache, k, v, batch, *, q=None, freqs=None, interleaved=
     columns of each head, in halves or in neighbouring pairs (``interleaved``);
     without it nothing is rotated.  ``positions`` (int32, a row each) takes the
     place of the batch's.  k, v and q have one dtype (float16, bfloat16 or
-    float32) and any row and head strides."""
+    float32) and any row and head strides; the caches share no memory."""
     _library()
     torch = _op.torch
     if _op._forward_ad._current_level >= 0:
@@ -248,8 +248,8 @@ def attend(q, k_cache, v_cache, batch, *, scale=None, cap=0.0, window=0, slopes=
     its own -- with the batch's tree, of this step's those on its path -- within
     ``window`` positions, from key ``first``[row] (int32) on, and its sequence's
     first ``prefix``[seq] (int32) keys even where they come after it.  Rows that
-    see nothing, and rows of no sequence, are 0.  ``out`` (which may be q)
-    receives the result."""
+    see nothing, and rows of no sequence, are 0.  ``out`` (q itself, or memory
+    apart from q's) receives the result."""
     lib = _library()
     torch = _op.torch
     if _op._forward_ad._current_level >= 0:
@@ -327,8 +327,8 @@ def adjust_logits(logits, batch, *, tokens=None, history=None, history_lengths=N
     ``presence`` if it was at all.  ``bias`` [n_seqs, n] (float32) is added to the
     tokens ``bias_ids`` (int32; ids outside the vocabulary are empty places, the
     last of equal ids counts); tokens whose bit in ``allowed`` (int32 [rows or 1,
-    ceil(vocab / 32)]) is 0 become -inf.  ``out`` (which may be logits) receives
-    the result; with ``write`` false only the best tokens are computed."""
+    ceil(vocab / 32)]) is 0 become -inf.  ``out`` (logits itself, or memory
+    apart from them) receives the result; with ``write`` false only the best tokens are computed."""
     lib = _library()
     torch = _op.torch
     if _op._forward_ad._current_level >= 0:
