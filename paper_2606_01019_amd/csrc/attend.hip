@@ -537,8 +537,9 @@ struct Wave {
 
   // Has the maximum and the sums up to date with a tile's scores; what they lack to a
   // weight's exponent.  That is the maximum times c, rounded: by at most 2^-13 up to kFar, but
-  // by more than an exponent may hold for scores past 2^30.  EXACT: whatever the
-  // maximum's size, it is taken off the scores here, which leaves what is near it exact.
+  // by more than an exponent may hold for scores past 2^30.  EXACT: a larger maximum
+  // is taken off the scores here, which leaves what is near it exact; a column with a smaller
+  // one has the same bits as without.
   template <bool APART, bool EXACT>
   __device__ __forceinline__ float follow(f32x16 (&s)[NB]) {
     float top = s[0][0];
@@ -548,7 +549,7 @@ struct Wave {
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
     top = other_half_max(top);
     // The maximum lags until a weight would pass 2^kLazy: most tiles rescale nothing
-    if (__builtin_amdgcn_ballot_w64(EXACT ? (top - m) * c > kLazy : top * c > m * c + kLazy)) {
+    if (__builtin_amdgcn_ballot_w64(EXACT && fabsf(m * c) > kFar ? (top - m) * c > kLazy : top * c > m * c + kLazy)) {
       if constexpr (APART) keep_apart();
       const float mn = fmaxf(m, top);
       const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * c);
@@ -561,12 +562,13 @@ struct Wave {
       m = mn;
     }
     if constexpr (EXACT) {
-      const float base = m == -INFINITY ? 0.f : m;
+      const bool far = m > -INFINITY && fabsf(m * c) > kFar;
+      const float base = far ? m : 0.f;
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[b][i] -= base;
-      return -H::kShift;
+      if (far) return -H::kShift;
     }
     return (m == -INFINITY ? 0.f : m * c) - H::kShift;
   }

@@ -906,6 +906,29 @@ def test_attend_what_is_not_finite_in_some_splits(hvd, rows, D, dtype, cap):
     assert int(got.isfinite().sum()) == got.numel() - 2 * (4 * rows + 1) - 2 * rows * D - 2 * D
 
 
+@pytest.mark.parametrize("rows,ctx", [(2, 60), (5, 2500), (60, 30), (60, 2500)])
+@pytest.mark.parametrize("D,dtype", [(64, F16), (128, BF16), (200, F16), (256, BF16)])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+def test_attend_hidden_places_leave_every_bit(hvd, rows, ctx, D, dtype, cap):
+    """Rows have the same bits whatever lies before their documents, on other branches of
+    their tree or behind them."""
+    c = Case([(rows, ctx), (rows, 40)], 2, D, dtype=dtype, seed=rows + D, tree=rows < 65)
+    b = c.batch(hvd)
+    first = torch.full((c.T,), 33, dtype=torch.int32, device="cuda")
+    q = c.rnd(c.T, 6, D).to(dtype).cuda()
+    want = hvd.attend(q, c.k_cache, c.v_cache, b, cap=cap, first=first)
+    for cache, what in ((c.v_cache, math.nan), (c.v_cache, -math.inf), (c.k_cache, math.nan), (c.k_cache, math.inf), (c.k_cache, 3e4)):
+        for j in range(33):
+            cache[int(c.pages[0, j // 16]), :, j % 16] = what
+        assert torch.equal(hvd.attend(q, c.k_cache, c.v_cache, b, cap=cap, first=first), want)
+    # the last row's own value and key, which no other row sees
+    for cache, what in ((c.v_cache, math.inf), (c.k_cache, math.nan)):
+        j = ctx + rows - 1
+        cache[int(c.pages[0, j // 16]), :, j % 16] = what
+        got = hvd.attend(q, c.k_cache, c.v_cache, b, cap=cap, first=first)
+        assert torch.equal(got[:rows - 1], want[:rows - 1]) and torch.equal(got[rows:], want[rows:])
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("rows", [(1, 3), (2, 60)])
 def test_adjust_in_place_of_strided_logits_writes_nothing_else(hvd, dtype, rows):
