@@ -532,7 +532,8 @@ hvd_status hvd_append_kv(const hvd_row_batch* batch, const hvd_paged_kv* kv, con
  * out = sum exp(x) v / sum exp(x), 0 for a row that sees no key (or whose scores
  * are all -inf) and for rows of no sequence.  What a key or value holds that a
  * row does not see does not reach it, infinities and NaNs included.  Scores past
- * 2^125 count as infinite (one of +inf makes its row a NaN).  q and out
+ * 2^125 count as infinite (one of +inf makes its row a NaN), and values past
+ * 2^96 may overflow the sums.  q and out
  * have the cache's type; scores, sums and outputs are 32-bit, weights are
  * rounded to the cache's type for the product with the values (one that rounds to
  * 0, from 2^-32 of the row's largest down in fp16, takes no infinity along). */

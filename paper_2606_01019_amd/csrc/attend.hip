@@ -38,7 +38,6 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kLazy = 8.f;     // the running maximum may lag by this (base 2)
 constexpr float kFar = 4096.f;   // larger maxima are taken off the scores themselves (base 2)
 constexpr float kCancels = 64.f;
 constexpr int kNoKey = 0x7fffffff;
@@ -48,6 +47,7 @@ struct Half;
 template <>
 struct Half<false> {
   static constexpr float kShift = 7.f;
+  static constexpr float kLazy = 8.f;  // the running maximum may lag by this (base 2): weights stay below 2^16
   static constexpr uint32_t kInf = 0x04000400u;  // 0x8000 - the exponent of infinities and NaNs
   __device__ static f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -57,6 +57,7 @@ struct Half<false> {
 template <>
 struct Half<true> {
   static constexpr float kShift = 0.f;
+  static constexpr float kLazy = 16.f;  // (bits do not depend on it; packed prompts of 256-wide heads with a bias 172 us, with 8 177)
   static constexpr uint32_t kInf = 0x00800080u;
   __device__ static f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -549,9 +550,11 @@ struct Wave {
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
     top = other_half_max(top);
     // The maximum lags until a weight would pass 2^kLazy: most tiles rescale nothing
-    if (__builtin_amdgcn_ballot_w64(EXACT && fabsf(m * c) > kFar ? (top - m) * c > kLazy : top * c > m * c + kLazy)) {
+    // (a column's own scores alone decide: what other rows see leaves its bits)
+    const bool lags = EXACT && fabsf(m * c) > kFar ? (top - m) * c > H::kLazy : top * c > m * c + H::kLazy;
+    if (__builtin_amdgcn_ballot_w64(lags)) {
       if constexpr (APART) keep_apart();
-      const float mn = fmaxf(m, top);
+      const float mn = lags ? top : m;
       const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * c);
       l *= f;
 #pragma unroll

@@ -906,12 +906,26 @@ def test_attend_what_is_not_finite_in_some_splits(hvd, rows, D, dtype, cap):
     assert int(got.isfinite().sum()) == got.numel() - 2 * (4 * rows + 1) - 2 * rows * D - 2 * D
 
 
+@pytest.mark.parametrize("rows,ctx", [(1, 60), (1, 5000), (60, 30), (150, 2500)])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("power", [96, -96])
+def test_attend_values_of_any_size(hvd, rows, ctx, D, power):
+    """Powers of two scale bfloat16 results exactly, with a bias that has the maximum rise
+    from tile to tile."""
+    c = Case([(rows, ctx)], 2, D, dtype=BF16, seed=rows + D)
+    q, slopes = c.rnd(c.T, 4, D).to(BF16).cuda(), torch.tensor([0.5, 0.25, 0.02, 0.0], device="cuda")
+    want = hvd.attend(q, c.k_cache, c.v_cache, c.batch(hvd), slopes=slopes)
+    c.v_cache.mul_(2.0 ** power)
+    got = hvd.attend(q, c.k_cache, c.v_cache, c.batch(hvd), slopes=slopes)
+    assert torch.equal(got.double(), want.double() * 2.0 ** power)
+
+
 @pytest.mark.parametrize("rows,ctx", [(2, 60), (5, 2500), (60, 30), (60, 2500)])
 @pytest.mark.parametrize("D,dtype", [(64, F16), (128, BF16), (200, F16), (256, BF16)])
 @pytest.mark.parametrize("cap", [0.0, 20.0])
 def test_attend_hidden_places_leave_every_bit(hvd, rows, ctx, D, dtype, cap):
     """Rows have the same bits whatever lies before their documents, on other branches of
-    their tree or behind them."""
+    their tree or behind them, and however large the scores of other rows are."""
     c = Case([(rows, ctx), (rows, 40)], 2, D, dtype=dtype, seed=rows + D, tree=rows < 65)
     b = c.batch(hvd)
     first = torch.full((c.T,), 33, dtype=torch.int32, device="cuda")
@@ -922,7 +936,7 @@ def test_attend_hidden_places_leave_every_bit(hvd, rows, ctx, D, dtype, cap):
             cache[int(c.pages[0, j // 16]), :, j % 16] = what
         assert torch.equal(hvd.attend(q, c.k_cache, c.v_cache, b, cap=cap, first=first), want)
     # the last row's own value and key, which no other row sees
-    for cache, what in ((c.v_cache, math.inf), (c.k_cache, math.nan)):
+    for cache, what in ((c.v_cache, math.inf), (c.k_cache, 3e4), (c.k_cache, math.nan)):
         j = ctx + rows - 1
         cache[int(c.pages[0, j // 16]), :, j % 16] = what
         got = hvd.attend(q, c.k_cache, c.v_cache, b, cap=cap, first=first)
