@@ -989,3 +989,68 @@ def test_batches_that_are_none_reach_no_other_memory(hvd, starts, lengths, tree)
                       frequency=torch.ones(2, device="cuda"), out=wide[3:-3, 5:105])
     wide[3:-3, 5:105] = 7
     assert bool((wide == 7).all())
+
+
+# ------------------------------------------------------------------- the limits
+
+def test_the_longest_sequence(hvd):
+    """2^29 keys on 2^19 pages.  Equal scores: every result is a count over a count, both
+    exact in 32 bits."""
+    n_pages, page = 1 << 19, 1024
+    L = n_pages * page
+    ids = torch.randperm(n_pages, device="cuda").to(torch.int32)
+    kc, vc = (torch.zeros(n_pages, 1, page, 8, dtype=F16, device="cuda") for _ in range(2))
+    vc[ids[n_pages // 4 * 3:].long(), ..., 0] = 1.0
+    vc[ids[:2].long(), ..., 1] = 1.0
+    b = hvd.RowBatch(ints([0, 2]), ints([L]), ids[None])
+    new = torch.zeros(2, 1, 8, device="cuda")
+    new[:, :, 2] = 1.0
+    freqs = torch.tensor([0.25], dtype=torch.float64, device="cuda")
+    hvd.append_kv(kc, vc, new, new, b, freqs=freqs)
+    at = int(ids[-1])
+    assert torch.equal(vc[at, 0, -2:], new[:, 0].to(F16)) and torch.equal(kc[at, 0, -2:], new[:, 0].to(F16))
+    assert not kc[at, 0, -3].any() and not kc[:, 0, 0].any()
+    q = torch.zeros(2, 2, 8, dtype=F16, device="cuda")
+    got = hvd.attend(q, kc, vc, b)
+    for row in range(2):
+        seen = L - 1 + row
+        count = torch.tensor([L // 4 - 2, 2 * page, 1 + row], dtype=torch.float64)
+        want = torch.where(count / seen < 2.0 ** -25, 0.0, count / seen).half().cuda()
+        assert torch.equal(got[row, :, :3], want.expand(2, 3)), (got[row, :, :3], want)
+    got = hvd.attend(q, kc, vc, b, window=7)
+    want = torch.tensor([[6 / 7, 0, 1 / 7], [5 / 7, 0, 2 / 7]], dtype=torch.float64).half().cuda()
+    assert torch.equal(got[:, 0, :3], want)
+    got = hvd.attend(q, kc, vc, b, first=ints([0, L - 3]))
+    assert torch.equal(got[1, 0, :3], torch.tensor([1 / 3, 0, 2 / 3], dtype=torch.float64).half().cuda())
+
+
+def test_the_most_rows(hvd):
+    """2^20 rows of 4096 sequences."""
+    S, n, D = 4096, 256, 8
+    T = S * n
+    g = torch.Generator("cuda").manual_seed(1)
+    k, v, q = (torch.randn(T, 1, D, generator=g, device="cuda").to(BF16) for _ in range(3))
+    kc, vc = (torch.full((S * n // 16, 1, 16, D), 9.0, dtype=BF16, device="cuda") for _ in range(2))
+    pages = torch.randperm(S * n // 16, generator=g, device="cuda").to(torch.int32).view(S, n // 16)
+    b = hvd.RowBatch(torch.arange(0, T + 1, n, dtype=torch.int32, device="cuda"), torch.full((S,), n, dtype=torch.int32, device="cuda"), pages)
+    hvd.append_kv(kc, vc, k, v, b)
+    assert torch.equal(kc[pages.flatten().long()].view(T, 1, D), k) and torch.equal(vc[pages.flatten().long()].view(T, 1, D), v)
+    got = hvd.attend(q, kc, vc, b).view(S, n, D).double()
+    u, seen = 2.0 ** -8, torch.ones(n, n, device="cuda", dtype=torch.bool).tril()
+    for s in range(0, S, 512):
+        K, V, Q = (t.view(S, n, D)[s:s + 512].double() for t in (k, v, q))
+        KT = K.transpose(1, 2).contiguous()
+        x = torch.bmm(Q, KT) * D ** -0.5
+        big = (torch.bmm(Q.abs(), KT.abs()) * D ** -0.5).masked_fill(~seen, 0).amax(2, keepdim=True)
+        d = (D + 8) * 2.0 ** -23 * big + 8 * 2.0 ** -23 * x.masked_fill(~seen, 0).abs().amax(2, keepdim=True)
+        p = torch.softmax(x.masked_fill(~seen, -math.inf), 2)
+        o, A = torch.bmm(p, V), torch.bmm(p, V.abs())
+        tol = 1.02 * (u * o.abs() + (u + 2 * d + n * 2.0 ** -23) * A + n * 2.0 ** -32 * V.abs().amax(1, keepdim=True))
+        assert bool(((got[s:s + 512] - o).abs() <= tol).all())
+    T, V = 65536, 35
+    l = torch.randn(T, V, generator=g, device="cuda")
+    toks = torch.randint(0, V, (T,), generator=g, device="cuda", dtype=torch.int32)
+    # a sequence of all rows: each token counts for the rows after it
+    out, best = hvd.adjust_logits(l, hvd.RowBatch(ints([0, T])), tokens=toks, frequency=torch.full((1,), 2.0 ** -10, device="cuda"))
+    want = l - torch.nn.functional.one_hot(toks.long(), V).cumsum(0).float() * 2.0 ** -10
+    assert torch.equal(out, want) and torch.equal(best.long(), want.argmax(1))
